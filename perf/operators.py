@@ -92,7 +92,8 @@ def work(case):
     T = c["T"]
     if c["op"] == "route":
         one = T * c["E"] * z
-        return {"bytes": one + 8 * T * c["k"] + (c["backward"] and 2 * one + 8 * T * c["k"]), "flops": 4.0 * T * c["E"] * (2 if c["backward"] else 1)}
+        back = (1 if c["renorm"] else 2) * one + 8 * T * c["k"]      # over the chosen alone, only their logits are read again
+        return {"bytes": one + 8 * T * c["k"] + (back if c["backward"] else 0), "flops": 4.0 * T * c["E"] * (2 if c["backward"] else 1)}
     if c["op"] == "dispatch":
         n, kept = T * c["k"], T * c["k"] * (1.0 - c["drop"])
         one = T * c["d"] * z + n * c["d"] * z + 12 * n
