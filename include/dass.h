@@ -63,7 +63,10 @@ typedef enum {
 } dass_status;
 
 typedef enum { DASS_BF16 = 0, DASS_F32 = 1 } dass_dtype;
-typedef enum { DASS_ACT_SILU = 0, DASS_ACT_GELU_TANH = 1, DASS_ACT_RELU = 2 } dass_act;
+typedef enum {
+    DASS_ACT_SILU = 0, DASS_ACT_GELU_TANH = 1, DASS_ACT_RELU = 2,
+    DASS_ACT_NONE = 3                                   /* dass_linear only */
+} dass_act;
 /* Which matrix axis an index runs along: ROWS = the row index varies, COLS = the column index varies. */
 typedef enum { DASS_AXIS_ROWS = 0, DASS_AXIS_COLS = 1 } dass_axis;
 
@@ -259,6 +262,82 @@ dass_status dass_mlp_forward(const void *X, int64_t T, int64_t ldx,
                              const void *Wd, int64_t ldd, dass_dtype dt, dass_act act,
                              void *Z, int64_t ldz,
                              void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* ------------------------------------------------------------------ mixture of experts
+ * (No counterpart in the paper, whose layers hold one GLU MLP.)  A layer of E such MLPs sends every token to k of them.
+ * These calls find an expert's tokens, lay them side by side, run them through that expert's (pruned) weights and put
+ * them back: route -> sort -> gather -> linear, linear -> combine.  The rows of one expert are a matrix in place, so
+ * dass_calib_accumulate and dass_prune_nm apply to each expert as they are.  The gradients of route, gather and combine
+ * are what tuning the router around fixed (pruned) experts needs.
+ *
+ * For these calls (and dass_linear): T = 0 is a valid request; row pointers need element alignment only and any pitch
+ * >= the row length is accepted, except where stated (16-byte aligned pointers, pitches and row lengths are faster);
+ * nothing past a row's last element is read or written; sums and softmax are in f32, in a fixed order (equal inputs give
+ * bit-equal results), with one rounding to `dt` at the end; inputs and outputs must not overlap except where stated.
+ * Device-side integers are not trusted: ids, slots and offsets out of range never lead outside a buffer.
+ */
+typedef enum { DASS_ROUTE_CHOSEN = 0, DASS_ROUTE_ALL = 1 } dass_route_norm;   /* what the weights' softmax runs over */
+
+/* The k experts with the highest logits of each token, highest first, equal logits in order of the lower index, and
+ *     weight[t,j] = exp(l_j - m) / sum exp(l_i - m),    m = the row's largest logit,
+ * the sum over the k chosen (DASS_ROUTE_CHOSEN) or over all experts (DASS_ROUTE_ALL).  A logit of -inf or NaN masks the
+ * expert: it is never chosen and has no part in the sum; +inf counts as the largest finite f32.  Where fewer than k
+ * experts are unmasked the remaining places hold expert -1, weight 0 (a row with none: all places).
+ * logits [T x E, ld] in `dt`; expert [T x k] int32; weight [T x k] f32.  E <= 1024, k <= min(E, 32).
+ * Errors: NULL / DTYPE / SHAPE / UNSUPPORTED (E > 1024, k > 32) / ALIGN / CUDA. */
+dass_status dass_route_topk(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, int k, dass_route_norm norm,
+                            int32_t *expert, float *weight, void *cuda_stream);
+/* dlogits from dweight [T x k] f32: with p the softmax above (0 for what it leaves out) and
+ * s = sum_j weight[t,j] dweight[t,j]:  dlogits[t,e] = p_e ((dweight[t,j] if e is expert[t,j], else 0) - s).
+ * Everything else is recomputed from `logits` and `expert` (dass_route_topk's; entries outside [0, E) are skipped, the
+ * ids of a row are distinct).  dlogits [T x E, ldd] in `dt` is written in full. */
+dass_status dass_route_topk_backward(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, int k, dass_route_norm norm,
+                                     const int32_t *expert, const float *dweight, void *dlogits, int64_t ldd, void *cuda_stream);
+
+/* The stable order by expert of the T * k choices (flat index f = t * k + j): rows offsets[e] .. offsets[e+1] - 1 of the
+ * sorted side belong to expert e, in ascending f.  Choices outside [0, E) are dropped.
+ * offsets [E + 1]; slot [T x k]: the row of choice (t,j), or -1; source [T * k] (nullable): the f of a row, -1 past
+ * offsets[E].  workspace: dass_expert_sort_workspace_bytes(...) bytes (may be 0), 16-byte aligned.  E <= 1024, k <= 32.
+ * Errors: NULL / SHAPE / UNSUPPORTED / ALIGN / WORKSPACE / CUDA. */
+dass_status dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t E, size_t *bytes /* HOST */);
+dass_status dass_expert_sort(const int32_t *expert, int64_t T, int64_t k, int64_t E, int32_t *offsets, int32_t *slot, int32_t *source,
+                             void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Xs[slot[t,j],:] = weight[t,j] * X[t,:]  (weight null: a copy).  X [T x d, ldx], Xs [rows x d, ldxs].  Slots outside
+ * [0, rows) are skipped.  rows_used (nullable, device): rows from *rows_used on are written as zeros -- offsets + E of
+ * dass_expert_sort; without it rows that no slot names are left alone.
+ * The gradient of the copy is dass_expert_combine of dXs without weights.
+ * Errors: NULL / DTYPE / SHAPE / UNSUPPORTED (k > 32) / ALIGN / CUDA. */
+dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx, dass_dtype dt, const int32_t *slot, int64_t k,
+                               const float *weight, const int32_t *rows_used, void *Xs, int64_t rows, int64_t ldxs, void *cuda_stream);
+/* Y[t,:] = residual[t,:] + sum_j weight[t,j] * Ys[slot[t,j],:]   (weight null: 1; residual null: 0; slots outside
+ * [0, rows): nothing).  Y may be the residual itself. */
+dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t ldys, dass_dtype dt, const int32_t *slot, int64_t T,
+                                int64_t k, const float *weight, const void *residual, int64_t ldr, void *Y, int64_t ldy, void *cuda_stream);
+/* Gradients of the weighted sum: dYs[slot[t,j],:] = weight[t,j] * dY[t,:] (weight null: 1) and, in f32,
+ * dweight[t,j] = sum_c dY[t,c] * Ys[slot[t,j],c] (0 for a skipped slot); each nullable, at least one required.
+ * rows_used as for dass_expert_gather (applies to dYs; with T = 0 nothing is written).  The residual's gradient is dY. */
+dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, int64_t lddy, const void *Ys, int64_t rows, int64_t ldys,
+                                         dass_dtype dt, const int32_t *slot, int64_t k, const float *weight, const int32_t *rows_used,
+                                         void *dYs, int64_t lddys, float *dweight, void *cuda_stream);
+
+/* Matrix product with its epilogue, dense or per expert:
+ *     Y = act(X W^T + bias) [ * (X W_up^T + bias_up) ] + residual          one rounding to `dt`, at Y
+ * X [T x K, ldx], W (and W_up, nullable: the GLU form) [N x K, ldw], bias / bias_up [N] in `dt`, nullable, residual
+ * [T x N, ldr], nullable, Y [T x N, ldy].  act: any dass_act.  Y may be the residual itself (same pitch).
+ * offsets (device, groups + 1 values, nullable): rows offsets[g] .. offsets[g+1] - 1 use group g's matrices W + g *
+ * group_stride (elements), W_up + g * group_stride and row g of bias / bias_up [groups x N]; rows of no group are
+ * written as zeros.  Null: groups = 1, all rows.
+ * bf16: tensor cores, f32 accumulators; f32: f32 FMAs.  X, W and W_up 16-byte aligned with pitches (and group_stride) of
+ * whole 16 bytes, as everywhere in this header; bias, residual and Y need element alignment only.
+ * Waits inside the tensor-core kernels are bounded (2 s); dass_linear_status waits for `cuda_stream` and returns
+ * DASS_ERR_TIMEOUT if one ran out on the current device since the last query (outputs of that call are then
+ * incomplete; the context stays usable), else DASS_OK, and clears the record.
+ * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (extents beyond 32-bit coordinates, groups > 65535) / CUDA. */
+dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const void *W, const void *W_up, int64_t N, int64_t ldw,
+                        int64_t group_stride, const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,
+                        void *Y, int64_t ldy, dass_dtype dt, const int32_t *offsets, int64_t groups, void *cuda_stream);
+dass_status dass_linear_status(void *cuda_stream);
 
 /* ------------------------------------------------------------------ checked-access build
  * (No counterpart in the paper: the stand-in for a memory sanitizer.)  libdass_check.so is this library compiled with

@@ -19,8 +19,9 @@ LIB_PATH = os.path.join(_PKG, "libdass.so")
 
 OK = 0
 BF16, F32 = 0, 1
-ACT_SILU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2
+ACT_SILU, ACT_GELU_TANH, ACT_RELU, ACT_NONE = 0, 1, 2, 3      # ACT_NONE: linear() only
 AXIS_ROWS, AXIS_COLS = 0, 1
+ROUTE_CHOSEN, ROUTE_ALL = 0, 1
 ACT_BY_NAME = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "relu": ACT_RELU}
 
 EXPORTS = (
@@ -29,6 +30,8 @@ EXPORTS = (
     "dass_score_nm", "dass_compress_nm", "dass_prune_nm", "dass_prune_status", "dass_select_workspace_bytes", "dass_select_unstructured",
     "dass_selftest_wait_timeout", "dass_feature_workspace_bytes", "dass_feature_sumsq",
     "dass_mlp_forward_workspace_bytes", "dass_mlp_forward",
+    "dass_route_topk", "dass_route_topk_backward", "dass_expert_sort_workspace_bytes", "dass_expert_sort",
+    "dass_expert_gather", "dass_expert_combine", "dass_expert_combine_backward", "dass_linear", "dass_linear_status",
     "dass_bounds_report", "dass_bounds_shrink_next",
     "dass_status_string", "dass_version",
 )
@@ -115,6 +118,25 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.dass_mlp_forward.restype = ctypes.c_int
     lib.dass_mlp_forward.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, vp, i64, ctypes.c_int, ctypes.c_int,
                                      vp, i64, vp, sz, vp]
+    ci = ctypes.c_int
+    lib.dass_route_topk.restype = ci
+    lib.dass_route_topk.argtypes = [vp, i64, i64, i64, ci, ci, ci, vp, vp, vp]
+    lib.dass_route_topk_backward.restype = ci
+    lib.dass_route_topk_backward.argtypes = [vp, i64, i64, i64, ci, ci, ci, vp, vp, vp, i64, vp]
+    lib.dass_expert_sort_workspace_bytes.restype = ci
+    lib.dass_expert_sort_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+    lib.dass_expert_sort.restype = ci
+    lib.dass_expert_sort.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.dass_expert_gather.restype = ci
+    lib.dass_expert_gather.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, vp, vp, i64, i64, vp]
+    lib.dass_expert_combine.restype = ci
+    lib.dass_expert_combine.argtypes = [vp, i64, i64, i64, ci, vp, i64, i64, vp, vp, i64, vp, i64, vp]
+    lib.dass_expert_combine_backward.restype = ci
+    lib.dass_expert_combine_backward.argtypes = [vp, i64, i64, i64, vp, i64, i64, ci, vp, i64, vp, vp, vp, i64, vp, vp]
+    lib.dass_linear.restype = ci
+    lib.dass_linear.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, i64, vp, vp, ci, vp, i64, vp, i64, ci, vp, i64, vp]
+    lib.dass_linear_status.restype = ci
+    lib.dass_linear_status.argtypes = [vp]
     lib.dass_status_string.restype = ctypes.c_char_p
     lib.dass_status_string.argtypes = [ctypes.c_int]
     lib.dass_version.restype = ctypes.c_int
@@ -476,3 +498,222 @@ def mlp_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.T
                                    workspace.data_ptr(), workspace.numel(), _stream(stream))
     _check(code, "dass_mlp_forward")
     return Z
+
+
+# ----------------------------------------------------------------------------- mixture of experts
+
+def _rows(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
+    """_matrix for calls that take any pitch: a single row, or none, has the pitch of its length."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a 2-D row-major tensor (unit stride along columns)")
+    rows, cols = t.shape
+    return rows, cols, t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _same(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> None:
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
+
+
+def _like(t: torch.Tensor, name: str, shape: Tuple[int, int], X: torch.Tensor) -> int:
+    """Checks a row-major matrix of X's dtype and device and returns its pitch."""
+    rows, cols, ld = _rows(t, name)
+    if (rows, cols) != shape or t.dtype != X.dtype or t.device != X.device:
+        raise ValueError(f"{name} must be a {X.dtype} matrix of shape {shape} on {X.device}")
+    return ld
+
+
+def route_topk(logits: torch.Tensor, k: int, renormalise: bool = True, expert: Optional[torch.Tensor] = None,
+               weight: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """The k experts with the highest logits of every row and their softmax weights: over the k chosen
+    (``renormalise``) or over all experts.  logits [T x E]; returns (expert int32 [T x k], weight float32 [T x k])."""
+    T, E, ld = _rows(logits, "logits")
+    k = int(k)
+    if expert is None:
+        expert = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+    if weight is None:
+        weight = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    _same(expert, "expert", (T, k), torch.int32, logits.device)
+    _same(weight, "weight", (T, k), torch.float32, logits.device)
+    dt = _dtype_code(logits)
+    if T:
+        _check(load().dass_route_topk(logits.data_ptr(), T, E, ld, dt, k, ROUTE_CHOSEN if renormalise else ROUTE_ALL,
+                                      expert.data_ptr(), weight.data_ptr(), _stream(stream)), "dass_route_topk")
+    return expert, weight
+
+
+def route_topk_backward(logits: torch.Tensor, expert: torch.Tensor, dweight: torch.Tensor, renormalise: bool = True,
+                        dlogits: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The logits' gradient [T x E] from that of route_topk's weights (``expert`` as it returned them)."""
+    T, E, ld = _rows(logits, "logits")
+    k = expert.shape[1] if expert.dim() == 2 else -1
+    _same(expert, "expert", (T, k), torch.int32, logits.device)
+    _same(dweight, "dweight", (T, k), torch.float32, logits.device)
+    if dlogits is None:
+        dlogits = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    ldd = _like(dlogits, "dlogits", (T, E), logits)
+    dt = _dtype_code(logits)
+    if T:
+        _check(load().dass_route_topk_backward(logits.data_ptr(), T, E, ld, dt, k, ROUTE_CHOSEN if renormalise else ROUTE_ALL,
+                                               expert.data_ptr(), dweight.data_ptr(), dlogits.data_ptr(), ldd, _stream(stream)),
+               "dass_route_topk_backward")
+    return dlogits
+
+
+def expert_sort_workspace_bytes(T: int, k: int, E: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().dass_expert_sort_workspace_bytes(int(T), int(k), int(E), ctypes.byref(out)), "dass_expert_sort_workspace_bytes")
+    return int(out.value)
+
+
+def expert_sort(expert: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = None, slot: Optional[torch.Tensor] = None,
+                source: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None):
+    """The stable order by expert of the choices ``expert`` [T x k] int32 (ids outside [0, E) are dropped).
+    Returns (offsets [E + 1], slot [T x k], source [T * k]), all int32: see dass_expert_sort."""
+    if expert.dim() != 2 or not expert.is_cuda:
+        raise ValueError("expert must be a 2-D CUDA tensor [T x k]")
+    (T, k), E, dev = expert.shape, int(E), expert.device
+    _same(expert, "expert", (T, k), torch.int32, dev)
+    if offsets is None:
+        offsets = torch.empty(max(E, 0) + 1, dtype=torch.int32, device=dev)
+    if slot is None:
+        slot = torch.empty((T, k), dtype=torch.int32, device=dev)
+    if source is None:
+        source = torch.empty(T * k, dtype=torch.int32, device=dev)
+    _same(offsets, "offsets", (max(E, 0) + 1,), torch.int32, dev)
+    _same(slot, "slot", (T, k), torch.int32, dev)
+    _same(source, "source", (T * k,), torch.int32, dev)
+    if workspace is None:
+        need = expert_sort_workspace_bytes(T, k, E)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check(load().dass_expert_sort(expert.data_ptr(), T, k, E, offsets.data_ptr(), slot.data_ptr(), source.data_ptr(),
+                                   _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)),
+           "dass_expert_sort")
+    return offsets, slot, source
+
+
+def _slots(slot: torch.Tensor, weight: Optional[torch.Tensor], device: torch.device) -> Tuple[int, int]:
+    if slot.dim() != 2:
+        raise ValueError("slot must be the [T x k] tensor expert_sort returned")
+    T, k = slot.shape
+    _same(slot, "slot", (T, k), torch.int32, device)
+    if weight is not None:
+        _same(weight, "weight", (T, k), torch.float32, device)
+    return T, k
+
+
+def _rows_used(offsets: Optional[torch.Tensor], device: torch.device) -> Optional[int]:
+    if offsets is None:
+        return None
+    _same(offsets, "offsets", (offsets.numel(),), torch.int32, device)
+    return offsets.data_ptr() + 4 * (offsets.numel() - 1)
+
+
+def expert_gather(X: torch.Tensor, slot: torch.Tensor, offsets: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                  Xs: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Xs[slot[t,j]] = (weight[t,j] *) X[t], [T * k x d] unless ``Xs`` is given.  With ``offsets`` the rows past the
+    last expert's are zeroed; without them rows that no slot names keep what they held."""
+    Tx, d, ldx = _rows(X, "X")
+    T, k = _slots(slot, weight, X.device)
+    if Tx != T:
+        raise ValueError("X and slot must have the same number of tokens")
+    if Xs is None:
+        Xs = torch.empty((T * k, d), dtype=X.dtype, device=X.device)
+    rows = Xs.shape[0]
+    ldxs = _like(Xs, "Xs", (rows, d), X)
+    _check(load().dass_expert_gather(X.data_ptr(), T, d, ldx, _dtype_code(X), slot.data_ptr(), k, _ptr(weight),
+                                     _rows_used(offsets, X.device), Xs.data_ptr(), rows, ldxs, _stream(stream)), "dass_expert_gather")
+    return Xs
+
+
+def expert_combine(Ys: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y[t] = residual[t] + sum_j weight[t,j] * Ys[slot[t,j]]  (``Y`` may be the residual itself)."""
+    rows, d, ldys = _rows(Ys, "Ys")
+    T, k = _slots(slot, weight, Ys.device)
+    ldr = _like(residual, "residual", (T, d), Ys) if residual is not None else 0
+    if Y is None:
+        Y = torch.empty((T, d), dtype=Ys.dtype, device=Ys.device)
+    ldy = _like(Y, "Y", (T, d), Ys)
+    _check(load().dass_expert_combine(Ys.data_ptr(), rows, d, ldys, _dtype_code(Ys), slot.data_ptr(), T, k, _ptr(weight),
+                                      _ptr(residual), ldr, Y.data_ptr(), ldy, _stream(stream)), "dass_expert_combine")
+    return Y
+
+
+def expert_gather_backward(dXs: torch.Tensor, slot: torch.Tensor, dX: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of the (unweighted) gather: dX[t] = sum_j dXs[slot[t,j]]."""
+    return expert_combine(dXs, slot, Y=dX, stream=stream)
+
+
+def expert_combine_backward(dY: torch.Tensor, Ys: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                            offsets: Optional[torch.Tensor] = None, dYs: Optional[torch.Tensor] = None,
+                            dweight: Optional[torch.Tensor] = None, want_rows: bool = True, want_weight: bool = True,
+                            stream: Optional[torch.cuda.Stream] = None):
+    """Gradients of expert_combine: (dYs [rows x d] or None, dweight float32 [T x k] or None).  With ``offsets`` the
+    rows of dYs past the last expert's are zeroed."""
+    Ty, d, lddy = _rows(dY, "dY")
+    T, k = _slots(slot, weight, dY.device)
+    rows = Ys.shape[0]
+    ldys = _like(Ys, "Ys", (rows, d), dY)
+    if Ty != T:
+        raise ValueError("dY and slot must have the same number of tokens")
+    if dYs is None and want_rows:
+        dYs = torch.empty((rows, d), dtype=dY.dtype, device=dY.device)
+    lddys = _like(dYs, "dYs", (rows, d), dY) if dYs is not None else 0
+    if dweight is None and want_weight:
+        dweight = torch.empty((T, k), dtype=torch.float32, device=dY.device)
+    if dweight is not None:
+        _same(dweight, "dweight", (T, k), torch.float32, dY.device)
+    dt = _dtype_code(dY)
+    if T:
+        _check(load().dass_expert_combine_backward(dY.data_ptr(), T, d, lddy, Ys.data_ptr(), rows, ldys, dt, slot.data_ptr(), k,
+                                                   _ptr(weight), _rows_used(offsets, dY.device), _ptr(dYs), lddys, _ptr(dweight),
+                                                   _stream(stream)), "dass_expert_combine_backward")
+    return dYs, dweight
+
+
+def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+           W_up: Optional[torch.Tensor] = None, bias_up: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+           offsets: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y = act(X W^T + bias) [* (X W_up^T + bias_up)] + residual, rounded once to X's dtype.
+
+    Dense: X [T x K], W (and W_up) [N x K], bias [N].  Per expert, with ``offsets`` (expert_sort's, on the device): W
+    (and W_up) [G x N x K], bias [G x N]; rows offsets[g] .. offsets[g+1]-1 use matrix g, rows of no expert give zeros.
+    ``Y`` may be the residual itself."""
+    T, K, ldx = _rows(X, "X")
+    dims = 2 if offsets is None else 3
+    if W.dim() != dims or W.shape[-1] != K or W.dtype != X.dtype or W.device != X.device or (K > 1 and W.stride(-1) != 1):
+        raise ValueError(f"W must be a row-major {'[N x K]' if dims == 2 else '[G x N x K]'} tensor of X's dtype and device")
+    N, groups = W.shape[-2], W.shape[0] if dims == 3 else 1
+    ldw = W.stride(-2) if N > 1 else max(W.stride(-2), K)
+    group_stride = W.stride(0) if dims == 3 else 0
+    if W_up is not None and (W_up.shape != W.shape or W_up.stride() != W.stride() or W_up.dtype != X.dtype or W_up.device != X.device):
+        raise ValueError("W_up must have W's shape, strides, dtype and device")
+    for t, name in ((bias, "bias"), (bias_up, "bias_up")):
+        if t is not None:
+            _same(t, name, (N,) if dims == 2 else (groups, N), X.dtype, X.device)
+    if bias_up is not None and W_up is None:
+        raise ValueError("bias_up goes with W_up")
+    if offsets is not None:
+        _same(offsets, "offsets", (groups + 1,), torch.int32, X.device)
+    ldr = _like(residual, "residual", (T, N), X) if residual is not None else 0
+    if Y is None:
+        Y = torch.empty((T, N), dtype=X.dtype, device=X.device)
+    ldy = _like(Y, "Y", (T, N), X)
+    dt = _dtype_code(X)
+    if T:
+        _check(load().dass_linear(X.data_ptr(), T, K, ldx, W.data_ptr(), _ptr(W_up), N, ldw, group_stride, _ptr(bias), _ptr(bias_up),
+                                  int(act), _ptr(residual), ldr, Y.data_ptr(), ldy, dt, _ptr(offsets), groups, _stream(stream)),
+               "dass_linear")
+    return Y
+
+
+def linear_status(stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Waits for the stream and raises if a bounded wait inside a linear kernel ran out since the last query."""
+    _check(load().dass_linear_status(_stream(stream)), "dass_linear_status")

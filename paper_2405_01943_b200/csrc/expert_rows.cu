@@ -1,0 +1,475 @@
+// Token rows sorted by expert and back: the order itself (a stable counting sort of the expert ids), the copy into it,
+// the weighted sum out of it, and the gradients of both.
+//
+// The order: flat index f = t * k + j; expert e's rows are those f with id e, ascending.  The ids are cut into one run
+// per block.  Pass 1 counts each run's ids per expert.  Pass 2 adds up, for its own run, what the runs before it hold
+// of every expert and what all runs hold of the experts before, counts again per warp, and then every warp walks its
+// part 32 ids at a time: __match_any finds the lanes with the same expert, their order inside the warp is the rank.
+// Nothing depends on the order in which blocks or atomics run.  A short list is one run and needs no pass 1.
+//
+// The rows: a thread owns 16 bytes of a token's row and reads it once for all k copies (gather), or reads the k
+// sources and sums them in f32 in j order (combine).  All of it is bound by memory: the row bytes in and out.
+#include "rows_common.cuh"
+
+namespace dass {
+
+int device_sm_count();   // dass_abi.cu
+
+constexpr int ER_MAX_E = 1024;
+constexpr int ER_MAX_K = 32;
+constexpr int ER_SORT_THREADS = 256;
+constexpr int ER_SORT_WARPS = ER_SORT_THREADS / 32;
+constexpr int64_t ER_ONE_RUN = 4096;           // ids that one block sorts alone
+
+static int64_t er_runs(int64_t n)
+{
+    if (n <= ER_ONE_RUN) return 1;
+    const int64_t most = device_sm_count();
+    const int64_t want = (n + 1023) / 1024;    // runs of 1024 ids at least: 4 steps of a warp
+    return want < most ? want : most;
+}
+
+// counts[run][e]
+__global__ void __launch_bounds__(ER_SORT_THREADS)
+expert_count_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len, int E, int32_t *__restrict__ counts)
+{
+    extern __shared__ int32_t er_smem[];
+    for (int e = threadIdx.x; e < E; e += blockDim.x) er_smem[e] = 0;
+    __syncthreads();
+    const int64_t f0 = blockIdx.x * run_len, f1 = f0 + run_len < n ? f0 + run_len : n;
+    for (int64_t f = f0 + threadIdx.x; f < f1; f += blockDim.x) {
+        const int id = DASS_LD(ids + f);
+        if (id >= 0 && id < E) atomicAdd(&er_smem[id], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) DASS_ST(counts + (int64_t)blockIdx.x * E + e, er_smem[e]);
+}
+
+__global__ void __launch_bounds__(ER_SORT_THREADS)
+expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len, int runs, int E, const int32_t *__restrict__ counts,
+                    int32_t *__restrict__ offsets, int32_t *__restrict__ slot, int32_t *__restrict__ source)
+{
+    extern __shared__ int32_t er_smem[];
+    int32_t *before = er_smem;                              // [E] rows of earlier runs, then this run's first rank
+    int32_t *total = er_smem + E;                           // [E] rows of all runs, then the experts' offsets
+    int32_t *mine = er_smem + 2 * E;                        // [warps][E] this run's counts by warp, then next ranks
+    __shared__ int32_t warp_sum[ER_SORT_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t f0 = blockIdx.x * run_len, f1 = f0 + run_len < n ? f0 + run_len : n;
+    const int64_t part = ((f1 - f0 + ER_SORT_WARPS - 1) / ER_SORT_WARPS + 31) / 32 * 32;
+    const int64_t w0 = f0 + warp * part, w1 = w0 + part < f1 ? w0 + part : f1;
+
+    for (int e = threadIdx.x; e < E * ER_SORT_WARPS; e += blockDim.x) mine[e] = 0;
+    for (int e = threadIdx.x; e < 2 * E; e += blockDim.x) er_smem[e] = 0;
+    __syncthreads();
+    for (int64_t f = w0 + lane; f < w1; f += 32) {
+        const int id = DASS_LD(ids + f);
+        if (id >= 0 && id < E) atomicAdd(&mine[warp * E + id], 1);
+    }
+    if (runs > 1) {
+        // threads are laid over experts and, where there are fewer experts than threads, over slices of the runs
+        const int width = E < ER_SORT_THREADS ? E : ER_SORT_THREADS;
+        const int slices = ER_SORT_THREADS / width;
+        const int slice = threadIdx.x / width;
+        if (slice < slices)
+            for (int e = threadIdx.x % width; e < E; e += width) {
+                int32_t b = 0, a = 0;
+                for (int r = slice; r < runs; r += slices) {
+                    const int32_t c = DASS_LD(counts + (int64_t)r * E + e);
+                    a += c;
+                    b += r < (int)blockIdx.x ? c : 0;
+                }
+                atomicAdd(&total[e], a);                    // integer sums: any order gives the same
+                atomicAdd(&before[e], b);
+            }
+    }
+    __syncthreads();
+    if (runs == 1) {
+        for (int e = threadIdx.x; e < E; e += blockDim.x) {
+            int32_t a = 0;
+            for (int w = 0; w < ER_SORT_WARPS; ++w) a += mine[w * E + e];
+            total[e] = a;
+        }
+        __syncthreads();
+    }
+    // exclusive scan of total over the experts, a block's width at a time
+    int32_t carry = 0;
+    for (int e0 = 0; e0 < E; e0 += ER_SORT_THREADS) {
+        const int e = e0 + threadIdx.x;
+        const int32_t v = e < E ? total[e] : 0;
+        int32_t inc = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t up = __shfl_up_sync(FULL_MASK, inc, o);
+            inc += lane >= o ? up : 0;
+        }
+        if (lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        int32_t base = carry, chunk = 0;
+#pragma unroll
+        for (int w = 0; w < ER_SORT_WARPS; ++w) {
+            const int32_t s = warp_sum[w];
+            base += w < warp ? s : 0;
+            chunk += s;
+        }
+        const int32_t at = base + inc - v;
+        if (e < E) {
+            if (blockIdx.x == 0) DASS_ST(offsets + e, at);
+            int32_t next = at + before[e];
+            for (int w = 0; w < ER_SORT_WARPS; ++w) {       // first rank of every warp's part
+                const int32_t c = mine[w * E + e];
+                mine[w * E + e] = next;
+                next += c;
+            }
+        }
+        carry += chunk;
+        __syncthreads();
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) DASS_ST(offsets + E, carry);
+    for (int64_t f = f0 + threadIdx.x; f < f1; f += blockDim.x)
+        if (source && f >= carry) DASS_ST(source + f, -1);
+    for (int64_t fb = w0; fb < w1; fb += 32) {
+        const int64_t f = fb + lane;
+        int id = f < w1 ? DASS_LD(ids + f) : -1;
+        if (id < 0 || id >= E) id = -1;
+        const unsigned peers = __match_any_sync(FULL_MASK, id);
+        int32_t first = id >= 0 ? mine[warp * E + id] : 0;
+        __syncwarp();
+        const int rank = __popc(peers & ((1u << lane) - 1u));
+        if (id >= 0 && rank == 0) mine[warp * E + id] = first + __popc(peers);
+        __syncwarp();
+        if (f < w1) {
+            const int32_t s = id >= 0 ? first + rank : -1;
+            DASS_ST(slot + f, s);
+            if (source && s >= 0) DASS_ST(source + s, (int32_t)f);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ rows in
+struct ErRows {
+    int64_t T, d, rows;              // tokens, row length, rows of the sorted side
+    int k;
+    int64_t vpr;                     // accesses per row
+};
+
+constexpr int ER_THREADS = 256;
+
+// dst[slot[t,j]] = scale * src[t]; rows past *used are zeroed (used null: left alone)
+template <bool BF16, int VEC>
+__global__ void __launch_bounds__(ER_THREADS)
+expert_gather_kernel(const void *__restrict__ src, int64_t lds, const int32_t *__restrict__ slot, const float *__restrict__ weight,
+                     const int32_t *__restrict__ used, void *__restrict__ dst, int64_t ldd, ErRows r)
+{
+    const int64_t stride = (int64_t)gridDim.x * ER_THREADS;
+    const int64_t first = (int64_t)blockIdx.x * ER_THREADS + threadIdx.x;
+    for (int64_t i = first; i < r.T * r.vpr; i += stride) {
+        const int64_t t = i / r.vpr, col = (i - t * r.vpr) * VEC;
+        float v[VEC];
+        row_load<BF16, VEC>(src, t * lds + col, v);
+        for (int j = 0; j < r.k; ++j) {
+            const int64_t s = DASS_LD(slot + t * r.k + j);
+            if (s < 0 || s >= r.rows) continue;
+            if (weight) {
+                const float w = DASS_LD(weight + t * r.k + j);
+                float x[VEC];
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) x[c] = w * v[c];
+                row_store<BF16, VEC>(dst, s * ldd + col, x);
+            } else {
+                row_store<BF16, VEC>(dst, s * ldd + col, v);
+            }
+        }
+    }
+    if (!used) return;
+    int64_t end = DASS_LD(used);
+    end = end < 0 ? 0 : end;
+    float zero[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) zero[c] = 0.f;
+    for (int64_t i = first; i < (r.rows - end) * r.vpr; i += stride) {
+        const int64_t t = i / r.vpr;
+        row_store<BF16, VEC>(dst, (end + t) * ldd + (i - t * r.vpr) * VEC, zero);
+    }
+}
+
+// ------------------------------------------------------------------ rows out
+// out[t] = residual[t] + sum_j weight[t,j] * rows[slot[t,j]], f32, j ascending, one rounding
+template <bool BF16, int VEC>
+__global__ void __launch_bounds__(ER_THREADS)
+expert_combine_kernel(const void *__restrict__ rows, int64_t ldr, const int32_t *__restrict__ slot, const float *__restrict__ weight,
+                      const void *__restrict__ residual, int64_t ldres, void *__restrict__ out, int64_t ldo, ErRows r)
+{
+    const int64_t stride = (int64_t)gridDim.x * ER_THREADS;
+    for (int64_t i = (int64_t)blockIdx.x * ER_THREADS + threadIdx.x; i < r.T * r.vpr; i += stride) {
+        const int64_t t = i / r.vpr, col = (i - t * r.vpr) * VEC;
+        float acc[VEC];
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) acc[c] = 0.f;
+#pragma unroll 4
+        for (int j = 0; j < r.k; ++j) {
+            const int64_t s = DASS_LD(slot + t * r.k + j);
+            if (s < 0 || s >= r.rows) continue;
+            const float w = weight ? DASS_LD(weight + t * r.k + j) : 1.0f;
+            float v[VEC];
+            row_load<BF16, VEC>(rows, s * ldr + col, v);
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) acc[c] = fmaf(w, v[c], acc[c]);
+        }
+        if (residual) {
+            float v[VEC];
+            row_load<BF16, VEC>(residual, t * ldres + col, v);
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) acc[c] += v[c];
+        }
+        row_store<BF16, VEC>(out, t * ldo + col, acc);
+    }
+}
+
+// Gradient of the weighted sum: drows[slot[t,j]] = weight[t,j] * dout[t] and dweight[t,j] = <dout[t], rows[slot[t,j]]>.
+// One block of WARPS warps per token; ER_J choices at a time share a read of dout[t].
+constexpr int ER_J = 4;
+template <bool BF16, int VEC, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32)
+expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const void *__restrict__ rows, int64_t ldr,
+                               const int32_t *__restrict__ slot, const float *__restrict__ weight, const int32_t *__restrict__ used,
+                               void *__restrict__ drows, int64_t lddr, float *__restrict__ dweight, ErRows r)
+{
+    __shared__ float part[WARPS][ER_J];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t t = blockIdx.x;
+    for (int j0 = 0; j0 < r.k; j0 += ER_J) {
+        int64_t s[ER_J];
+        float w[ER_J], acc[ER_J];
+#pragma unroll
+        for (int q = 0; q < ER_J; ++q) {
+            s[q] = j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
+            if (s[q] >= r.rows) s[q] = -1;
+            w[q] = s[q] < 0 ? 0.f : (weight ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f);
+            acc[q] = 0.f;
+        }
+        for (int64_t i = threadIdx.x; i < r.vpr; i += WARPS * 32) {
+            float g[VEC];
+            row_load<BF16, VEC>(dout, t * ldo + i * VEC, g);
+#pragma unroll
+            for (int q = 0; q < ER_J; ++q) {
+                if (s[q] < 0) continue;
+                float v[VEC];
+                if (dweight) {
+                    row_load<BF16, VEC>(rows, s[q] * ldr + i * VEC, v);
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) acc[q] = fmaf(g[c], v[c], acc[q]);
+                }
+                if (drows) {
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) v[c] = w[q] * g[c];
+                    row_store<BF16, VEC>(drows, s[q] * lddr + i * VEC, v);
+                }
+            }
+        }
+        if (dweight) {
+#pragma unroll
+            for (int q = 0; q < ER_J; ++q) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) acc[q] += __shfl_xor_sync(FULL_MASK, acc[q], o);
+                if (lane == 0) part[warp][q] = acc[q];
+            }
+            __syncthreads();
+            if (threadIdx.x < ER_J && j0 + threadIdx.x < r.k) {
+                float sum = 0.f;
+                for (int x = 0; x < WARPS; ++x) sum += part[x][threadIdx.x];
+                DASS_ST(dweight + t * r.k + j0 + threadIdx.x, sum);
+            }
+            __syncthreads();
+        }
+    }
+    if (!drows || !used) return;
+    int64_t end = DASS_LD(used);
+    end = end < 0 ? 0 : end;
+    float zero[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) zero[c] = 0.f;
+    for (int64_t row = end + t; row < r.rows; row += r.T)
+        for (int64_t i = threadIdx.x; i < r.vpr; i += WARPS * 32) row_store<BF16, VEC>(drows, row * lddr + i * VEC, zero);
+}
+
+// ------------------------------------------------------------------ host side
+static unsigned er_grid(int64_t work)
+{
+    const int64_t blocks = (work + ER_THREADS - 1) / ER_THREADS;
+    const int64_t most = 1ll << 30;
+    return (unsigned)(blocks < 1 ? 1 : (blocks < most ? blocks : most));
+}
+
+static dass_status er_check(int64_t T, int64_t k, int64_t d, int dt)
+{
+    if (dt != DASS_BF16 && dt != DASS_F32) return DASS_ERR_DTYPE;
+    if (T < 0 || k < 1 || d < 1) return DASS_ERR_SHAPE;
+    if (k > ER_MAX_K || T * k > (1ll << 31) - 1 || T > (1ll << 31) - 1) return DASS_ERR_UNSUPPORTED;
+    return DASS_OK;
+}
+
+}  // namespace dass
+
+using namespace dass;
+
+extern "C" {
+
+dass_status dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t E, size_t *bytes)
+{
+    if (!bytes) return DASS_ERR_NULL;
+    if (T < 0 || k < 1 || E < 1) return DASS_ERR_SHAPE;
+    if (E > ER_MAX_E || k > ER_MAX_K || T > ((1ll << 31) - 1) / k) return DASS_ERR_UNSUPPORTED;
+    const int64_t runs = er_runs(T * k);
+    *bytes = runs > 1 ? (size_t)runs * (size_t)E * sizeof(int32_t) : 0;
+    return DASS_OK;
+}
+
+dass_status dass_expert_sort(const int32_t *expert, int64_t T, int64_t k, int64_t E, int32_t *offsets, int32_t *slot, int32_t *source,
+                             void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if ((!expert && T > 0) || !offsets || (!slot && T > 0)) return DASS_ERR_NULL;
+    size_t need = 0;
+    const dass_status qs = dass_expert_sort_workspace_bytes(T, k, E, &need);
+    if (qs != DASS_OK) return qs;
+    if (!elem_aligned(expert, false) || !elem_aligned(offsets, false) || !elem_aligned(slot, false) || !elem_aligned(source, false))
+        return DASS_ERR_ALIGN;
+    if (need && (!workspace || workspace_bytes < need)) return DASS_ERR_WORKSPACE;
+    if (need && (reinterpret_cast<uintptr_t>(workspace) & 15u)) return DASS_ERR_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int64_t n = T * k;
+    const int64_t runs = er_runs(n);
+    const int64_t run_len = (n + runs - 1) / runs;
+    DASS_BOUNDS_SCOPE(bs);
+    DASS_BOUNDS_ADD(bs, expert, (size_t)n * 4);
+    DASS_BOUNDS_ADD(bs, slot, (size_t)n * 4);
+    DASS_BOUNDS_ADD(bs, source, (size_t)n * 4);
+    DASS_BOUNDS_ADD(bs, offsets, (size_t)(E + 1) * 4);
+    DASS_BOUNDS_ADD(bs, workspace, need);
+    DASS_BOUNDS_COMMIT(bs, st);
+    int32_t *counts = static_cast<int32_t *>(workspace);
+    if (runs > 1) {
+        expert_count_kernel<<<(unsigned)runs, ER_SORT_THREADS, (size_t)E * 4, st>>>(expert, n, run_len, (int)E, counts);
+        if (cudaGetLastError() != cudaSuccess) return DASS_ERR_CUDA;
+    }
+    expert_place_kernel<<<(unsigned)runs, ER_SORT_THREADS, (size_t)E * 4 * (2 + ER_SORT_WARPS), st>>>(expert, n, run_len, (int)runs, (int)E,
+                                                                                                     counts, offsets, slot, source);
+    return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
+}
+
+dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx, dass_dtype dt, const int32_t *slot, int64_t k,
+                               const float *weight, const int32_t *rows_used, void *Xs, int64_t rows, int64_t ldxs, void *cuda_stream)
+{
+    const dass_status cs = er_check(T, k, d, (int)dt);
+    if (cs != DASS_OK) return cs;
+    if (ldx < d || ldxs < d || rows < 0) return DASS_ERR_SHAPE;
+    if (rows > 0 && !Xs) return DASS_ERR_NULL;
+    if (T > 0 && (!X || !slot)) return DASS_ERR_NULL;
+    const bool bf16 = dt == DASS_BF16;
+    if (!elem_aligned(X, bf16) || !elem_aligned(Xs, bf16) || !elem_aligned(slot, false) || !elem_aligned(weight, false) ||
+        !elem_aligned(rows_used, false))
+        return DASS_ERR_ALIGN;
+    if (rows == 0 || (T == 0 && !rows_used)) return DASS_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const size_t elt = bf16 ? 2 : 4;
+    const int vec = bf16 ? 8 : 4;
+    const bool vector = rows_vec_ok(X, ldx, bf16) && rows_vec_ok(Xs, ldxs, bf16) && d % vec == 0;
+    ErRows r{T, d, rows, (int)k, vector ? d / vec : d};
+    DASS_BOUNDS_SCOPE(bs);
+    if (T > 0) DASS_BOUNDS_ADD(bs, X, ((size_t)(T - 1) * ldx + d) * elt);
+    DASS_BOUNDS_ADD(bs, Xs, ((size_t)(rows - 1) * ldxs + d) * elt);
+    DASS_BOUNDS_ADD(bs, slot, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, weight, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, rows_used, 4);
+    DASS_BOUNDS_COMMIT(bs, st);
+    (void)elt;
+    const unsigned grid = er_grid((T > 0 ? T : rows) * r.vpr);
+    if (bf16) {
+        if (vector) expert_gather_kernel<true, 8><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+        else expert_gather_kernel<true, 1><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+    } else {
+        if (vector) expert_gather_kernel<false, 4><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+        else expert_gather_kernel<false, 1><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+    }
+    return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
+}
+
+dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t ldys, dass_dtype dt, const int32_t *slot, int64_t T,
+                                int64_t k, const float *weight, const void *residual, int64_t ldr, void *Y, int64_t ldy, void *cuda_stream)
+{
+    const dass_status cs = er_check(T, k, d, (int)dt);
+    if (cs != DASS_OK) return cs;
+    if (ldys < d || ldy < d || rows < 0 || (residual && ldr < d)) return DASS_ERR_SHAPE;
+    if (T > 0 && (!slot || !Y)) return DASS_ERR_NULL;
+    if (T > 0 && rows > 0 && !Ys) return DASS_ERR_NULL;
+    const bool bf16 = dt == DASS_BF16;
+    if (!elem_aligned(Ys, bf16) || !elem_aligned(residual, bf16) || !elem_aligned(Y, bf16) || !elem_aligned(slot, false) ||
+        !elem_aligned(weight, false))
+        return DASS_ERR_ALIGN;
+    if (T == 0) return DASS_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const size_t elt = bf16 ? 2 : 4;
+    const int vec = bf16 ? 8 : 4;
+    const bool vector = rows_vec_ok(Ys, ldys, bf16) && rows_vec_ok(Y, ldy, bf16) && (!residual || rows_vec_ok(residual, ldr, bf16)) && d % vec == 0;
+    ErRows r{T, d, rows, (int)k, vector ? d / vec : d};
+    DASS_BOUNDS_SCOPE(bs);
+    if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
+    DASS_BOUNDS_ADD(bs, residual, ((size_t)(T - 1) * ldr + d) * elt);
+    DASS_BOUNDS_ADD(bs, Y, ((size_t)(T - 1) * ldy + d) * elt);
+    DASS_BOUNDS_ADD(bs, slot, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, weight, (size_t)T * k * 4);
+    DASS_BOUNDS_COMMIT(bs, st);
+    (void)elt;
+    const unsigned grid = er_grid(T * r.vpr);
+    if (bf16) {
+        if (vector) expert_combine_kernel<true, 8><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+        else expert_combine_kernel<true, 1><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+    } else {
+        if (vector) expert_combine_kernel<false, 4><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+        else expert_combine_kernel<false, 1><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+    }
+    return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
+}
+
+dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, int64_t lddy, const void *Ys, int64_t rows, int64_t ldys,
+                                         dass_dtype dt, const int32_t *slot, int64_t k, const float *weight, const int32_t *rows_used,
+                                         void *dYs, int64_t lddys, float *dweight, void *cuda_stream)
+{
+    const dass_status cs = er_check(T, k, d, (int)dt);
+    if (cs != DASS_OK) return cs;
+    if (!dYs && !dweight) return DASS_ERR_NULL;
+    if (lddy < d || rows < 0 || (Ys && ldys < d) || (dYs && lddys < d)) return DASS_ERR_SHAPE;
+    if (T > 0 && (!dY || !slot || (dweight && !Ys && rows > 0))) return DASS_ERR_NULL;
+    const bool bf16 = dt == DASS_BF16;
+    if (!elem_aligned(dY, bf16) || !elem_aligned(Ys, bf16) || !elem_aligned(dYs, bf16) || !elem_aligned(slot, false) ||
+        !elem_aligned(weight, false) || !elem_aligned(dweight, false) || !elem_aligned(rows_used, false))
+        return DASS_ERR_ALIGN;
+    if (T == 0) return DASS_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const size_t elt = bf16 ? 2 : 4;
+    const int vec = bf16 ? 8 : 4;
+    const bool vector = rows_vec_ok(dY, lddy, bf16) && (!dweight || rows_vec_ok(Ys, ldys, bf16)) && (!dYs || rows_vec_ok(dYs, lddys, bf16)) &&
+                        d % vec == 0;
+    ErRows r{T, d, rows, (int)k, vector ? d / vec : d};
+    DASS_BOUNDS_SCOPE(bs);
+    DASS_BOUNDS_ADD(bs, dY, ((size_t)(T - 1) * lddy + d) * elt);
+    if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
+    if (rows > 0) DASS_BOUNDS_ADD(bs, dYs, ((size_t)(rows - 1) * lddys + d) * elt);
+    DASS_BOUNDS_ADD(bs, slot, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, weight, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, dweight, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, rows_used, 4);
+    DASS_BOUNDS_COMMIT(bs, st);
+    (void)elt;
+    const unsigned grid = (unsigned)T;
+    if (bf16) {
+        if (vector) expert_combine_backward_kernel<true, 8, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+        else expert_combine_backward_kernel<true, 1, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+    } else {
+        if (vector) expert_combine_backward_kernel<false, 4, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+        else expert_combine_backward_kernel<false, 1, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+    }
+    return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,89 @@
+// What the kernels of dass_linear share: the arguments, the walk over groups of rows, the epilogue's arithmetic.
+// Internal header.
+#pragma once
+
+#include "rows_common.cuh"
+
+namespace dass {
+
+struct LinearArgs {
+    const void *X; int64_t T, K, ldx;
+    const void *W, *W_up; int64_t N, ldw, group_stride;    // group g's matrix starts at W + g * group_stride
+    const void *bias, *bias_up;                            // [groups x N], nullable
+    const void *residual; int64_t ldr;                     // [T x N], nullable
+    void *Y; int64_t ldy;
+    const int32_t *offsets; int groups;                    // offsets null: one group of all T rows
+    int act;
+    bool bf16;
+    cudaStream_t st;
+};
+
+// Rows [lo, hi) of group g, whatever the offsets hold: never outside [0, T).
+__device__ __forceinline__ void lin_group_rows(const int32_t *offsets, int g, int64_t T, int64_t &lo, int64_t &hi)
+{
+    if (!offsets) { lo = 0; hi = T; return; }
+    const int64_t a = DASS_LD(offsets + g), b = DASS_LD(offsets + g + 1);
+    lo = a < 0 ? 0 : (a > T ? T : a);
+    hi = b < lo ? lo : (b > T ? T : b);
+}
+
+struct LinTile { int g; int64_t lo, hi; };                 // group, rows of the tile; g < 0: there is no such tile
+
+// The index-th tile of `rows` rows when every group is cut into tiles by itself, groups in order.  Called by a whole warp.
+__device__ __forceinline__ LinTile lin_find_tile(const int32_t *offsets, int groups, int64_t T, int rows, int64_t index)
+{
+    const int lane = threadIdx.x & 31;
+    LinTile r{-1, 0, 0};
+    for (int g0 = 0; g0 < groups; g0 += 32) {
+        int64_t lo = 0, hi = 0;
+        if (g0 + lane < groups) lin_group_rows(offsets, g0 + lane, T, lo, hi);
+        const int tiles = (int)((hi - lo + rows - 1) / rows);
+        int inc = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(FULL_MASK, inc, o);
+            inc += lane >= o ? up : 0;
+        }
+        const unsigned past = __ballot_sync(FULL_MASK, index < inc);
+        if (past) {
+            const int src = __ffs(past) - 1;
+            const int64_t at = lo + (index - (inc - tiles)) * rows;
+            r.g = g0 + src;
+            r.lo = __shfl_sync(FULL_MASK, at, src);
+            r.hi = __shfl_sync(FULL_MASK, at + rows < hi ? at + rows : hi, src);
+            return r;
+        }
+        index -= __shfl_sync(FULL_MASK, inc, 31);
+    }
+    return r;
+}
+
+// The activation in f32, from accurate functions.
+__device__ __forceinline__ float lin_act(float x, int act)
+{
+    switch (act) {
+    case DASS_ACT_SILU: return x / (1.0f + expf(-x));
+    case DASS_ACT_GELU_TANH: return 0.5f * x * (1.0f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
+    case DASS_ACT_RELU: return fmaxf(x, 0.0f);
+    default: return x;
+    }
+}
+
+// Rows of no group are zero.  Strided over all threads of the grid.
+template <bool BF16>
+__device__ __forceinline__ void lin_zero_outside(const int32_t *offsets, int groups, int64_t T, int64_t N, void *Y, int64_t ldy,
+                                                 int64_t thread, int64_t threads)
+{
+    if (!offsets) return;
+    int64_t first, last, ignore;
+    lin_group_rows(offsets, 0, T, first, ignore);
+    lin_group_rows(offsets, groups - 1, T, ignore, last);
+    const int64_t outside = first + (T - last);
+    const float zero[1] = {0.f};
+    for (int64_t i = thread; i < outside * N; i += threads) {
+        const int64_t r = i / N;
+        row_store<BF16, 1>(Y, (r < first ? r : last + r - first) * ldy + (i - r * N), zero);
+    }
+}
+
+}  // namespace dass

@@ -1,0 +1,301 @@
+// The router's selection: the k experts with the highest logits of every token, their softmax weights, and the gradient.
+//
+// A token's row is held in registers by a group of L lanes (a power of two), V consecutive logits to a lane, so a warp
+// works on 32 / L tokens.  A logit becomes an unsigned key of the same order (masked: 0), every lane keeps the largest
+// of its keys, and each of the k rounds takes the group's maximum (log2 L shuffles) and lets the lowest lane that holds
+// it remove its lowest element of that value: lanes hold consecutive indices, so equal logits go to the lower index.
+// Sums are in f32 and in a fixed order.
+//
+// Bound: the logits are read once, k ids and weights are written; with few tokens the launch is what is left.
+#include "rows_common.cuh"
+
+namespace dass {
+
+constexpr int RT_THREADS = 128;
+constexpr int RT_MAX_E = 1024;
+constexpr int RT_MAX_K = 32;
+
+// Order-preserving key of a logit: 0 for a masked one (-inf, NaN); -0 and +0 are one value, +inf is the largest finite one.
+__device__ __forceinline__ uint32_t rt_key(float x)
+{
+    if (!(x > -INFINITY)) return 0u;
+    const uint32_t u = __float_as_uint(fminf(x, 3.402823466e38f) + 0.0f);
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+// The logit a key stands for.
+__device__ __forceinline__ float rt_value(uint32_t key)
+{
+    return __uint_as_float((key & 0x80000000u) ? (key ^ 0x80000000u) : ~key);
+}
+
+template <int L> __device__ __forceinline__ uint32_t group_max(uint32_t v)
+{
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(FULL_MASK, v, o));
+    return v;
+}
+template <int L> __device__ __forceinline__ float group_sum(float v)
+{
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(FULL_MASK, v, o);
+    return v;
+}
+
+// V consecutive logits from element e0 of a row of E, as keys (absent ones are masked).
+template <bool BF16, bool VECTOR, int V>
+__device__ __forceinline__ void rt_load(const void *logits, int64_t row, int e0, int E, uint32_t (&key)[V])
+{
+    constexpr int W = VECTOR ? ROW_VEC<BF16> : 1;
+#pragma unroll
+    for (int i = 0; i < V; i += W) {
+        if (e0 + i + W <= E) {
+            float x[W];
+            row_load<BF16, W>(logits, row + e0 + i, x);
+#pragma unroll
+            for (int c = 0; c < W; ++c) key[i + c] = rt_key(x[c]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < W; ++c) {
+                float x[1] = {0.f};
+                if (e0 + i + c < E) row_load<BF16, 1>(logits, row + e0 + i + c, x);
+                key[i + c] = e0 + i + c < E ? rt_key(x[0]) : 0u;
+            }
+        }
+    }
+}
+
+template <bool BF16, bool VECTOR, int V, int L>
+__global__ void __launch_bounds__(RT_THREADS)
+route_topk_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, bool over_all,
+                  int32_t *__restrict__ expert, float *__restrict__ weight)
+{
+    extern __shared__ uint32_t rt_smem[];
+    constexpr int TOKENS = RT_THREADS / L;
+    const int lane = threadIdx.x & 31;
+    const int gl = lane & (L - 1);                                  // lane within the token's group
+    const int64_t t = (int64_t)blockIdx.x * TOKENS + threadIdx.x / L;
+    const bool live = t < T;
+    int32_t *s_id = reinterpret_cast<int32_t *>(rt_smem) + (threadIdx.x / L) * k;
+    uint32_t *s_key = rt_smem + TOKENS * k + (threadIdx.x / L) * k;
+
+    uint32_t key[V];
+    rt_load<BF16, VECTOR, V>(logits, (live ? t : 0) * ld, gl * V, live ? E : 0, key);
+
+    float all = 0.f, top = 0.f;
+    uint32_t best = 0u;
+#pragma unroll
+    for (int i = 0; i < V; ++i) best = max(best, key[i]);
+    const unsigned group_bits = (L == 32 ? FULL_MASK : ((1u << (L & 31)) - 1u)) << (lane & ~(L - 1));
+    for (int j = 0; j < k; ++j) {
+        const uint32_t m = group_max<L>(best);
+        if (j == 0) {
+            top = rt_value(m);
+            if (over_all) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) all += key[i] ? expf(rt_value(key[i]) - top) : 0.f;
+            }
+        }
+        const unsigned holders = __ballot_sync(FULL_MASK, best == m) & group_bits;
+        if (lane == __ffs(holders) - 1) {
+            int at = 0;
+#pragma unroll
+            for (int i = V - 1; i >= 0; --i) at = key[i] == m ? i : at;
+            s_id[j] = m ? gl * V + at : -1;
+            s_key[j] = m;
+            best = 0u;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { key[i] = i == at ? 0u : key[i]; best = max(best, key[i]); }
+        }
+    }
+    __syncwarp();
+    float chosen = 0.f;
+    if (!over_all)
+        for (int j = gl; j < k; j += L) chosen += s_key[j] ? expf(rt_value(s_key[j]) - top) : 0.f;
+    const float total = group_sum<L>(over_all ? all : chosen);
+    if (!live) return;
+    for (int j = gl; j < k; j += L) {
+        const uint32_t m = s_key[j];
+        DASS_ST(expert + t * k + j, s_id[j]);
+        DASS_ST(weight + t * k + j, m ? expf(rt_value(m) - top) / total : 0.f);
+    }
+}
+
+// dlogits.  With p the softmax (over the chosen, or over all unmasked) and s = sum_j w_j dw_j over the chosen:
+// dl_e = p_e ([e chosen] dw_e - s), 0 for what p leaves out.  The row is written as it is for experts that were not
+// chosen, then (after a warp barrier, which orders the two) the chosen elements over it.
+template <bool BF16, bool VECTOR, int V, int L>
+__global__ void __launch_bounds__(RT_THREADS)
+route_topk_backward_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, bool over_all,
+                           const int32_t *__restrict__ expert, const float *__restrict__ dweight,
+                           void *__restrict__ dlogits, int64_t ldd)
+{
+    constexpr int TOKENS = RT_THREADS / L;
+    constexpr int W = VECTOR ? ROW_VEC<BF16> : 1;
+    const int gl = threadIdx.x & (L - 1);
+    const int64_t t = (int64_t)blockIdx.x * TOKENS + threadIdx.x / L;
+    const bool live = t < T;
+    uint32_t key[V];
+    uint32_t m = 0u;
+    if (over_all) {
+        rt_load<BF16, VECTOR, V>(logits, (live ? t : 0) * ld, gl * V, live ? E : 0, key);
+#pragma unroll
+        for (int i = 0; i < V; ++i) m = max(m, key[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = 0u;
+    }
+    auto chosen_key = [&](int j) -> uint32_t {                       // key of the j-th chosen expert, 0 if there is none
+        const int id = DASS_LD(expert + t * k + j);
+        if (id < 0 || id >= E) return 0u;
+        float x[1];
+        row_load<BF16, 1>(logits, t * ld + id, x);
+        return rt_key(x[0]);
+    };
+    if (live && !over_all)
+        for (int j = gl; j < k; j += L) m = max(m, chosen_key(j));
+    const float top = rt_value(group_max<L>(m));
+    float sum = 0.f, dot = 0.f;
+    if (over_all) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum += key[i] ? expf(rt_value(key[i]) - top) : 0.f;
+    }
+    if (live)
+        for (int j = gl; j < k; j += L) {
+            const uint32_t c = chosen_key(j);
+            const float e = c ? expf(rt_value(c) - top) : 0.f;
+            if (!over_all) sum += e;
+            if (c) dot += e * DASS_LD(dweight + t * k + j);
+        }
+    sum = group_sum<L>(sum);
+    dot = group_sum<L>(dot);
+    const float share = sum > 0.f ? 1.0f / sum : 0.f;
+    const float s = dot * share;
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < V; i += W) {
+            const int e = gl * V + i;
+            float g[W];
+#pragma unroll
+            for (int c = 0; c < W; ++c) g[c] = key[i + c] ? -s * (expf(rt_value(key[i + c]) - top) * share) : 0.f;
+            if (e + W <= E) row_store<BF16, W>(dlogits, t * ldd + e, g);
+            else {
+#pragma unroll
+                for (int c = 0; c < W; ++c) {
+                    const float one[1] = {g[c]};
+                    if (e + c < E) row_store<BF16, 1>(dlogits, t * ldd + e + c, one);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if (live)
+        for (int j = gl; j < k; j += L) {
+            const uint32_t c = chosen_key(j);
+            if (!c) continue;
+            const float p = expf(rt_value(c) - top) * share;
+            const float g[1] = {p * (DASS_LD(dweight + t * k + j) - s)};
+            row_store<BF16, 1>(dlogits, t * ldd + DASS_LD(expert + t * k + j), g);
+        }
+}
+
+struct RouteArgs {
+    const void *logits; int64_t T; int E; int64_t ld; int k; bool over_all;
+    int32_t *expert; float *weight;                                  // forward
+    const int32_t *chosen; const float *dweight; void *dlogits; int64_t ldd;   // backward (dlogits not null)
+    bool vector; cudaStream_t st;
+};
+
+template <bool BF16, bool VECTOR, int V, int L>
+static cudaError_t rt_launch(const RouteArgs &a)
+{
+    constexpr int TOKENS = RT_THREADS / L;
+    const unsigned grid = (unsigned)((a.T + TOKENS - 1) / TOKENS);
+    if (a.dlogits)
+        route_topk_backward_kernel<BF16, VECTOR, V, L><<<grid, RT_THREADS, 0, a.st>>>(a.logits, a.T, a.E, a.ld, a.k, a.over_all,
+                                                                                      a.chosen, a.dweight, a.dlogits, a.ldd);
+    else
+        route_topk_kernel<BF16, VECTOR, V, L><<<grid, RT_THREADS, (size_t)TOKENS * a.k * 8, a.st>>>(a.logits, a.T, a.E, a.ld, a.k,
+                                                                                                    a.over_all, a.expert, a.weight);
+    return cudaGetLastError();
+}
+template <bool BF16, bool VECTOR>
+static cudaError_t rt_pick(const RouteArgs &a)
+{
+    if (a.E <= 8) return rt_launch<BF16, VECTOR, 8, 1>(a);
+    if (a.E <= 16) return rt_launch<BF16, VECTOR, 8, 2>(a);
+    if (a.E <= 32) return rt_launch<BF16, VECTOR, 8, 4>(a);
+    if (a.E <= 64) return rt_launch<BF16, VECTOR, 8, 8>(a);
+    if (a.E <= 128) return rt_launch<BF16, VECTOR, 8, 16>(a);
+    if (a.E <= 256) return rt_launch<BF16, VECTOR, 8, 32>(a);
+    if (a.E <= 512) return rt_launch<BF16, VECTOR, 16, 32>(a);
+    return rt_launch<BF16, VECTOR, 32, 32>(a);
+}
+static cudaError_t rt_dispatch(const RouteArgs &a, bool bf16)
+{
+    if (bf16) return a.vector ? rt_pick<true, true>(a) : rt_pick<true, false>(a);
+    return a.vector ? rt_pick<false, true>(a) : rt_pick<false, false>(a);
+}
+
+static dass_status rt_check(int64_t T, int64_t E, int64_t ld, int dt, int k, int norm)
+{
+    if (dt != DASS_BF16 && dt != DASS_F32) return DASS_ERR_DTYPE;
+    if (norm != DASS_ROUTE_CHOSEN && norm != DASS_ROUTE_ALL) return DASS_ERR_DTYPE;
+    if (T < 0 || E < 1 || ld < E || k < 1 || k > E) return DASS_ERR_SHAPE;
+    if (E > RT_MAX_E || k > RT_MAX_K || T > (1ll << 31) - 1) return DASS_ERR_UNSUPPORTED;
+    return DASS_OK;
+}
+
+}  // namespace dass
+
+using namespace dass;
+
+extern "C" {
+
+dass_status dass_route_topk(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, int k, dass_route_norm norm,
+                            int32_t *expert, float *weight, void *cuda_stream)
+{
+    if (!logits || !expert || !weight) return DASS_ERR_NULL;
+    const dass_status cs = rt_check(T, E, ld, (int)dt, k, (int)norm);
+    if (cs != DASS_OK) return cs;
+    const bool bf16 = dt == DASS_BF16;
+    if (!elem_aligned(logits, bf16) || !elem_aligned(expert, false) || !elem_aligned(weight, false)) return DASS_ERR_ALIGN;
+    if (T == 0) return DASS_OK;
+    RouteArgs a{};
+    a.logits = logits; a.T = T; a.E = (int)E; a.ld = ld; a.k = k; a.over_all = norm == DASS_ROUTE_ALL;
+    a.expert = expert; a.weight = weight;
+    a.vector = rows_vec_ok(logits, ld, bf16);
+    a.st = static_cast<cudaStream_t>(cuda_stream);
+    DASS_BOUNDS_SCOPE(bs);
+    DASS_BOUNDS_ADD(bs, logits, ((size_t)(T - 1) * ld + E) * (bf16 ? 2 : 4));
+    DASS_BOUNDS_ADD(bs, expert, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, weight, (size_t)T * k * 4);
+    DASS_BOUNDS_COMMIT(bs, a.st);
+    return rt_dispatch(a, bf16) == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
+}
+
+dass_status dass_route_topk_backward(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, int k, dass_route_norm norm,
+                                     const int32_t *expert, const float *dweight, void *dlogits, int64_t ldd, void *cuda_stream)
+{
+    if (!logits || !expert || !dweight || !dlogits) return DASS_ERR_NULL;
+    const dass_status cs = rt_check(T, E, ld, (int)dt, k, (int)norm);
+    if (cs != DASS_OK) return cs;
+    if (ldd < E) return DASS_ERR_SHAPE;
+    const bool bf16 = dt == DASS_BF16;
+    if (!elem_aligned(logits, bf16) || !elem_aligned(dlogits, bf16) || !elem_aligned(expert, false) || !elem_aligned(dweight, false))
+        return DASS_ERR_ALIGN;
+    if (T == 0) return DASS_OK;
+    RouteArgs a{};
+    a.logits = logits; a.T = T; a.E = (int)E; a.ld = ld; a.k = k; a.over_all = norm == DASS_ROUTE_ALL;
+    a.chosen = expert; a.dweight = dweight; a.dlogits = dlogits; a.ldd = ldd;
+    a.vector = rows_vec_ok(logits, ld, bf16) && rows_vec_ok(dlogits, ldd, bf16);
+    a.st = static_cast<cudaStream_t>(cuda_stream);
+    DASS_BOUNDS_SCOPE(bs);
+    DASS_BOUNDS_ADD(bs, logits, ((size_t)(T - 1) * ld + E) * (bf16 ? 2 : 4));
+    DASS_BOUNDS_ADD(bs, expert, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, dweight, (size_t)T * k * 4);
+    DASS_BOUNDS_ADD(bs, dlogits, ((size_t)(T - 1) * ldd + E) * (bf16 ? 2 : 4));
+    DASS_BOUNDS_COMMIT(bs, a.st);
+    return rt_dispatch(a, bf16) == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
+}
+
+}  // extern "C"
