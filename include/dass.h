@@ -333,7 +333,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
  * Waits inside the tensor-core kernels are bounded (2 s); dass_linear_status waits for `cuda_stream` and returns
  * DASS_ERR_TIMEOUT if one ran out on the current device since the last query (outputs of that call are then
  * incomplete; the context stays usable), else DASS_OK, and clears the record.
- * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (extents beyond 32-bit coordinates, groups > 65535) / CUDA. */
+ * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (more than 2^28 rows, K or N beyond 32-bit coordinates, groups > 1024) / CUDA. */
 dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const void *W, const void *W_up, int64_t N, int64_t ldw,
                         int64_t group_stride, const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,
                         void *Y, int64_t ldy, dass_dtype dt, const int32_t *offsets, int64_t groups, void *cuda_stream);

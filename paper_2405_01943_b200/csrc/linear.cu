@@ -6,6 +6,7 @@
 namespace dass {
 
 dass_status linear_simt_launch(const LinearArgs &a);       // linear_simt.cu
+dass_status linear_tc_launch(const LinearArgs &a);         // linear_tc.cu
 
 __device__ int g_linear_status = 0;      // DASS_OK or DASS_ERR_TIMEOUT; read and cleared through dass_linear_status
 
@@ -47,7 +48,8 @@ dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const 
         !elem_aligned(offsets, false))
         return DASS_ERR_ALIGN;
     const int64_t lim = 0x7fffffffll - 512;                // 32-bit tile coordinates
-    if (T > lim || K > lim || N > lim || groups > 65535) return DASS_ERR_UNSUPPORTED;
+    const int64_t most_rows = 1ll << 28;                   // so are sums of tile counts, whatever the offsets hold
+    if (T > most_rows || K > lim || N > lim || groups > LIN_MAX_GROUPS) return DASS_ERR_UNSUPPORTED;
     if (T == 0) return DASS_OK;
 
     LinearArgs a{};
@@ -66,7 +68,7 @@ dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const 
     DASS_BOUNDS_ADD(bs, Y, ((size_t)(T - 1) * ldy + N) * (bf16 ? 2 : 4));
     DASS_BOUNDS_ADD(bs, offsets, (size_t)(groups + 1) * 4);
     DASS_BOUNDS_COMMIT(bs, a.st);
-    return linear_simt_launch(a);
+    return bf16 ? linear_tc_launch(a) : linear_simt_launch(a);
 }
 
 dass_status dass_linear_status(void *cuda_stream)

@@ -6,6 +6,8 @@
 
 namespace dass {
 
+constexpr int LIN_MAX_GROUPS = 1024;
+
 struct LinearArgs {
     const void *X; int64_t T, K, ldx;
     const void *W, *W_up; int64_t N, ldw, group_stride;    // group g's matrix starts at W + g * group_stride
@@ -71,7 +73,7 @@ __device__ __forceinline__ float lin_act(float x, int act)
 
 // Rows of no group are zero.  Strided over all threads of the grid.
 template <bool BF16>
-__device__ __forceinline__ void lin_zero_outside(const int32_t *offsets, int groups, int64_t T, int64_t N, void *Y, int64_t ldy,
+__device__ __forceinline__ void lin_zero_outside(const int32_t *offsets, int groups, int64_t T, int64_t N, void *Y, int64_t ldy, bool vec,
                                                  int64_t thread, int64_t threads)
 {
     if (!offsets) return;
@@ -79,10 +81,18 @@ __device__ __forceinline__ void lin_zero_outside(const int32_t *offsets, int gro
     lin_group_rows(offsets, 0, T, first, ignore);
     lin_group_rows(offsets, groups - 1, T, ignore, last);
     const int64_t outside = first + (T - last);
-    const float zero[1] = {0.f};
-    for (int64_t i = thread; i < outside * N; i += threads) {
-        const int64_t r = i / N;
-        row_store<BF16, 1>(Y, (r < first ? r : last + r - first) * ldy + (i - r * N), zero);
+    const int64_t wide = vec ? N / ROW_VEC<BF16> : 0;              // whole accesses of a row, then single elements
+    const int64_t per = wide + (N - wide * ROW_VEC<BF16>);
+    for (int64_t i = thread; i < outside * per; i += threads) {
+        const int64_t r = i / per, c = i - r * per;
+        const int64_t at = (r < first ? r : last + r - first) * ldy;
+        if (c < wide) {
+            float zero[ROW_VEC<BF16>] = {};
+            row_store<BF16, ROW_VEC<BF16>>(Y, at + c * ROW_VEC<BF16>, zero);
+        } else {
+            const float zero[1] = {0.f};
+            row_store<BF16, 1>(Y, at + wide * ROW_VEC<BF16> + (c - wide), zero);
+        }
     }
 }
 

@@ -8,13 +8,13 @@ constexpr int LS_T = 64, LS_N = 64, LS_K = 16, LS_THREADS = 256;
 
 template <bool BF16, bool GLU>
 __global__ void __launch_bounds__(LS_THREADS)
-linear_simt_kernel(const LinearArgs a, int64_t n_tiles)
+linear_simt_kernel(const LinearArgs a, int64_t n_tiles, bool y_vec)
 {
     __shared__ float sx[LS_K][LS_T + 4];
     __shared__ float sw[LS_K][LS_N + 4];
     __shared__ float sv[GLU ? LS_K : 1][LS_N + 4];
     const int tid = threadIdx.x;
-    lin_zero_outside<BF16>(a.offsets, a.groups, a.T, a.N, a.Y, a.ldy, (int64_t)blockIdx.x * LS_THREADS + tid, (int64_t)gridDim.x * LS_THREADS);
+    lin_zero_outside<BF16>(a.offsets, a.groups, a.T, a.N, a.Y, a.ldy, y_vec, (int64_t)blockIdx.x * LS_THREADS + tid, (int64_t)gridDim.x * LS_THREADS);
     const LinTile tile = lin_find_tile(a.offsets, a.groups, a.T, LS_T, blockIdx.x / n_tiles);
     if (tile.g < 0) return;
     const int64_t n0 = (blockIdx.x % n_tiles) * LS_N;
@@ -78,12 +78,13 @@ dass_status linear_simt_launch(const LinearArgs &a)
     const int64_t row_tiles = (a.T + LS_T - 1) / LS_T + (a.offsets ? a.groups : 0);
     if (n_tiles * row_tiles > 0x7fffffffll) return DASS_ERR_UNSUPPORTED;
     const unsigned grid = (unsigned)(n_tiles * row_tiles);
+    const bool y_vec = rows_vec_ok(a.Y, a.ldy, a.bf16);
     if (a.bf16) {
-        if (a.W_up) linear_simt_kernel<true, true><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles);
-        else linear_simt_kernel<true, false><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles);
+        if (a.W_up) linear_simt_kernel<true, true><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles, y_vec);
+        else linear_simt_kernel<true, false><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles, y_vec);
     } else {
-        if (a.W_up) linear_simt_kernel<false, true><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles);
-        else linear_simt_kernel<false, false><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles);
+        if (a.W_up) linear_simt_kernel<false, true><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles, y_vec);
+        else linear_simt_kernel<false, false><<<grid, LS_THREADS, 0, a.st>>>(a, n_tiles, y_vec);
     }
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
