@@ -20,6 +20,16 @@ struct LinearArgs {
     cudaStream_t st;
 };
 
+// What the host can say about the groups, whose sizes only the device knows: how many have rows at most, and how many
+// rows a tile should hold so that a group's weights are read once -- twice the average and a little, since a router does
+// not spread its tokens evenly.
+inline int64_t lin_active_groups(const LinearArgs &a) { return a.offsets ? (a.groups < a.T ? a.groups : a.T) : 1; }
+inline int64_t lin_rows_wanted(const LinearArgs &a)
+{
+    const int64_t twice = a.offsets ? 2 * ((a.T + a.groups - 1) / a.groups) + 6 : a.T;
+    return twice < a.T ? twice : a.T;
+}
+
 // Rows [lo, hi) of group g, whatever the offsets hold: never outside [0, T).
 __device__ __forceinline__ void lin_group_rows(const int32_t *offsets, int g, int64_t T, int64_t &lo, int64_t &hi)
 {

@@ -6,15 +6,45 @@
 
 namespace dass {
 
-// The activation before a rounding to bf16 (8 bits): __expf and an approximate quotient are exact enough by 2^10.
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float ex2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The activation before a rounding to bf16 (8 bits): an exponential and a reciprocal of the special-function unit, a few
+// units of f32's last place off, are exact enough by 2^10 and keep the epilogue at two such instructions per element.
+// x / (1 + e^-x) holds at the ends too: e^-x = inf gives a reciprocal of 0.
 template <int ACT>
 __device__ __forceinline__ float lt_act(float x)
 {
-    if constexpr (ACT == DASS_ACT_SILU) return __fdividef(x, 1.0f + __expf(-x));
-    else if constexpr (ACT == DASS_ACT_GELU_TANH)           // 0.5 (1 + tanh z) = sigmoid(2 z)
-        return __fdividef(x, 1.0f + __expf(-1.5957691216057308f * x * fmaf(0.044715f * x, x, 1.0f)));
+    constexpr float LOG2E = 1.4426950408889634f;
+    if constexpr (ACT == DASS_ACT_SILU) return x * rcp_approx(1.0f + ex2_approx(-LOG2E * x));
+    else if constexpr (ACT == DASS_ACT_GELU_TANH)           // 0.5 (1 + tanh z) = sigmoid(2 z), z = sqrt(2 / pi) (x + 0.044715 x^3)
+        return x * rcp_approx(1.0f + ex2_approx(-1.5957691216057308f * LOG2E * x * fmaf(0.044715f * x, x, 1.0f)));
     else if constexpr (ACT == DASS_ACT_RELU) return fmaxf(x, 0.0f);
     else return x;
+}
+template <int ACT, int V> __device__ __forceinline__ void lt_act_each(float (&x)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = lt_act<ACT>(x[i]);
+}
+template <int V> __device__ __forceinline__ void lt_act_all(float (&x)[V], int act)
+{
+    switch (act) {
+    case DASS_ACT_SILU: lt_act_each<DASS_ACT_SILU>(x); break;
+    case DASS_ACT_GELU_TANH: lt_act_each<DASS_ACT_GELU_TANH>(x); break;
+    case DASS_ACT_RELU: lt_act_each<DASS_ACT_RELU>(x); break;
+    default: break;
+    }
 }
 
 }  // namespace dass
