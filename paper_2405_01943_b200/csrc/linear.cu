@@ -16,32 +16,34 @@ struct LinPlan { int path, tile, split; };                 // path 1: few (rows 
 
 // Which kernel a bf16 product takes.
 //
-// linear_few.cu starts fastest (3.2 us) and is slowed by rows and by clusters: it takes products whose weights are small.
-// Between the other two the choice is the shorter estimate, in microseconds, of a model fitted to measurements on a B200
-// (rows 1 .. 8192, K 256 .. 14336, N 128 .. 14336, dense and per expert):
-//   linear_tc.cu, n = 256 or 128 accumulator columns:  START + rounds of the CTA pairs * k-blocks * KB
-//   linear_mid.cu, nt rows a tile, split s:            START + log2(s) * SPLIT + max(1, blocks / SMs) * (k-blocks / s * KB + END)
-// and neither is faster than its bytes at 6.3 GB per ms.  The constants are in lin_plan.
+// linear_few.cu starts fastest (3.2 us) and slows with the rows: it takes what is small.  Between the other two the choice
+// is the shorter estimate, in microseconds, of a model fitted to measurements on a B200 (rows 1 .. 8192, K 64 .. 14336, N 33
+// .. 14336, dense and per expert; on random shapes the choice is within a tenth of the best one on average):
+//   linear_tc.cu, n = 256 or 128 accumulator columns: a start, and per round of the CTA pairs the k-blocks, but no less
+//   than an epilogue;
+//   linear_mid.cu, nt rows a tile, split s: a start, a little for the split, and per wave of blocks the k-blocks (slower the
+//   more SMs read at once) and the epilogue.
+// Neither is faster than its weights, at 4.8 and 6.3 GB per ms.
 static double lin_rounds_up(double x) { return (double)(int64_t)(x + 0.999999); }
 
 LinPlan lin_plan(const LinearArgs &a)
 {
+    const bool glu = a.W_up != nullptr;
     const int64_t groups = lin_active_groups(a);
     const int64_t rows = a.offsets ? (a.T + a.groups - 1) / a.groups : a.T;           // of an average group
-    const int64_t weights = a.N * a.K * (a.W_up ? 2 : 1) * groups;
-    if ((rows <= 16 && weights <= 8 << 20) || (rows <= 32 && weights <= 4 << 20) || (rows <= 64 && weights <= 1 << 20)) {
+    const int64_t weights = a.N * a.K * (glu ? 2 : 1) * groups;
+    const double products = (double)a.T * a.N * a.K * (glu ? 2 : 1);
+    if (weights <= 8 << 20 && (products <= 32e6 || (rows <= 16 && a.T <= 64))) {
         // Weights that stay in L2 anyway are better read once per 8 rows, by more blocks (27 rows, 411 x 472: 3.9 us,
         // against 5.2 with all rows in a block).  A cluster costs more to place than a block, so k is split only where
         // most SMs would have none.
         const int64_t want = lin_rows_wanted(a), blocks = (a.N + 15) / 16 * groups;
-        const int nt = want <= 8 || weights <= 1 << 20 ? 1 : want <= 16 ? 2 : 4;
+        const int nt = want <= 8 || weights <= 2 << 20 ? 1 : want <= 16 || weights <= 4 << 20 ? 2 : 4;
         int split = 1;
         while (split < 8 && blocks * split < device_sm_count() && a.K >= 768 * split) split *= 2;
-        return {1, nt, split};
+        if (blocks * (a.offsets ? 1 : (a.T + 8 * nt - 1) / (8 * nt)) <= 1024) return {1, nt, split};
     }
-    const bool glu = a.W_up != nullptr;
     const double sms = device_sm_count(), kb = (double)((a.K + 63) / 64);
-    const double floor = weights * 2.0 / 6.3e6;
     auto row_tiles = [&](int64_t r) {                                                  // about: a group's last tile is half full
         if (!a.offsets) return (double)((a.T + r - 1) / r);
         const double t = (double)a.T / r + 0.5 * groups;
@@ -51,23 +53,25 @@ LinPlan lin_plan(const LinearArgs &a)
     double least = 1e30;
     for (int n = 256; n >= 128; n /= 2) {
         const double cols = (double)((a.N + (glu ? n / 2 : n) - 1) / (glu ? n / 2 : n));
-        const double start = n == 256 ? (glu ? 9.5 : 11.0) : (glu ? 8.3 : 9.5);
-        const double t = start + lin_rounds_up(row_tiles(256) * cols / (sms / 2)) * kb * (n == 256 ? 0.28 : 0.175);
+        const double main = kb * (n == 256 ? 0.30 : 0.19), end = n == 256 ? 3.2 : 2.5;
+        double t = lin_rounds_up(row_tiles(256) * cols / (sms / 2)) * ((main > end ? main : end) + 0.8);
+        const double bytes = weights * 2.0 / 4.8e6;
+        t = (n == 256 ? 7.0 : 6.5) + (t > bytes ? t : bytes);
         if (t < least) { least = t; best = {2, n, 1}; }
     }
     if (rows > 1024) return best;
     const double cols = (double)((a.N + 127) / 128);
-    static const struct { int nt; double kb, end, split; } PLAIN[4] = {{16, 0.205, 1.5, 0.1}, {32, 0.208, 2.0, 0.1}, {64, 0.212, 3.1, 0.2}, {128, 0.22, 4.9, 0.3}},
+    static const struct { int nt; double kb, end, split; } PLAIN[4] = {{16, 0.20, 1.5, 0.1}, {32, 0.20, 2.0, 0.1}, {64, 0.21, 3.1, 0.2}, {128, 0.22, 4.9, 0.3}},
                                                           GATED[4] = {{16, 0.29, 2.1, 0.5}, {32, 0.30, 2.7, 0.5}, {64, 0.31, 4.2, 0.7}, {128, 0.35, 6.7, 1.3}};
     for (int i = 0; i < 4; ++i) {
         const auto &m = glu ? GATED[i] : PLAIN[i];
-        if (a.offsets ? rows > m.nt : rows > 8 * m.nt) continue;
-        // per expert the loads are uneven: a tile below twice the average leaves second tiles, that read the weights again
-        const double again = a.offsets && m.nt < lin_rows_wanted(a) / 2 ? 1.2 : 1.0;
-        for (int s = 1; s <= 8 && kb >= 4 * s; s *= 2) {
-            const double blocks = row_tiles(m.nt) * cols * s;
-            double t = (blocks > sms ? blocks / sms : 1.0) * (kb / s * m.kb + m.end);
-            t = 3.3 + (s == 8 ? 3 : s == 4 ? 2 : s == 2 ? 1 : 0) * m.split + (t > floor * again ? t : floor * again);
+        if (rows > (a.offsets ? 2 : 8) * m.nt) continue;
+        // per expert the loads are uneven: tiles below twice the average leave second tiles, that read the weights again
+        const double bytes = weights * 2.0 / 6.3e6 * (a.offsets && m.nt < lin_rows_wanted(a) / 2 ? 1.2 : 1.0);
+        for (int s = 1; s <= 8 && (s == 1 || kb >= 4 * s); s *= 2) {
+            const double blocks = row_tiles(m.nt) * cols * s, full = blocks / (s > 2 ? 0.8 * sms : sms);   // clusters do not fill every SM
+            double t = (full > 1.0 ? full : 1.0) * (kb / s * (m.kb + 0.12 * (full > 1.0 ? 1.0 : full)) + m.end);
+            t = 3.3 + (s == 8 ? 3 : s == 4 ? 2 : s == 2 ? 1 : 0) * m.split + (t > bytes ? t : bytes);
             if (t < least) { least = t; best = {3, m.nt, s}; }
         }
     }
