@@ -183,6 +183,12 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return int(s.cuda_stream)
 
 
+def _stream_of(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
+    """The given stream, or the current one of the tensor's device (by its raw handle: building a Stream object costs as
+    much as the launch of a small kernel)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -501,27 +507,43 @@ def mlp_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.T
 
 
 # ----------------------------------------------------------------------------- mixture of experts
+#
+# These calls are made once per layer and decode step, so what they do on the host is kept short: one pass over each
+# tensor's shape and strides, outputs from new_empty, the stream by its handle.
+
+_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _code(t: torch.Tensor) -> int:
+    code = _CODES.get(t.dtype)
+    return _dtype_code(t) if code is None else code
+
 
 def _rows(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
-    """_matrix for calls that take any pitch: a single row, or none, has the pitch of its length."""
+    """(rows, columns, pitch) of a row-major CUDA matrix of any pitch; a single row, or none, has the pitch of its length."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D row-major tensor (unit stride along columns)")
     rows, cols = t.shape
-    return rows, cols, t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name} must be a 2-D row-major tensor (unit stride along columns)")
+    return rows, cols, ld if rows > 1 or ld > cols else cols
 
 
-def _same(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> None:
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
+def _same(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> int:
+    """Checks a dense tensor and returns its address."""
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return t.data_ptr()
 
 
-def _like(t: torch.Tensor, name: str, shape: Tuple[int, int], X: torch.Tensor) -> int:
+def _like(t: torch.Tensor, name: str, rows: int, cols: int, X: torch.Tensor) -> int:
     """Checks a row-major matrix of X's dtype and device and returns its pitch."""
-    rows, cols, ld = _rows(t, name)
-    if (rows, cols) != shape or t.dtype != X.dtype or t.device != X.device:
-        raise ValueError(f"{name} must be a {X.dtype} matrix of shape {shape} on {X.device}")
+    r, c, ld = _rows(t, name)
+    if r != rows or c != cols or t.dtype != X.dtype or t.device != X.device:
+        raise ValueError(f"{name} must be a {X.dtype} matrix of shape {(rows, cols)} on {X.device}")
     return ld
 
 
@@ -530,17 +552,18 @@ def route_topk(logits: torch.Tensor, k: int, renormalise: bool = True, expert: O
     """The k experts with the highest logits of every row and their softmax weights: over the k chosen
     (``renormalise``) or over all experts.  logits [T x E]; returns (expert int32 [T x k], weight float32 [T x k])."""
     T, E, ld = _rows(logits, "logits")
-    k = int(k)
+    k, dt = int(k), _code(logits)
     if expert is None:
-        expert = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+        expert = logits.new_empty((T, max(k, 0)), dtype=torch.int32)
+    else:
+        _same(expert, "expert", (T, k), torch.int32, logits.device)
     if weight is None:
-        weight = torch.empty((T, k), dtype=torch.float32, device=logits.device)
-    _same(expert, "expert", (T, k), torch.int32, logits.device)
-    _same(weight, "weight", (T, k), torch.float32, logits.device)
-    dt = _dtype_code(logits)
+        weight = logits.new_empty((T, max(k, 0)), dtype=torch.float32)
+    else:
+        _same(weight, "weight", (T, k), torch.float32, logits.device)
     if T:
         _check(load().dass_route_topk(logits.data_ptr(), T, E, ld, dt, k, ROUTE_CHOSEN if renormalise else ROUTE_ALL,
-                                      expert.data_ptr(), weight.data_ptr(), _stream(stream)), "dass_route_topk")
+                                      expert.data_ptr(), weight.data_ptr(), _stream_of(logits, stream)), "dass_route_topk")
     return expert, weight
 
 
@@ -548,17 +571,17 @@ def route_topk_backward(logits: torch.Tensor, expert: torch.Tensor, dweight: tor
                         dlogits: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The logits' gradient [T x E] from that of route_topk's weights (``expert`` as it returned them)."""
     T, E, ld = _rows(logits, "logits")
+    dt = _code(logits)
     k = expert.shape[1] if expert.dim() == 2 else -1
-    _same(expert, "expert", (T, k), torch.int32, logits.device)
-    _same(dweight, "dweight", (T, k), torch.float32, logits.device)
+    ids = _same(expert, "expert", (T, k), torch.int32, logits.device)
+    dw = _same(dweight, "dweight", (T, k), torch.float32, logits.device)
     if dlogits is None:
-        dlogits = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
-    ldd = _like(dlogits, "dlogits", (T, E), logits)
-    dt = _dtype_code(logits)
+        dlogits, ldd = logits.new_empty((T, E)), E
+    else:
+        ldd = _like(dlogits, "dlogits", T, E, logits)
     if T:
         _check(load().dass_route_topk_backward(logits.data_ptr(), T, E, ld, dt, k, ROUTE_CHOSEN if renormalise else ROUTE_ALL,
-                                               expert.data_ptr(), dweight.data_ptr(), dlogits.data_ptr(), ldd, _stream(stream)),
-               "dass_route_topk_backward")
+                                               ids, dw, dlogits.data_ptr(), ldd, _stream_of(logits, stream)), "dass_route_topk_backward")
     return dlogits
 
 
@@ -576,21 +599,25 @@ def expert_sort(expert: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = 
     if expert.dim() != 2 or not expert.is_cuda:
         raise ValueError("expert must be a 2-D CUDA tensor [T x k]")
     (T, k), E, dev = expert.shape, int(E), expert.device
-    _same(expert, "expert", (T, k), torch.int32, dev)
+    ids = _same(expert, "expert", (T, k), torch.int32, dev)
+    edges = E + 1 if E > 0 else 1
     if offsets is None:
-        offsets = torch.empty(max(E, 0) + 1, dtype=torch.int32, device=dev)
+        offsets = expert.new_empty(edges)
+    else:
+        _same(offsets, "offsets", (edges,), torch.int32, dev)
     if slot is None:
-        slot = torch.empty((T, k), dtype=torch.int32, device=dev)
+        slot = expert.new_empty((T, k))
+    else:
+        _same(slot, "slot", (T, k), torch.int32, dev)
     if source is None:
-        source = torch.empty(T * k, dtype=torch.int32, device=dev)
-    _same(offsets, "offsets", (max(E, 0) + 1,), torch.int32, dev)
-    _same(slot, "slot", (T, k), torch.int32, dev)
-    _same(source, "source", (T * k,), torch.int32, dev)
+        source = expert.new_empty(T * k)
+    else:
+        _same(source, "source", (T * k,), torch.int32, dev)
     if workspace is None:
         need = expert_sort_workspace_bytes(T, k, E)
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check(load().dass_expert_sort(expert.data_ptr(), T, k, E, offsets.data_ptr(), slot.data_ptr(), source.data_ptr(),
-                                   _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)),
+        workspace = expert.new_empty(need, dtype=torch.uint8) if need else None
+    _check(load().dass_expert_sort(ids, T, k, E, offsets.data_ptr(), slot.data_ptr(), source.data_ptr(),
+                                   _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream_of(expert, stream)),
            "dass_expert_sort")
     return offsets, slot, source
 
@@ -598,18 +625,18 @@ def expert_sort(expert: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = 
 def _slots(slot: torch.Tensor, weight: Optional[torch.Tensor], device: torch.device) -> Tuple[int, int]:
     if slot.dim() != 2:
         raise ValueError("slot must be the [T x k] tensor expert_sort returned")
-    T, k = slot.shape
-    _same(slot, "slot", (T, k), torch.int32, device)
+    shape = slot.shape
+    _same(slot, "slot", shape, torch.int32, device)
     if weight is not None:
-        _same(weight, "weight", (T, k), torch.float32, device)
-    return T, k
+        _same(weight, "weight", shape, torch.float32, device)
+    return shape
 
 
 def _rows_used(offsets: Optional[torch.Tensor], device: torch.device) -> Optional[int]:
     if offsets is None:
         return None
-    _same(offsets, "offsets", (offsets.numel(),), torch.int32, device)
-    return offsets.data_ptr() + 4 * (offsets.numel() - 1)
+    n = offsets.numel()
+    return _same(offsets, "offsets", (n,), torch.int32, device) + 4 * (n - 1)
 
 
 def expert_gather(X: torch.Tensor, slot: torch.Tensor, offsets: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
@@ -621,11 +648,13 @@ def expert_gather(X: torch.Tensor, slot: torch.Tensor, offsets: Optional[torch.T
     if Tx != T:
         raise ValueError("X and slot must have the same number of tokens")
     if Xs is None:
-        Xs = torch.empty((T * k, d), dtype=X.dtype, device=X.device)
-    rows = Xs.shape[0]
-    ldxs = _like(Xs, "Xs", (rows, d), X)
-    _check(load().dass_expert_gather(X.data_ptr(), T, d, ldx, _dtype_code(X), slot.data_ptr(), k, _ptr(weight),
-                                     _rows_used(offsets, X.device), Xs.data_ptr(), rows, ldxs, _stream(stream)), "dass_expert_gather")
+        rows, ldxs = T * k, d
+        Xs = X.new_empty((rows, d))
+    else:
+        rows = Xs.shape[0]
+        ldxs = _like(Xs, "Xs", rows, d, X)
+    _check(load().dass_expert_gather(X.data_ptr(), T, d, ldx, _code(X), slot.data_ptr(), k, _ptr(weight),
+                                     _rows_used(offsets, X.device), Xs.data_ptr(), rows, ldxs, _stream_of(X, stream)), "dass_expert_gather")
     return Xs
 
 
@@ -635,12 +664,13 @@ def expert_combine(Ys: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.
     """Y[t] = residual[t] + sum_j weight[t,j] * Ys[slot[t,j]]  (``Y`` may be the residual itself)."""
     rows, d, ldys = _rows(Ys, "Ys")
     T, k = _slots(slot, weight, Ys.device)
-    ldr = _like(residual, "residual", (T, d), Ys) if residual is not None else 0
+    ldr = _like(residual, "residual", T, d, Ys) if residual is not None else 0
     if Y is None:
-        Y = torch.empty((T, d), dtype=Ys.dtype, device=Ys.device)
-    ldy = _like(Y, "Y", (T, d), Ys)
-    _check(load().dass_expert_combine(Ys.data_ptr(), rows, d, ldys, _dtype_code(Ys), slot.data_ptr(), T, k, _ptr(weight),
-                                      _ptr(residual), ldr, Y.data_ptr(), ldy, _stream(stream)), "dass_expert_combine")
+        Y, ldy = Ys.new_empty((T, d)), d
+    else:
+        ldy = _like(Y, "Y", T, d, Ys)
+    _check(load().dass_expert_combine(Ys.data_ptr(), rows, d, ldys, _code(Ys), slot.data_ptr(), T, k, _ptr(weight),
+                                      _ptr(residual), ldr, Y.data_ptr(), ldy, _stream_of(Ys, stream)), "dass_expert_combine")
     return Y
 
 
@@ -659,21 +689,23 @@ def expert_combine_backward(dY: torch.Tensor, Ys: torch.Tensor, slot: torch.Tens
     Ty, d, lddy = _rows(dY, "dY")
     T, k = _slots(slot, weight, dY.device)
     rows = Ys.shape[0]
-    ldys = _like(Ys, "Ys", (rows, d), dY)
+    ldys = _like(Ys, "Ys", rows, d, dY)
     if Ty != T:
         raise ValueError("dY and slot must have the same number of tokens")
-    if dYs is None and want_rows:
-        dYs = torch.empty((rows, d), dtype=dY.dtype, device=dY.device)
-    lddys = _like(dYs, "dYs", (rows, d), dY) if dYs is not None else 0
-    if dweight is None and want_weight:
-        dweight = torch.empty((T, k), dtype=torch.float32, device=dY.device)
+    lddys = d
+    if dYs is not None:
+        lddys = _like(dYs, "dYs", rows, d, dY)
+    elif want_rows:
+        dYs = dY.new_empty((rows, d))
     if dweight is not None:
         _same(dweight, "dweight", (T, k), torch.float32, dY.device)
-    dt = _dtype_code(dY)
+    elif want_weight:
+        dweight = dY.new_empty((T, k), dtype=torch.float32)
+    dt = _code(dY)
     if T:
         _check(load().dass_expert_combine_backward(dY.data_ptr(), T, d, lddy, Ys.data_ptr(), rows, ldys, dt, slot.data_ptr(), k,
                                                    _ptr(weight), _rows_used(offsets, dY.device), _ptr(dYs), lddys, _ptr(dweight),
-                                                   _stream(stream)), "dass_expert_combine_backward")
+                                                   _stream_of(dY, stream)), "dass_expert_combine_backward")
     return dYs, dweight
 
 
@@ -687,30 +719,32 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     (and W_up) [G x N x K], bias [G x N]; rows offsets[g] .. offsets[g+1]-1 use matrix g, rows of no expert give zeros.
     ``Y`` may be the residual itself."""
     T, K, ldx = _rows(X, "X")
-    dims = 2 if offsets is None else 3
-    if W.dim() != dims or W.shape[-1] != K or W.dtype != X.dtype or W.device != X.device or (K > 1 and W.stride(-1) != 1):
-        raise ValueError(f"W must be a row-major {'[N x K]' if dims == 2 else '[G x N x K]'} tensor of X's dtype and device")
-    N, groups = W.shape[-2], W.shape[0] if dims == 3 else 1
-    ldw = W.stride(-2) if N > 1 else max(W.stride(-2), K)
-    group_stride = W.stride(0) if dims == 3 else 0
-    if W_up is not None and (W_up.shape != W.shape or W_up.stride() != W.stride() or W_up.dtype != X.dtype or W_up.device != X.device):
+    dtype, device = X.dtype, X.device
+    shape, strides = W.shape, W.stride()
+    if len(shape) != (2 if offsets is None else 3) or shape[-1] != K or W.dtype != dtype or W.device != device or (strides[-1] != 1 and K > 1):
+        raise ValueError(f"W must be a row-major {'[N x K]' if offsets is None else '[G x N x K]'} tensor of X's dtype and device")
+    N = shape[-2]
+    ldw = strides[-2] if N > 1 or strides[-2] > K else K
+    if W_up is not None and (W_up.shape != shape or W_up.stride() != strides or W_up.dtype != dtype or W_up.device != device):
         raise ValueError("W_up must have W's shape, strides, dtype and device")
-    for t, name in ((bias, "bias"), (bias_up, "bias_up")):
-        if t is not None:
-            _same(t, name, (N,) if dims == 2 else (groups, N), X.dtype, X.device)
+    if offsets is None:
+        groups, group_stride, edges, per = 1, 0, None, (N,)
+    else:
+        groups, group_stride = shape[0], strides[0]
+        edges, per = _same(offsets, "offsets", (groups + 1,), torch.int32, device), (groups, N)
+    b = _same(bias, "bias", per, dtype, device) if bias is not None else None
     if bias_up is not None and W_up is None:
         raise ValueError("bias_up goes with W_up")
-    if offsets is not None:
-        _same(offsets, "offsets", (groups + 1,), torch.int32, X.device)
-    ldr = _like(residual, "residual", (T, N), X) if residual is not None else 0
+    bu = _same(bias_up, "bias_up", per, dtype, device) if bias_up is not None else None
+    ldr = _like(residual, "residual", T, N, X) if residual is not None else 0
+    dt = _code(X)
     if Y is None:
-        Y = torch.empty((T, N), dtype=X.dtype, device=X.device)
-    ldy = _like(Y, "Y", (T, N), X)
-    dt = _dtype_code(X)
+        Y, ldy = X.new_empty((T, N)), N
+    else:
+        ldy = _like(Y, "Y", T, N, X)
     if T:
-        _check(load().dass_linear(X.data_ptr(), T, K, ldx, W.data_ptr(), _ptr(W_up), N, ldw, group_stride, _ptr(bias), _ptr(bias_up),
-                                  int(act), _ptr(residual), ldr, Y.data_ptr(), ldy, dt, _ptr(offsets), groups, _stream(stream)),
-               "dass_linear")
+        _check(load().dass_linear(X.data_ptr(), T, K, ldx, W.data_ptr(), _ptr(W_up), N, ldw, group_stride, b, bu, act, _ptr(residual), ldr,
+                                  Y.data_ptr(), ldy, dt, edges, groups, _stream_of(X, stream)), "dass_linear")
     return Y
 
 
