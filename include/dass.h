@@ -307,7 +307,7 @@ dass_status dass_expert_sort(const int32_t *expert, int64_t T, int64_t k, int64_
  * [0, rows) are skipped.  rows_used (nullable, device): rows from *rows_used on are written as zeros -- offsets + E of
  * dass_expert_sort; without it rows that no slot names are left alone.
  * The gradient of the copy is dass_expert_combine of dXs without weights.
- * Errors: NULL / DTYPE / SHAPE / UNSUPPORTED (k > 32) / ALIGN / CUDA. */
+ * Errors: NULL / DTYPE / SHAPE / UNSUPPORTED (k > 32, d > 2^21) / ALIGN / CUDA. */
 dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx, dass_dtype dt, const int32_t *slot, int64_t k,
                                const float *weight, const int32_t *rows_used, void *Xs, int64_t rows, int64_t ldxs, void *cuda_stream);
 /* Y[t,:] = residual[t,:] + sum_j weight[t,j] * Ys[slot[t,j],:]   (weight null: 1; residual null: 0; slots outside

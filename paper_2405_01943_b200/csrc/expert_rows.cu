@@ -17,6 +17,7 @@ int device_sm_count();   // dass_abi.cu
 
 constexpr int ER_MAX_E = 1024;
 constexpr int ER_MAX_K = 32;
+constexpr int64_t ER_MAX_D = 1 << 21;          // row length: accesses of a row fit a grid's y extent
 constexpr int ER_SORT_THREADS = 256;
 constexpr int ER_SORT_WARPS = ER_SORT_THREADS / 32;
 constexpr int64_t ER_ONE_RUN = 4096;           // ids that one block sorts alone
@@ -146,14 +147,34 @@ expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len,
     }
 }
 
-// ------------------------------------------------------------------ rows in
+// ------------------------------------------------------------------ rows
+// Every kernel below cuts its rows into accesses (16 bytes, or one element where alignment does not allow them) and lays
+// threads over them without a division: blockDim.x threads on a row, blockDim.y rows a block, and blocks along y for rows
+// longer than a block.  Loads are held as they lie in memory until all that a thread wants are in flight.
 struct ErRows {
-    int64_t T, d, rows;              // tokens, row length, rows of the sorted side
+    int64_t T, rows;                 // tokens, rows of the sorted side
     int k;
-    int64_t vpr;                     // accesses per row
+    int vpr;                         // accesses per row
 };
 
 constexpr int ER_THREADS = 256;
+constexpr int ER_BATCH = 4;          // choices whose rows are in flight at once
+constexpr int ER_COLS = 2;           // accesses of a row per thread
+
+// Rows from *used on are zeroed, by all blocks together.
+template <bool BF16, int VEC, int COLS>
+__device__ __forceinline__ void er_zero_tail(const int32_t *used, int64_t rows, int vpr, void *dst, int64_t ldd, int64_t first, int64_t step, int v0)
+{
+    int64_t end = DASS_LD(used);
+    end = end < 0 ? 0 : end;
+    float zero[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) zero[c] = 0.f;
+    for (int64_t row = end + first; row < rows; row += step)
+#pragma unroll
+        for (int u = 0; u < COLS; ++u)
+            if (v0 + u * (int)blockDim.x < vpr) row_store<BF16, VEC>(dst, row * ldd + (int64_t)(v0 + u * blockDim.x) * VEC, zero);
+}
 
 // dst[slot[t,j]] = scale * src[t]; rows past *used are zeroed (used null: left alone)
 template <bool BF16, int VEC>
@@ -161,151 +182,206 @@ __global__ void __launch_bounds__(ER_THREADS)
 expert_gather_kernel(const void *__restrict__ src, int64_t lds, const int32_t *__restrict__ slot, const float *__restrict__ weight,
                      const int32_t *__restrict__ used, void *__restrict__ dst, int64_t ldd, ErRows r)
 {
-    const int64_t stride = (int64_t)gridDim.x * ER_THREADS;
-    const int64_t first = (int64_t)blockIdx.x * ER_THREADS + threadIdx.x;
-    for (int64_t i = first; i < r.T * r.vpr; i += stride) {
-        const int64_t t = i / r.vpr, col = (i - t * r.vpr) * VEC;
-        float v[VEC];
-        row_load<BF16, VEC>(src, t * lds + col, v);
-        for (int j = 0; j < r.k; ++j) {
-            const int64_t s = DASS_LD(slot + t * r.k + j);
-            if (s < 0 || s >= r.rows) continue;
-            if (weight) {
-                const float w = DASS_LD(weight + t * r.k + j);
-                float x[VEC];
+    const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int v0 = blockIdx.y * (blockDim.x * ER_COLS) + threadIdx.x;
+    if (t < r.T && v0 < r.vpr) {
+        const int32_t *to = slot + t * r.k;
+        RowRaw<BF16, VEC> raw[ER_COLS];
 #pragma unroll
-                for (int c = 0; c < VEC; ++c) x[c] = w * v[c];
-                row_store<BF16, VEC>(dst, s * ldd + col, x);
-            } else {
-                row_store<BF16, VEC>(dst, s * ldd + col, v);
+        for (int u = 0; u < ER_COLS; ++u)
+            if (v0 + u * (int)blockDim.x < r.vpr) raw_load<BF16, VEC, true>(raw[u], src, t * lds + (int64_t)(v0 + u * blockDim.x) * VEC);
+        for (int j0 = 0; j0 < r.k; j0 += ER_BATCH) {
+            int s[ER_BATCH];
+#pragma unroll
+            for (int q = 0; q < ER_BATCH; ++q) s[q] = j0 + q < r.k ? DASS_LD(to + j0 + q) : -1;
+#pragma unroll
+            for (int q = 0; q < ER_BATCH; ++q) {
+                if (s[q] < 0 || s[q] >= r.rows) continue;
+                const float w = weight ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f;
+#pragma unroll
+                for (int u = 0; u < ER_COLS; ++u) {
+                    if (v0 + u * (int)blockDim.x >= r.vpr) continue;
+                    float y[VEC];
+                    raw_floats(raw[u], y);
+                    if (weight) {
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) y[c] *= w;
+                    }
+                    row_store<BF16, VEC>(dst, s[q] * ldd + (int64_t)(v0 + u * blockDim.x) * VEC, y);
+                }
             }
         }
     }
-    if (!used) return;
-    int64_t end = DASS_LD(used);
-    end = end < 0 ? 0 : end;
-    float zero[VEC];
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) zero[c] = 0.f;
-    for (int64_t i = first; i < (r.rows - end) * r.vpr; i += stride) {
-        const int64_t t = i / r.vpr;
-        row_store<BF16, VEC>(dst, (end + t) * ldd + (i - t * r.vpr) * VEC, zero);
-    }
+    if (used) er_zero_tail<BF16, VEC, ER_COLS>(used, r.rows, r.vpr, dst, ldd, t, (int64_t)gridDim.x * blockDim.y, v0);
 }
 
-// ------------------------------------------------------------------ rows out
 // out[t] = residual[t] + sum_j weight[t,j] * rows[slot[t,j]], f32, j ascending, one rounding
 template <bool BF16, int VEC>
 __global__ void __launch_bounds__(ER_THREADS)
 expert_combine_kernel(const void *__restrict__ rows, int64_t ldr, const int32_t *__restrict__ slot, const float *__restrict__ weight,
-                      const void *__restrict__ residual, int64_t ldres, void *__restrict__ out, int64_t ldo, ErRows r)
+                      const void *residual, int64_t ldres, void *out, int64_t ldo, ErRows r)
 {
-    const int64_t stride = (int64_t)gridDim.x * ER_THREADS;
-    for (int64_t i = (int64_t)blockIdx.x * ER_THREADS + threadIdx.x; i < r.T * r.vpr; i += stride) {
-        const int64_t t = i / r.vpr, col = (i - t * r.vpr) * VEC;
-        float acc[VEC];
+    const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int v0 = blockIdx.y * (blockDim.x * ER_COLS) + threadIdx.x;
+    if (t >= r.T || v0 >= r.vpr) return;
+    float acc[ER_COLS][VEC];
+    RowRaw<BF16, VEC> res[ER_COLS];
 #pragma unroll
-        for (int c = 0; c < VEC; ++c) acc[c] = 0.f;
-#pragma unroll 4
-        for (int j = 0; j < r.k; ++j) {
-            const int64_t s = DASS_LD(slot + t * r.k + j);
-            if (s < 0 || s >= r.rows) continue;
-            const float w = weight ? DASS_LD(weight + t * r.k + j) : 1.0f;
-            float v[VEC];
-            row_load<BF16, VEC>(rows, s * ldr + col, v);
+    for (int u = 0; u < ER_COLS; ++u) {
 #pragma unroll
-            for (int c = 0; c < VEC; ++c) acc[c] = fmaf(w, v[c], acc[c]);
+        for (int c = 0; c < VEC; ++c) acc[u][c] = 0.f;
+        if (residual && v0 + u * (int)blockDim.x < r.vpr)
+            raw_load<BF16, VEC>(res[u], residual, t * ldres + (int64_t)(v0 + u * blockDim.x) * VEC);
+    }
+    for (int j0 = 0; j0 < r.k; j0 += ER_BATCH) {
+        int s[ER_BATCH];
+        float w[ER_BATCH];
+        RowRaw<BF16, VEC> x[ER_BATCH][ER_COLS];
+#pragma unroll
+        for (int q = 0; q < ER_BATCH; ++q) s[q] = j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
+#pragma unroll
+        for (int q = 0; q < ER_BATCH; ++q) {
+            if (s[q] >= r.rows) s[q] = -1;
+            w[q] = s[q] >= 0 && weight ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f;
+#pragma unroll
+            for (int u = 0; u < ER_COLS; ++u)
+                if (s[q] >= 0 && v0 + u * (int)blockDim.x < r.vpr)
+                    raw_load<BF16, VEC, true>(x[q][u], rows, s[q] * ldr + (int64_t)(v0 + u * blockDim.x) * VEC);
         }
+#pragma unroll
+        for (int q = 0; q < ER_BATCH; ++q) {
+            if (s[q] < 0) continue;                               // a skipped choice adds nothing, whatever its row would hold
+#pragma unroll
+            for (int u = 0; u < ER_COLS; ++u) {
+                float v[VEC];
+                raw_floats(x[q][u], v);
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) acc[u][c] = fmaf(w[q], v[c], acc[u][c]);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < ER_COLS; ++u) {
+        if (v0 + u * (int)blockDim.x >= r.vpr) continue;
         if (residual) {
             float v[VEC];
-            row_load<BF16, VEC>(residual, t * ldres + col, v);
+            raw_floats(res[u], v);
 #pragma unroll
-            for (int c = 0; c < VEC; ++c) acc[c] += v[c];
+            for (int c = 0; c < VEC; ++c) acc[u][c] += v[c];
         }
-        row_store<BF16, VEC>(out, t * ldo + col, acc);
+        row_store<BF16, VEC>(out, t * ldo + (int64_t)(v0 + u * blockDim.x) * VEC, acc[u]);
     }
 }
 
 // Gradient of the weighted sum: drows[slot[t,j]] = weight[t,j] * dout[t] and dweight[t,j] = <dout[t], rows[slot[t,j]]>.
-// One block of WARPS warps per token; ER_J choices at a time share a read of dout[t].
-constexpr int ER_J = 4;
-template <bool BF16, int VEC, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32)
+// blockDim.x threads per token, blockDim.y tokens a block; dout[t] is read once for ER_BATCH choices.
+template <bool BF16, int VEC>
+__global__ void __launch_bounds__(ER_THREADS)
 expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const void *__restrict__ rows, int64_t ldr,
                                const int32_t *__restrict__ slot, const float *__restrict__ weight, const int32_t *__restrict__ used,
                                void *__restrict__ drows, int64_t lddr, float *__restrict__ dweight, ErRows r)
 {
-    __shared__ float part[WARPS][ER_J];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t t = blockIdx.x;
-    for (int j0 = 0; j0 < r.k; j0 += ER_J) {
-        int64_t s[ER_J];
-        float w[ER_J], acc[ER_J];
+    __shared__ float part[ER_THREADS / 32][ER_BATCH];
+    const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const bool live = t < r.T;
+    const int width = blockDim.x;
+    for (int j0 = 0; j0 < r.k; j0 += ER_BATCH) {
+        int s[ER_BATCH];
+        float w[ER_BATCH], acc[ER_BATCH];
 #pragma unroll
-        for (int q = 0; q < ER_J; ++q) {
-            s[q] = j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
-            if (s[q] >= r.rows) s[q] = -1;
-            w[q] = s[q] < 0 ? 0.f : (weight ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f);
+        for (int q = 0; q < ER_BATCH; ++q) {
+            s[q] = live && j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
             acc[q] = 0.f;
         }
-        for (int64_t i = threadIdx.x; i < r.vpr; i += WARPS * 32) {
-            float g[VEC];
-            row_load<BF16, VEC>(dout, t * ldo + i * VEC, g);
 #pragma unroll
-            for (int q = 0; q < ER_J; ++q) {
-                if (s[q] < 0) continue;
-                float v[VEC];
+        for (int q = 0; q < ER_BATCH; ++q) {
+            if (s[q] >= r.rows) s[q] = -1;
+            w[q] = drows && weight && s[q] >= 0 ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f;
+        }
+        for (int v0 = threadIdx.x; live && v0 < r.vpr; v0 += ER_COLS * width) {
+            RowRaw<BF16, VEC> g[ER_COLS], x[ER_BATCH][ER_COLS];
+#pragma unroll
+            for (int u = 0; u < ER_COLS; ++u) {
+                const int64_t col = (int64_t)(v0 + u * width) * VEC;
+                if (v0 + u * width >= r.vpr) continue;
+                raw_load<BF16, VEC>(g[u], dout, t * ldo + col);
                 if (dweight) {
-                    row_load<BF16, VEC>(rows, s[q] * ldr + i * VEC, v);
 #pragma unroll
-                    for (int c = 0; c < VEC; ++c) acc[q] = fmaf(g[c], v[c], acc[q]);
+                    for (int q = 0; q < ER_BATCH; ++q)
+                        if (s[q] >= 0) raw_load<BF16, VEC, true>(x[q][u], rows, s[q] * ldr + col);
                 }
-                if (drows) {
+            }
 #pragma unroll
-                    for (int c = 0; c < VEC; ++c) v[c] = w[q] * g[c];
-                    row_store<BF16, VEC>(drows, s[q] * lddr + i * VEC, v);
+            for (int u = 0; u < ER_COLS; ++u) {
+                if (v0 + u * width >= r.vpr) continue;
+                float gf[VEC];
+                raw_floats(g[u], gf);
+#pragma unroll
+                for (int q = 0; q < ER_BATCH; ++q) {
+                    if (s[q] < 0) continue;
+                    float v[VEC];
+                    if (dweight) {
+                        raw_floats(x[q][u], v);
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) acc[q] = fmaf(gf[c], v[c], acc[q]);
+                    }
+                    if (drows) {
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) v[c] = w[q] * gf[c];
+                        row_store<BF16, VEC>(drows, s[q] * lddr + (int64_t)(v0 + u * width) * VEC, v);
+                    }
                 }
             }
         }
         if (dweight) {
+            const int group = width < 32 ? width : 32;               // lanes of a token within a warp
 #pragma unroll
-            for (int q = 0; q < ER_J; ++q) {
+            for (int q = 0; q < ER_BATCH; ++q)
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) acc[q] += __shfl_xor_sync(FULL_MASK, acc[q], o);
-                if (lane == 0) part[warp][q] = acc[q];
+                for (int o = 16; o > 0; o >>= 1) {
+                    const float other = __shfl_xor_sync(FULL_MASK, acc[q], o);
+                    acc[q] += o < group ? other : 0.f;
+                }
+            if (width > 32) {                                        // a token's warps: through shared memory, in order
+                const int warp = (threadIdx.y * width + threadIdx.x) >> 5, first = (threadIdx.y * width) >> 5;
+                if ((threadIdx.x & 31) == 0)
+#pragma unroll
+                    for (int q = 0; q < ER_BATCH; ++q) part[warp][q] = acc[q];
+                __syncthreads();
+#pragma unroll
+                for (int q = 0; q < ER_BATCH; ++q) {
+                    acc[q] = 0.f;
+                    for (int i = 0; i < width / 32; ++i) acc[q] += part[first + i][q];
+                }
+                __syncthreads();
             }
-            __syncthreads();
-            if (threadIdx.x < ER_J && j0 + threadIdx.x < r.k) {
-                float sum = 0.f;
-                for (int x = 0; x < WARPS; ++x) sum += part[x][threadIdx.x];
-                DASS_ST(dweight + t * r.k + j0 + threadIdx.x, sum);
-            }
-            __syncthreads();
+            if (live && threadIdx.x == 0)
+#pragma unroll
+                for (int q = 0; q < ER_BATCH; ++q)
+                    if (j0 + q < r.k) DASS_ST(dweight + t * r.k + j0 + q, acc[q]);
         }
     }
-    if (!drows || !used) return;
-    int64_t end = DASS_LD(used);
-    end = end < 0 ? 0 : end;
-    float zero[VEC];
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) zero[c] = 0.f;
-    for (int64_t row = end + t; row < r.rows; row += r.T)
-        for (int64_t i = threadIdx.x; i < r.vpr; i += WARPS * 32) row_store<BF16, VEC>(drows, row * lddr + i * VEC, zero);
+    if (drows && used)
+        for (int v0 = threadIdx.x; v0 < r.vpr; v0 += ER_COLS * width)
+            er_zero_tail<BF16, VEC, ER_COLS>(used, r.rows, r.vpr, drows, lddr, t, (int64_t)gridDim.x * blockDim.y, v0);
 }
 
 // ------------------------------------------------------------------ host side
-static unsigned er_grid(int64_t work)
+// Threads over `vpr` accesses of a row, `cols` each, as many rows as fill the block; blocks over rows and long rows.
+struct ErGrid { dim3 grid, block; };
+static ErGrid er_grid(int64_t rows, int vpr, int most)
 {
-    const int64_t blocks = (work + ER_THREADS - 1) / ER_THREADS;
-    const int64_t most = 1ll << 30;
-    return (unsigned)(blocks < 1 ? 1 : (blocks < most ? blocks : most));
+    int x = 4;
+    while (x < most && x * ER_COLS < vpr) x *= 2;
+    const int y = ER_THREADS / x;
+    return {dim3((unsigned)((rows + y - 1) / y), (unsigned)((vpr + x * ER_COLS - 1) / (x * ER_COLS))), dim3(x, y)};
 }
 
 static dass_status er_check(int64_t T, int64_t k, int64_t d, int dt)
 {
     if (dt != DASS_BF16 && dt != DASS_F32) return DASS_ERR_DTYPE;
     if (T < 0 || k < 1 || d < 1) return DASS_ERR_SHAPE;
-    if (k > ER_MAX_K || T * k > (1ll << 31) - 1 || T > (1ll << 31) - 1) return DASS_ERR_UNSUPPORTED;
+    if (k > ER_MAX_K || T > ((1ll << 31) - 1) / k || d > ER_MAX_D) return DASS_ERR_UNSUPPORTED;
     return DASS_OK;
 }
 
@@ -374,7 +450,7 @@ dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx,
     const size_t elt = bf16 ? 2 : 4;
     const int vec = bf16 ? 8 : 4;
     const bool vector = rows_vec_ok(X, ldx, bf16) && rows_vec_ok(Xs, ldxs, bf16) && d % vec == 0;
-    ErRows r{T, d, rows, (int)k, vector ? d / vec : d};
+    const ErRows r{T, rows, (int)k, (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
     if (T > 0) DASS_BOUNDS_ADD(bs, X, ((size_t)(T - 1) * ldx + d) * elt);
     DASS_BOUNDS_ADD(bs, Xs, ((size_t)(rows - 1) * ldxs + d) * elt);
@@ -383,13 +459,13 @@ dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx,
     DASS_BOUNDS_ADD(bs, rows_used, 4);
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
-    const unsigned grid = er_grid((T > 0 ? T : rows) * r.vpr);
+    const ErGrid g = er_grid(T > 0 ? T : rows, r.vpr, ER_THREADS);
     if (bf16) {
-        if (vector) expert_gather_kernel<true, 8><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
-        else expert_gather_kernel<true, 1><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+        if (vector) expert_gather_kernel<true, 8><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+        else expert_gather_kernel<true, 1><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
     } else {
-        if (vector) expert_gather_kernel<false, 4><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
-        else expert_gather_kernel<false, 1><<<grid, ER_THREADS, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+        if (vector) expert_gather_kernel<false, 4><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
+        else expert_gather_kernel<false, 1><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
     }
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
@@ -411,7 +487,7 @@ dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t
     const size_t elt = bf16 ? 2 : 4;
     const int vec = bf16 ? 8 : 4;
     const bool vector = rows_vec_ok(Ys, ldys, bf16) && rows_vec_ok(Y, ldy, bf16) && (!residual || rows_vec_ok(residual, ldr, bf16)) && d % vec == 0;
-    ErRows r{T, d, rows, (int)k, vector ? d / vec : d};
+    const ErRows r{T, rows, (int)k, (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
     if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
     DASS_BOUNDS_ADD(bs, residual, ((size_t)(T - 1) * ldr + d) * elt);
@@ -420,13 +496,13 @@ dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t
     DASS_BOUNDS_ADD(bs, weight, (size_t)T * k * 4);
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
-    const unsigned grid = er_grid(T * r.vpr);
+    const ErGrid g = er_grid(T, r.vpr, ER_THREADS);
     if (bf16) {
-        if (vector) expert_combine_kernel<true, 8><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
-        else expert_combine_kernel<true, 1><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+        if (vector) expert_combine_kernel<true, 8><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+        else expert_combine_kernel<true, 1><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
     } else {
-        if (vector) expert_combine_kernel<false, 4><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
-        else expert_combine_kernel<false, 1><<<grid, ER_THREADS, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+        if (vector) expert_combine_kernel<false, 4><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
+        else expert_combine_kernel<false, 1><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
     }
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
@@ -450,7 +526,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     const int vec = bf16 ? 8 : 4;
     const bool vector = rows_vec_ok(dY, lddy, bf16) && (!dweight || rows_vec_ok(Ys, ldys, bf16)) && (!dYs || rows_vec_ok(dYs, lddys, bf16)) &&
                         d % vec == 0;
-    ErRows r{T, d, rows, (int)k, vector ? d / vec : d};
+    const ErRows r{T, rows, (int)k, (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
     DASS_BOUNDS_ADD(bs, dY, ((size_t)(T - 1) * lddy + d) * elt);
     if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
@@ -461,13 +537,16 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     DASS_BOUNDS_ADD(bs, rows_used, 4);
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
-    const unsigned grid = (unsigned)T;
+    // few threads a token keep its sums inside a warp; a whole block where there are few tokens
+    ErGrid g = er_grid(T, r.vpr, T >= 148 * 32 ? 64 : ER_THREADS);
+    g.grid.y = 1;                                                     // a token's threads walk its whole row
+    const dim3 grid = g.grid, block = g.block;
     if (bf16) {
-        if (vector) expert_combine_backward_kernel<true, 8, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
-        else expert_combine_backward_kernel<true, 1, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+        if (vector) expert_combine_backward_kernel<true, 8><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+        else expert_combine_backward_kernel<true, 1><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
     } else {
-        if (vector) expert_combine_backward_kernel<false, 4, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
-        else expert_combine_backward_kernel<false, 1, 4><<<grid, 128, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+        if (vector) expert_combine_backward_kernel<false, 4><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
+        else expert_combine_backward_kernel<false, 1><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
     }
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }

@@ -48,6 +48,33 @@ __device__ __forceinline__ void row_store(void *base, int64_t off, const float (
     }
 }
 
+// One access of a row as it lies in memory, for kernels that hold many in flight before they use the first.
+template <bool BF16, int VEC> struct RowRaw { uint4 w; };
+template <> struct RowRaw<true, 1> { uint16_t w; };
+template <> struct RowRaw<false, 1> { float w; };
+
+template <bool BF16, int VEC, bool ONCE = false>
+__device__ __forceinline__ void raw_load(RowRaw<BF16, VEC> &r, const void *base, int64_t off)
+{
+    using W = decltype(r.w);
+    const W *p = reinterpret_cast<const W *>(static_cast<const char *>(base) + off * (BF16 ? 2 : 4));
+    if constexpr (ONCE) r.w = DASS_LD_CS(p); else r.w = DASS_LD(p);
+}
+template <bool BF16, int VEC>
+__device__ __forceinline__ void raw_floats(const RowRaw<BF16, VEC> &r, float (&v)[VEC])
+{
+    if constexpr (VEC == 1) {
+        if constexpr (BF16) v[0] = __uint_as_float((uint32_t)r.w << 16); else v[0] = r.w;
+    } else {
+        const uint32_t x[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (BF16) { v[2 * i] = __uint_as_float(x[i] << 16); v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u); }
+            else v[i] = __uint_as_float(x[i]);
+        }
+    }
+}
+
 // Whether rows that start at `p` and are `ld` elements apart can be read 16 bytes at a time.
 inline bool rows_vec_ok(const void *p, int64_t ld, bool bf16)
 {
