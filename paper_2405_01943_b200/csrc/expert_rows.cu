@@ -2,10 +2,12 @@
 // the weighted sum out of it, and the gradients of both.
 //
 // The order: flat index f = t * k + j; expert e's rows are those f with id e, ascending.  The ids are cut into one run
-// per block.  Pass 1 counts each run's ids per expert.  Pass 2 adds up, for its own run, what the runs before it hold
-// of every expert and what all runs hold of the experts before, counts again per warp, and then every warp walks its
-// part 32 ids at a time: __match_any finds the lanes with the same expert, their order inside the warp is the rank.
-// Nothing depends on the order in which blocks or atomics run.  A short list is one run and needs no pass 1.
+// per block.  Pass 1 counts each run's ids per expert.  Pass 2 needs, for its own run, what the runs before it hold of
+// every expert and what all runs hold of the experts before; it counts again per warp, and then every warp walks its part
+// 32 ids at a time: __match_any finds the lanes with the same expert, their order inside the warp is the rank.  Nothing
+// depends on the order in which blocks or atomics run.  A short list is one run and needs no pass 1.  The sums over the
+// runs are taken by every block of pass 2 itself, or, where there are many experts, once by a scan between
+// the passes.
 //
 // The rows: a thread owns 16 bytes of a token's row and reads it once for all k copies (gather), or reads the k
 // sources and sums them in f32 in j order (combine).  All of it is bound by memory: the row bytes in and out.
@@ -18,20 +20,23 @@ int device_sm_count();   // dass_abi.cu
 constexpr int ER_MAX_E = 1024;
 constexpr int ER_MAX_K = 32;
 constexpr int64_t ER_MAX_D = 1 << 21;          // row length: accesses of a row fit a grid's y extent
-constexpr int ER_SORT_THREADS = 256;
-constexpr int ER_SORT_WARPS = ER_SORT_THREADS / 32;
+// Few warps: each step of the scan over experts walks them (32 instead of 8: 4.5 instead of 2.6 us for a short list).
+constexpr int ER_SORT_WARPS = 8;
 constexpr int64_t ER_ONE_RUN = 4096;           // ids that one block sorts alone
 
+// Runs of 1024 ids at least, one to an SM at most.
 static int64_t er_runs(int64_t n)
 {
     if (n <= ER_ONE_RUN) return 1;
-    const int64_t most = device_sm_count();
-    const int64_t want = (n + 1023) / 1024;    // runs of 1024 ids at least: 4 steps of a warp
+    const int64_t most = device_sm_count(), want = (n + 1023) / 1024;
     return want < most ? want : most;
 }
+// Experts up to which every block adds up the runs itself: 32768 choices of 8 experts 5.8 us, and 7.2 with the scan; 131072
+// of 128 experts 14.1 and 8.6.
+constexpr int64_t ER_SUM_EXPERTS = 32;
 
-// counts[run][e]
-__global__ void __launch_bounds__(ER_SORT_THREADS)
+// counts[e][run]
+__global__ void __launch_bounds__(ER_SORT_WARPS * 32)
 expert_count_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len, int E, int32_t *__restrict__ counts)
 {
     extern __shared__ int32_t er_smem[];
@@ -43,11 +48,34 @@ expert_count_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len,
         if (id >= 0 && id < E) atomicAdd(&er_smem[id], 1);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += blockDim.x) DASS_ST(counts + (int64_t)blockIdx.x * E + e, er_smem[e]);
+    for (int e = threadIdx.x; e < E; e += blockDim.x) DASS_ST(counts + (int64_t)e * gridDim.x + blockIdx.x, er_smem[e]);
 }
 
-__global__ void __launch_bounds__(ER_SORT_THREADS)
+// One warp per expert: counts[e][0 .. runs) become what the runs before hold, totals[e] what all hold.
+__global__ void __launch_bounds__(ER_SORT_WARPS * 32)
+expert_scan_kernel(int32_t *__restrict__ counts, int32_t *__restrict__ totals, int runs, int E)
+{
+    const int lane = threadIdx.x & 31, e = blockIdx.x * ER_SORT_WARPS + (threadIdx.x >> 5);
+    if (e >= E) return;
+    int32_t *row = counts + (int64_t)e * runs;
+    int32_t carry = 0;
+    for (int r0 = 0; r0 < runs; r0 += 32) {
+        const int32_t v = r0 + lane < runs ? DASS_LD(row + r0 + lane) : 0;
+        int32_t inc = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t up = __shfl_up_sync(FULL_MASK, inc, o);
+            inc += lane >= o ? up : 0;
+        }
+        if (r0 + lane < runs) DASS_ST(row + r0 + lane, carry + inc - v);
+        carry += __shfl_sync(FULL_MASK, inc, 31);
+    }
+    if (lane == 0) DASS_ST(totals + e, carry);
+}
+
+__global__ void __launch_bounds__(ER_SORT_WARPS * 32)
 expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len, int runs, int E, const int32_t *__restrict__ counts,
+                    const int32_t *__restrict__ totals,
                     int32_t *__restrict__ offsets, int32_t *__restrict__ slot, int32_t *__restrict__ source)
 {
     extern __shared__ int32_t er_smem[];
@@ -55,47 +83,49 @@ expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len,
     int32_t *total = er_smem + E;                           // [E] rows of all runs, then the experts' offsets
     int32_t *mine = er_smem + 2 * E;                        // [warps][E] this run's counts by warp, then next ranks
     __shared__ int32_t warp_sum[ER_SORT_WARPS];
+    constexpr int threads = ER_SORT_WARPS * 32, warps = ER_SORT_WARPS;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t f0 = blockIdx.x * run_len, f1 = f0 + run_len < n ? f0 + run_len : n;
-    const int64_t part = ((f1 - f0 + ER_SORT_WARPS - 1) / ER_SORT_WARPS + 31) / 32 * 32;
+    const int64_t part = ((f1 - f0 + warps - 1) / warps + 31) / 32 * 32;
     const int64_t w0 = f0 + warp * part, w1 = w0 + part < f1 ? w0 + part : f1;
 
-    for (int e = threadIdx.x; e < E * ER_SORT_WARPS; e += blockDim.x) mine[e] = 0;
+    for (int e = threadIdx.x; e < E * warps; e += blockDim.x) mine[e] = 0;
     for (int e = threadIdx.x; e < 2 * E; e += blockDim.x) er_smem[e] = 0;
     __syncthreads();
     for (int64_t f = w0 + lane; f < w1; f += 32) {
         const int id = DASS_LD(ids + f);
         if (id >= 0 && id < E) atomicAdd(&mine[warp * E + id], 1);
     }
-    if (runs > 1) {
-        // threads are laid over experts and, where there are fewer experts than threads, over slices of the runs
-        const int width = E < ER_SORT_THREADS ? E : ER_SORT_THREADS;
-        const int slices = ER_SORT_THREADS / width;
-        const int slice = threadIdx.x / width;
-        if (slice < slices)
-            for (int e = threadIdx.x % width; e < E; e += width) {
-                int32_t b = 0, a = 0;
-                for (int r = slice; r < runs; r += slices) {
-                    const int32_t c = DASS_LD(counts + (int64_t)r * E + e);
-                    a += c;
-                    b += r < (int)blockIdx.x ? c : 0;
-                }
-                atomicAdd(&total[e], a);                    // integer sums: any order gives the same
-                atomicAdd(&before[e], b);
+    if (totals) {                                           // the scan has run
+        for (int e = threadIdx.x; e < E; e += threads) {
+            total[e] = DASS_LD(totals + e);
+            before[e] = DASS_LD(counts + (int64_t)e * runs + blockIdx.x);
+        }
+    } else if (runs > 1) {
+        for (int e = warp; e < E; e += warps) {             // a warp per expert, lanes over the runs
+            int32_t b = 0, a = 0;
+            for (int r = lane; r < runs; r += 32) {
+                const int32_t c = DASS_LD(counts + (int64_t)e * runs + r);
+                a += c;
+                b += r < (int)blockIdx.x ? c : 0;
             }
+            a = __reduce_add_sync(FULL_MASK, a);
+            b = __reduce_add_sync(FULL_MASK, b);
+            if (lane == 0) { total[e] = a; before[e] = b; }
+        }
     }
     __syncthreads();
     if (runs == 1) {
         for (int e = threadIdx.x; e < E; e += blockDim.x) {
             int32_t a = 0;
-            for (int w = 0; w < ER_SORT_WARPS; ++w) a += mine[w * E + e];
+            for (int w = 0; w < warps; ++w) a += mine[w * E + e];
             total[e] = a;
         }
         __syncthreads();
     }
     // exclusive scan of total over the experts, a block's width at a time
     int32_t carry = 0;
-    for (int e0 = 0; e0 < E; e0 += ER_SORT_THREADS) {
+    for (int e0 = 0; e0 < E; e0 += threads) {
         const int e = e0 + threadIdx.x;
         const int32_t v = e < E ? total[e] : 0;
         int32_t inc = v;
@@ -107,8 +137,7 @@ expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len,
         if (lane == 31) warp_sum[warp] = inc;
         __syncthreads();
         int32_t base = carry, chunk = 0;
-#pragma unroll
-        for (int w = 0; w < ER_SORT_WARPS; ++w) {
+        for (int w = 0; w < warps; ++w) {
             const int32_t s = warp_sum[w];
             base += w < warp ? s : 0;
             chunk += s;
@@ -117,7 +146,7 @@ expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len,
         if (e < E) {
             if (blockIdx.x == 0) DASS_ST(offsets + e, at);
             int32_t next = at + before[e];
-            for (int w = 0; w < ER_SORT_WARPS; ++w) {       // first rank of every warp's part
+            for (int w = 0; w < warps; ++w) {       // first rank of every warp's part
                 const int32_t c = mine[w * E + e];
                 mine[w * E + e] = next;
                 next += c;
@@ -153,13 +182,17 @@ expert_place_kernel(const int32_t *__restrict__ ids, int64_t n, int64_t run_len,
 // longer than a block.  Loads are held as they lie in memory until all that a thread wants are in flight.
 struct ErRows {
     int64_t T, rows;                 // tokens, rows of the sorted side
-    int k;
+    int k, step;                     // choices per token, and of them taken at once (turns alike: 6 are 3 + 3)
     int vpr;                         // accesses per row
 };
 
 constexpr int ER_THREADS = 256;
-constexpr int ER_BATCH = 4;          // choices whose rows are in flight at once
-constexpr int ER_COLS = 2;           // accesses of a row per thread
+// Accesses of a row per thread: what a thread reads it reads at once, so these and BATCH, the choices it takes at once, set
+// the bytes in flight.  At 16 bytes: 4 choices of 2 accesses, or 2 of 4 where there are no more than two choices (16384
+// tokens, k = 2, d = 4096: the sum with residual 117 -> 89 us); 4 of 4 costs too many registers (k = 6, d = 2048: 98 ->
+// 202 us).  At single elements more.
+template <int VEC> constexpr int ER_GATHER_COLS = VEC == 1 ? 8 : 2;
+template <int VEC, int BATCH> constexpr int ER_SUM_COLS = (VEC == 1 ? 16 : 8) / BATCH;
 
 // Rows from *used on are zeroed, by all blocks together.
 template <bool BF16, int VEC, int COLS>
@@ -182,24 +215,25 @@ __global__ void __launch_bounds__(ER_THREADS)
 expert_gather_kernel(const void *__restrict__ src, int64_t lds, const int32_t *__restrict__ slot, const float *__restrict__ weight,
                      const int32_t *__restrict__ used, void *__restrict__ dst, int64_t ldd, ErRows r)
 {
+    constexpr int COLS = ER_GATHER_COLS<VEC>, BATCH = 4;
     const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int v0 = blockIdx.y * (blockDim.x * ER_COLS) + threadIdx.x;
+    const int v0 = blockIdx.y * (blockDim.x * COLS) + threadIdx.x;
     if (t < r.T && v0 < r.vpr) {
         const int32_t *to = slot + t * r.k;
-        RowRaw<BF16, VEC> raw[ER_COLS];
+        RowRaw<BF16, VEC> raw[COLS];
 #pragma unroll
-        for (int u = 0; u < ER_COLS; ++u)
+        for (int u = 0; u < COLS; ++u)
             if (v0 + u * (int)blockDim.x < r.vpr) raw_load<BF16, VEC, true>(raw[u], src, t * lds + (int64_t)(v0 + u * blockDim.x) * VEC);
-        for (int j0 = 0; j0 < r.k; j0 += ER_BATCH) {
-            int s[ER_BATCH];
+        for (int j0 = 0; j0 < r.k; j0 += BATCH) {
+            int s[BATCH];
 #pragma unroll
-            for (int q = 0; q < ER_BATCH; ++q) s[q] = j0 + q < r.k ? DASS_LD(to + j0 + q) : -1;
+            for (int q = 0; q < BATCH; ++q) s[q] = j0 + q < r.k ? DASS_LD(to + j0 + q) : -1;
 #pragma unroll
-            for (int q = 0; q < ER_BATCH; ++q) {
+            for (int q = 0; q < BATCH; ++q) {
                 if (s[q] < 0 || s[q] >= r.rows) continue;
                 const float w = weight ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f;
 #pragma unroll
-                for (int u = 0; u < ER_COLS; ++u) {
+                for (int u = 0; u < COLS; ++u) {
                     if (v0 + u * (int)blockDim.x >= r.vpr) continue;
                     float y[VEC];
                     raw_floats(raw[u], y);
@@ -212,47 +246,48 @@ expert_gather_kernel(const void *__restrict__ src, int64_t lds, const int32_t *_
             }
         }
     }
-    if (used) er_zero_tail<BF16, VEC, ER_COLS>(used, r.rows, r.vpr, dst, ldd, t, (int64_t)gridDim.x * blockDim.y, v0);
+    if (used) er_zero_tail<BF16, VEC, COLS>(used, r.rows, r.vpr, dst, ldd, t, (int64_t)gridDim.x * blockDim.y, v0);
 }
 
 // out[t] = residual[t] + sum_j weight[t,j] * rows[slot[t,j]], f32, j ascending, one rounding
-template <bool BF16, int VEC>
+template <bool BF16, int VEC, int BATCH>
 __global__ void __launch_bounds__(ER_THREADS)
 expert_combine_kernel(const void *__restrict__ rows, int64_t ldr, const int32_t *__restrict__ slot, const float *__restrict__ weight,
                       const void *residual, int64_t ldres, void *out, int64_t ldo, ErRows r)
 {
+    constexpr int COLS = ER_SUM_COLS<VEC, BATCH>;
     const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int v0 = blockIdx.y * (blockDim.x * ER_COLS) + threadIdx.x;
+    const int v0 = blockIdx.y * (blockDim.x * COLS) + threadIdx.x;
     if (t >= r.T || v0 >= r.vpr) return;
-    float acc[ER_COLS][VEC];
-    RowRaw<BF16, VEC> res[ER_COLS];
+    float acc[COLS][VEC];
+    RowRaw<BF16, VEC> res[COLS];
 #pragma unroll
-    for (int u = 0; u < ER_COLS; ++u) {
+    for (int u = 0; u < COLS; ++u) {
 #pragma unroll
         for (int c = 0; c < VEC; ++c) acc[u][c] = 0.f;
         if (residual && v0 + u * (int)blockDim.x < r.vpr)
             raw_load<BF16, VEC>(res[u], residual, t * ldres + (int64_t)(v0 + u * blockDim.x) * VEC);
     }
-    for (int j0 = 0; j0 < r.k; j0 += ER_BATCH) {
-        int s[ER_BATCH];
-        float w[ER_BATCH];
-        RowRaw<BF16, VEC> x[ER_BATCH][ER_COLS];
+    for (int j0 = 0; j0 < r.k; j0 += r.step) {
+        int s[BATCH];
+        float w[BATCH];
+        RowRaw<BF16, VEC> x[BATCH][COLS];
 #pragma unroll
-        for (int q = 0; q < ER_BATCH; ++q) s[q] = j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
+        for (int q = 0; q < BATCH; ++q) s[q] = q < r.step && j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
 #pragma unroll
-        for (int q = 0; q < ER_BATCH; ++q) {
+        for (int q = 0; q < BATCH; ++q) {
             if (s[q] >= r.rows) s[q] = -1;
             w[q] = s[q] >= 0 && weight ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f;
 #pragma unroll
-            for (int u = 0; u < ER_COLS; ++u)
+            for (int u = 0; u < COLS; ++u)
                 if (s[q] >= 0 && v0 + u * (int)blockDim.x < r.vpr)
                     raw_load<BF16, VEC, true>(x[q][u], rows, s[q] * ldr + (int64_t)(v0 + u * blockDim.x) * VEC);
         }
 #pragma unroll
-        for (int q = 0; q < ER_BATCH; ++q) {
+        for (int q = 0; q < BATCH; ++q) {
             if (s[q] < 0) continue;                               // a skipped choice adds nothing, whatever its row would hold
 #pragma unroll
-            for (int u = 0; u < ER_COLS; ++u) {
+            for (int u = 0; u < COLS; ++u) {
                 float v[VEC];
                 raw_floats(x[q][u], v);
 #pragma unroll
@@ -261,7 +296,7 @@ expert_combine_kernel(const void *__restrict__ rows, int64_t ldr, const int32_t 
         }
     }
 #pragma unroll
-    for (int u = 0; u < ER_COLS; ++u) {
+    for (int u = 0; u < COLS; ++u) {
         if (v0 + u * (int)blockDim.x >= r.vpr) continue;
         if (residual) {
             float v[VEC];
@@ -274,50 +309,51 @@ expert_combine_kernel(const void *__restrict__ rows, int64_t ldr, const int32_t 
 }
 
 // Gradient of the weighted sum: drows[slot[t,j]] = weight[t,j] * dout[t] and dweight[t,j] = <dout[t], rows[slot[t,j]]>.
-// blockDim.x threads per token, blockDim.y tokens a block; dout[t] is read once for ER_BATCH choices.
-template <bool BF16, int VEC>
+// blockDim.x threads per token, blockDim.y tokens a block; dout[t] is read once for BATCH choices.
+template <bool BF16, int VEC, int BATCH>
 __global__ void __launch_bounds__(ER_THREADS)
 expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const void *__restrict__ rows, int64_t ldr,
                                const int32_t *__restrict__ slot, const float *__restrict__ weight, const int32_t *__restrict__ used,
                                void *__restrict__ drows, int64_t lddr, float *__restrict__ dweight, ErRows r)
 {
-    __shared__ float part[ER_THREADS / 32][ER_BATCH];
+    constexpr int COLS = ER_SUM_COLS<VEC, BATCH>;
+    __shared__ float part[ER_THREADS / 32][BATCH];
     const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const bool live = t < r.T;
     const int width = blockDim.x;
-    for (int j0 = 0; j0 < r.k; j0 += ER_BATCH) {
-        int s[ER_BATCH];
-        float w[ER_BATCH], acc[ER_BATCH];
+    for (int j0 = 0; j0 < r.k; j0 += r.step) {
+        int s[BATCH];
+        float w[BATCH], acc[BATCH];
 #pragma unroll
-        for (int q = 0; q < ER_BATCH; ++q) {
-            s[q] = live && j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
+        for (int q = 0; q < BATCH; ++q) {
+            s[q] = live && q < r.step && j0 + q < r.k ? DASS_LD(slot + t * r.k + j0 + q) : -1;
             acc[q] = 0.f;
         }
 #pragma unroll
-        for (int q = 0; q < ER_BATCH; ++q) {
+        for (int q = 0; q < BATCH; ++q) {
             if (s[q] >= r.rows) s[q] = -1;
             w[q] = drows && weight && s[q] >= 0 ? DASS_LD(weight + t * r.k + j0 + q) : 1.0f;
         }
-        for (int v0 = threadIdx.x; live && v0 < r.vpr; v0 += ER_COLS * width) {
-            RowRaw<BF16, VEC> g[ER_COLS], x[ER_BATCH][ER_COLS];
+        for (int v0 = threadIdx.x; live && v0 < r.vpr; v0 += COLS * width) {
+            RowRaw<BF16, VEC> g[COLS], x[BATCH][COLS];
 #pragma unroll
-            for (int u = 0; u < ER_COLS; ++u) {
+            for (int u = 0; u < COLS; ++u) {
                 const int64_t col = (int64_t)(v0 + u * width) * VEC;
                 if (v0 + u * width >= r.vpr) continue;
                 raw_load<BF16, VEC>(g[u], dout, t * ldo + col);
                 if (dweight) {
 #pragma unroll
-                    for (int q = 0; q < ER_BATCH; ++q)
+                    for (int q = 0; q < BATCH; ++q)
                         if (s[q] >= 0) raw_load<BF16, VEC, true>(x[q][u], rows, s[q] * ldr + col);
                 }
             }
 #pragma unroll
-            for (int u = 0; u < ER_COLS; ++u) {
+            for (int u = 0; u < COLS; ++u) {
                 if (v0 + u * width >= r.vpr) continue;
                 float gf[VEC];
                 raw_floats(g[u], gf);
 #pragma unroll
-                for (int q = 0; q < ER_BATCH; ++q) {
+                for (int q = 0; q < BATCH; ++q) {
                     if (s[q] < 0) continue;
                     float v[VEC];
                     if (dweight) {
@@ -336,7 +372,7 @@ expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const
         if (dweight) {
             const int group = width < 32 ? width : 32;               // lanes of a token within a warp
 #pragma unroll
-            for (int q = 0; q < ER_BATCH; ++q)
+            for (int q = 0; q < BATCH; ++q)
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
                     const float other = __shfl_xor_sync(FULL_MASK, acc[q], o);
@@ -346,10 +382,10 @@ expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const
                 const int warp = (threadIdx.y * width + threadIdx.x) >> 5, first = (threadIdx.y * width) >> 5;
                 if ((threadIdx.x & 31) == 0)
 #pragma unroll
-                    for (int q = 0; q < ER_BATCH; ++q) part[warp][q] = acc[q];
+                    for (int q = 0; q < BATCH; ++q) part[warp][q] = acc[q];
                 __syncthreads();
 #pragma unroll
-                for (int q = 0; q < ER_BATCH; ++q) {
+                for (int q = 0; q < BATCH; ++q) {
                     acc[q] = 0.f;
                     for (int i = 0; i < width / 32; ++i) acc[q] += part[first + i][q];
                 }
@@ -357,24 +393,30 @@ expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const
             }
             if (live && threadIdx.x == 0)
 #pragma unroll
-                for (int q = 0; q < ER_BATCH; ++q)
-                    if (j0 + q < r.k) DASS_ST(dweight + t * r.k + j0 + q, acc[q]);
+                for (int q = 0; q < BATCH; ++q)
+                    if (q < r.step && j0 + q < r.k) DASS_ST(dweight + t * r.k + j0 + q, acc[q]);
         }
     }
     if (drows && used)
-        for (int v0 = threadIdx.x; v0 < r.vpr; v0 += ER_COLS * width)
-            er_zero_tail<BF16, VEC, ER_COLS>(used, r.rows, r.vpr, drows, lddr, t, (int64_t)gridDim.x * blockDim.y, v0);
+        for (int v0 = threadIdx.x; v0 < r.vpr; v0 += COLS * width)
+            er_zero_tail<BF16, VEC, COLS>(used, r.rows, r.vpr, drows, lddr, t, (int64_t)gridDim.x * blockDim.y, v0);
 }
 
 // ------------------------------------------------------------------ host side
-// Threads over `vpr` accesses of a row, `cols` each, as many rows as fill the block; blocks over rows and long rows.
+// Threads over a row's accesses, some each, as many rows as fill the block; blocks over rows and long rows.
 struct ErGrid { dim3 grid, block; };
-static ErGrid er_grid(int64_t rows, int vpr, int most)
+static ErGrid er_grid(int64_t rows, const ErRows &r, int cols, int most)
 {
     int x = 4;
-    while (x < most && x * ER_COLS < vpr) x *= 2;
+    while (x < most && x * cols < r.vpr) x *= 2;
     const int y = ER_THREADS / x;
-    return {dim3((unsigned)((rows + y - 1) / y), (unsigned)((vpr + x * ER_COLS - 1) / (x * ER_COLS))), dim3(x, y)};
+    return {dim3((unsigned)((rows + y - 1) / y), (unsigned)((r.vpr + x * cols - 1) / (x * cols))), dim3(x, y)};
+}
+
+static int er_sum_cols(bool vector, int64_t k)
+{
+    if (vector) return k <= 2 ? ER_SUM_COLS<8, 2> : ER_SUM_COLS<8, 4>;
+    return k <= 2 ? ER_SUM_COLS<1, 2> : ER_SUM_COLS<1, 4>;
 }
 
 static dass_status er_check(int64_t T, int64_t k, int64_t d, int dt)
@@ -397,7 +439,7 @@ dass_status dass_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t E, si
     if (T < 0 || k < 1 || E < 1) return DASS_ERR_SHAPE;
     if (E > ER_MAX_E || k > ER_MAX_K || T > ((1ll << 31) - 1) / k) return DASS_ERR_UNSUPPORTED;
     const int64_t runs = er_runs(T * k);
-    *bytes = runs > 1 ? (size_t)runs * (size_t)E * sizeof(int32_t) : 0;
+    *bytes = runs > 1 ? (size_t)(runs + 1) * (size_t)E * sizeof(int32_t) : 0;
     return DASS_OK;
 }
 
@@ -425,11 +467,16 @@ dass_status dass_expert_sort(const int32_t *expert, int64_t T, int64_t k, int64_
     DASS_BOUNDS_COMMIT(bs, st);
     int32_t *counts = static_cast<int32_t *>(workspace);
     if (runs > 1) {
-        expert_count_kernel<<<(unsigned)runs, ER_SORT_THREADS, (size_t)E * 4, st>>>(expert, n, run_len, (int)E, counts);
+        expert_count_kernel<<<(unsigned)runs, ER_SORT_WARPS * 32, (size_t)E * 4, st>>>(expert, n, run_len, (int)E, counts);
         if (cudaGetLastError() != cudaSuccess) return DASS_ERR_CUDA;
     }
-    expert_place_kernel<<<(unsigned)runs, ER_SORT_THREADS, (size_t)E * 4 * (2 + ER_SORT_WARPS), st>>>(expert, n, run_len, (int)runs, (int)E,
-                                                                                                     counts, offsets, slot, source);
+    int32_t *totals = runs > 1 && E > ER_SUM_EXPERTS ? counts + runs * E : nullptr;
+    if (totals) {
+        expert_scan_kernel<<<(unsigned)((E + ER_SORT_WARPS - 1) / ER_SORT_WARPS), ER_SORT_WARPS * 32, 0, st>>>(counts, totals, (int)runs, (int)E);
+        if (cudaGetLastError() != cudaSuccess) return DASS_ERR_CUDA;
+    }
+    expert_place_kernel<<<(unsigned)runs, ER_SORT_WARPS * 32, (size_t)E * 4 * (2 + ER_SORT_WARPS), st>>>(expert, n, run_len, (int)runs, (int)E,
+                                                                                                     counts, totals, offsets, slot, source);
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
 
@@ -450,7 +497,7 @@ dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx,
     const size_t elt = bf16 ? 2 : 4;
     const int vec = bf16 ? 8 : 4;
     const bool vector = rows_vec_ok(X, ldx, bf16) && rows_vec_ok(Xs, ldxs, bf16) && d % vec == 0;
-    const ErRows r{T, rows, (int)k, (int)(vector ? d / vec : d)};
+    const ErRows r{T, rows, (int)k, (int)(k <= 2 ? k : (k + (k + 3) / 4 - 1) / ((k + 3) / 4)), (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
     if (T > 0) DASS_BOUNDS_ADD(bs, X, ((size_t)(T - 1) * ldx + d) * elt);
     DASS_BOUNDS_ADD(bs, Xs, ((size_t)(rows - 1) * ldxs + d) * elt);
@@ -459,14 +506,12 @@ dass_status dass_expert_gather(const void *X, int64_t T, int64_t d, int64_t ldx,
     DASS_BOUNDS_ADD(bs, rows_used, 4);
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
-    const ErGrid g = er_grid(T > 0 ? T : rows, r.vpr, ER_THREADS);
-    if (bf16) {
-        if (vector) expert_gather_kernel<true, 8><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
-        else expert_gather_kernel<true, 1><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
-    } else {
-        if (vector) expert_gather_kernel<false, 4><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
-        else expert_gather_kernel<false, 1><<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r);
-    }
+    const ErGrid g = er_grid(T > 0 ? T : rows, r, vector ? ER_GATHER_COLS<8> : ER_GATHER_COLS<1>, ER_THREADS);
+    auto launch = [&](auto kernel) { kernel<<<g.grid, g.block, 0, st>>>(X, ldx, slot, weight, rows_used, Xs, ldxs, r); };
+    if (bf16 && vector) launch(expert_gather_kernel<true, 8>);
+    else if (bf16) launch(expert_gather_kernel<true, 1>);
+    else if (vector) launch(expert_gather_kernel<false, 4>);
+    else launch(expert_gather_kernel<false, 1>);
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
 
@@ -487,7 +532,7 @@ dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t
     const size_t elt = bf16 ? 2 : 4;
     const int vec = bf16 ? 8 : 4;
     const bool vector = rows_vec_ok(Ys, ldys, bf16) && rows_vec_ok(Y, ldy, bf16) && (!residual || rows_vec_ok(residual, ldr, bf16)) && d % vec == 0;
-    const ErRows r{T, rows, (int)k, (int)(vector ? d / vec : d)};
+    const ErRows r{T, rows, (int)k, (int)(k <= 2 ? k : (k + (k + 3) / 4 - 1) / ((k + 3) / 4)), (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
     if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
     DASS_BOUNDS_ADD(bs, residual, ((size_t)(T - 1) * ldr + d) * elt);
@@ -496,14 +541,12 @@ dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t
     DASS_BOUNDS_ADD(bs, weight, (size_t)T * k * 4);
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
-    const ErGrid g = er_grid(T, r.vpr, ER_THREADS);
-    if (bf16) {
-        if (vector) expert_combine_kernel<true, 8><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
-        else expert_combine_kernel<true, 1><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
-    } else {
-        if (vector) expert_combine_kernel<false, 4><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
-        else expert_combine_kernel<false, 1><<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r);
-    }
+    const ErGrid g = er_grid(T, r, er_sum_cols(vector, k), ER_THREADS);
+    auto launch = [&](auto kernel) { kernel<<<g.grid, g.block, 0, st>>>(Ys, ldys, slot, weight, residual, ldr, Y, ldy, r); };
+    if (bf16 && vector) k <= 2 ? launch(expert_combine_kernel<true, 8, 2>) : launch(expert_combine_kernel<true, 8, 4>);
+    else if (bf16) k <= 2 ? launch(expert_combine_kernel<true, 1, 2>) : launch(expert_combine_kernel<true, 1, 4>);
+    else if (vector) k <= 2 ? launch(expert_combine_kernel<false, 4, 2>) : launch(expert_combine_kernel<false, 4, 4>);
+    else k <= 2 ? launch(expert_combine_kernel<false, 1, 2>) : launch(expert_combine_kernel<false, 1, 4>);
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
 
@@ -526,7 +569,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     const int vec = bf16 ? 8 : 4;
     const bool vector = rows_vec_ok(dY, lddy, bf16) && (!dweight || rows_vec_ok(Ys, ldys, bf16)) && (!dYs || rows_vec_ok(dYs, lddys, bf16)) &&
                         d % vec == 0;
-    const ErRows r{T, rows, (int)k, (int)(vector ? d / vec : d)};
+    const ErRows r{T, rows, (int)k, (int)(k <= 2 ? k : (k + (k + 3) / 4 - 1) / ((k + 3) / 4)), (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
     DASS_BOUNDS_ADD(bs, dY, ((size_t)(T - 1) * lddy + d) * elt);
     if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
@@ -538,16 +581,14 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
     // few threads a token keep its sums inside a warp; a whole block where there are few tokens
-    ErGrid g = er_grid(T, r.vpr, T >= 148 * 32 ? 64 : ER_THREADS);
+    ErGrid g = er_grid(T, r, er_sum_cols(vector, k), T >= 148 * 32 ? 64 : ER_THREADS);
     g.grid.y = 1;                                                     // a token's threads walk its whole row
     const dim3 grid = g.grid, block = g.block;
-    if (bf16) {
-        if (vector) expert_combine_backward_kernel<true, 8><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
-        else expert_combine_backward_kernel<true, 1><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
-    } else {
-        if (vector) expert_combine_backward_kernel<false, 4><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
-        else expert_combine_backward_kernel<false, 1><<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r);
-    }
+    auto launch = [&](auto kernel) { kernel<<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r); };
+    if (bf16 && vector) k <= 2 ? launch(expert_combine_backward_kernel<true, 8, 2>) : launch(expert_combine_backward_kernel<true, 8, 4>);
+    else if (bf16) k <= 2 ? launch(expert_combine_backward_kernel<true, 1, 2>) : launch(expert_combine_backward_kernel<true, 1, 4>);
+    else if (vector) k <= 2 ? launch(expert_combine_backward_kernel<false, 4, 2>) : launch(expert_combine_backward_kernel<false, 4, 4>);
+    else k <= 2 ? launch(expert_combine_backward_kernel<false, 1, 2>) : launch(expert_combine_backward_kernel<false, 1, 4>);
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
 }
 

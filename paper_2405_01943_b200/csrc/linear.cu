@@ -5,7 +5,7 @@
 
 namespace dass {
 
-dass_status linear_simt_launch(const LinearArgs &a);       // linear_simt.cu
+dass_status linear_f32_launch(const LinearArgs &a);        // linear_f32.cu
 dass_status linear_tc_launch(const LinearArgs &a, int columns);         // linear_tc.cu
 dass_status linear_few_launch(const LinearArgs &a, int eights, int split);        // linear_few.cu
 dass_status linear_mid_launch(const LinearArgs &a, int rows, int split);        // linear_mid.cu
@@ -138,7 +138,7 @@ dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const 
     DASS_BOUNDS_ADD(bs, Y, ((size_t)(T - 1) * ldy + N) * (bf16 ? 2 : 4));
     DASS_BOUNDS_ADD(bs, offsets, (size_t)(groups + 1) * 4);
     DASS_BOUNDS_COMMIT(bs, a.st);
-    if (!bf16) return linear_simt_launch(a);
+    if (!bf16) return linear_f32_launch(a);
     const LinPlan plan = lin_plan(a);
     return plan.path == 1 ? linear_few_launch(a, plan.tile, plan.split) : plan.path == 3 ? linear_mid_launch(a, plan.tile, plan.split) : linear_tc_launch(a, plan.tile);
 }
