@@ -1,12 +1,14 @@
 // The router's selection: the k experts with the highest logits of every token, their softmax weights, and the gradient.
 //
 // A token's row is held in registers by a group of L lanes (a power of two), V consecutive logits to a lane, so a warp
-// works on 32 / L tokens.  A logit becomes an unsigned key of the same order (masked: 0), every lane keeps the largest
-// of its keys, and each of the k rounds takes the group's maximum (log2 L shuffles) and lets the lowest lane that holds
-// it remove its lowest element of that value: lanes hold consecutive indices, so equal logits go to the lower index.
-// Sums are in f32 and in a fixed order.
+// works on 32 / L tokens.  A logit becomes an unsigned key of the same order (masked: 0).  Its last log2(V L) bits give way
+// to the index, lower indices above higher ones: keys are then unique, and each of the k rounds is a maximum over the
+// group and a compare that removes it.  For bf16 nothing is lost, the bits are empty.  For f32 two chosen logits, or the
+// last chosen and the first not, that agree in all but those bits leave the order open: such a warp (one in about a
+// hundred on random logits of 128 experts) repeats its tokens with whole keys, each round finding the lowest lane and element
+// that hold the maximum.  Sums are in f32 and in a fixed order.
 //
-// Bound: the logits are read once, k ids and weights are written; with few tokens the launch is what is left.
+// Bound: instructions, RT_NOTE.
 #include "rows_common.cuh"
 
 namespace dass {
@@ -78,37 +80,62 @@ route_topk_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld,
     int32_t *s_id = reinterpret_cast<int32_t *>(rt_smem) + (threadIdx.x / L) * k;
     uint32_t *s_key = rt_smem + TOKENS * k + (threadIdx.x / L) * k;
 
+    constexpr uint32_t LOW = V * L - 1;                             // the bits that hold V * L - 1 - index
     uint32_t key[V];
-    rt_load<BF16, VECTOR, V>(logits, (live ? t : 0) * ld, gl * V, live ? E : 0, key);
-
-    float all = 0.f, top = 0.f;
-    uint32_t best = 0u;
+    auto load_keys = [&]() { rt_load<BF16, VECTOR, V>(logits, (live ? t : 0) * ld, gl * V, live ? E : 0, key); };
+    load_keys();
 #pragma unroll
-    for (int i = 0; i < V; ++i) best = max(best, key[i]);
-    const unsigned group_bits = (L == 32 ? FULL_MASK : ((1u << (L & 31)) - 1u)) << (lane & ~(L - 1));
-    for (int j = 0; j < k; ++j) {
+    for (int i = 0; i < V; ++i) key[i] = key[i] ? (key[i] & ~LOW) | (LOW - (gl * V + i)) : 0u;
+    uint32_t best = 0u, last = 0u;
+    bool open = false;
+    for (int j = 0; j <= k; ++j) {
+        best = 0u;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { key[i] = key[i] == last ? 0u : key[i]; best = max(best, key[i]); }
         const uint32_t m = group_max<L>(best);
-        if (j == 0) {
-            top = rt_value(m);
-            if (over_all) {
+        open |= !BF16 && m && ((last ^ m) & ~LOW) == 0u;
+        if (j < k && gl == 0) s_key[j] = m;
+        last = m;
+    }
+    const bool fast = !__any_sync(FULL_MASK, open);
+    if (!fast) {
+        load_keys();
+        best = 0u;
 #pragma unroll
-                for (int i = 0; i < V; ++i) all += key[i] ? expf(rt_value(key[i]) - top) : 0.f;
+        for (int i = 0; i < V; ++i) best = max(best, key[i]);
+        const unsigned group_bits = (L == 32 ? FULL_MASK : ((1u << (L & 31)) - 1u)) << (lane & ~(L - 1));
+        for (int j = 0; j < k; ++j) {
+            const uint32_t m = group_max<L>(best);
+            const unsigned holders = __ballot_sync(FULL_MASK, best == m) & group_bits;
+            if (lane == __ffs(holders) - 1) {
+                int at = 0;
+#pragma unroll
+                for (int i = V - 1; i >= 0; --i) at = key[i] == m ? i : at;
+                s_id[j] = m ? gl * V + at : -1;
+                s_key[j] = m;
+                best = 0u;
+#pragma unroll
+                for (int i = 0; i < V; ++i) { key[i] = i == at ? 0u : key[i]; best = max(best, key[i]); }
             }
-        }
-        const unsigned holders = __ballot_sync(FULL_MASK, best == m) & group_bits;
-        if (lane == __ffs(holders) - 1) {
-            int at = 0;
-#pragma unroll
-            for (int i = V - 1; i >= 0; --i) at = key[i] == m ? i : at;
-            s_id[j] = m ? gl * V + at : -1;
-            s_key[j] = m;
-            best = 0u;
-#pragma unroll
-            for (int i = 0; i < V; ++i) { key[i] = i == at ? 0u : key[i]; best = max(best, key[i]); }
         }
     }
     __syncwarp();
-    float chosen = 0.f;
+    for (int j = gl; live && fast && j < k; j += L) {               // the exact logits of the indices found
+        const uint32_t m = s_key[j];
+        const int id = m ? (int)(LOW - (m & LOW)) : -1;
+        float x[1] = {0.f};
+        if (m) row_load<BF16, 1>(logits, t * ld + id, x);
+        s_id[j] = id;
+        s_key[j] = m ? rt_key(x[0]) : 0u;
+    }
+    __syncwarp();
+    const float top = rt_value(s_key[0]);
+    float all = 0.f, chosen = 0.f;
+    if (over_all) {
+        rt_load<BF16, VECTOR, V>(logits, (live ? t : 0) * ld, gl * V, live ? E : 0, key);
+#pragma unroll
+        for (int i = 0; i < V; ++i) all += key[i] ? expf(rt_value(key[i]) - top) : 0.f;
+    }
     if (!over_all)
         for (int j = gl; j < k; j += L) chosen += s_key[j] ? expf(rt_value(s_key[j]) - top) : 0.f;
     const float total = group_sum<L>(over_all ? all : chosen);
@@ -144,28 +171,36 @@ route_topk_backward_kernel(const void *__restrict__ logits, int64_t T, int E, in
 #pragma unroll
         for (int i = 0; i < V; ++i) key[i] = 0u;
     }
-    auto chosen_key = [&](int j) -> uint32_t {                       // key of the j-th chosen expert, 0 if there is none
-        const int id = DASS_LD(expert + t * k + j);
-        if (id < 0 || id >= E) return 0u;
-        float x[1];
-        row_load<BF16, 1>(logits, t * ld + id, x);
-        return rt_key(x[0]);
-    };
-    if (live && !over_all)
-        for (int j = gl; j < k; j += L) m = max(m, chosen_key(j));
+    constexpr int J = L >= 4 ? 32 / L : 8;                           // choices of a lane: k <= min(32, V L)
+    int id[J];
+    uint32_t ck[J];
+    float dw[J], ce[J];
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        const int j = gl + q * L;
+        id[q] = live && j < k ? DASS_LD(expert + t * k + j) : -1;
+        dw[q] = live && j < k ? DASS_LD(dweight + t * k + j) : 0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        float x[1] = {0.f};
+        const bool in = id[q] >= 0 && id[q] < E;
+        if (in) row_load<BF16, 1>(logits, t * ld + id[q], x);
+        ck[q] = in ? rt_key(x[0]) : 0u;
+        m = max(m, ck[q]);
+    }
     const float top = rt_value(group_max<L>(m));
     float sum = 0.f, dot = 0.f;
     if (over_all) {
 #pragma unroll
         for (int i = 0; i < V; ++i) sum += key[i] ? expf(rt_value(key[i]) - top) : 0.f;
     }
-    if (live)
-        for (int j = gl; j < k; j += L) {
-            const uint32_t c = chosen_key(j);
-            const float e = c ? expf(rt_value(c) - top) : 0.f;
-            if (!over_all) sum += e;
-            if (c) dot += e * DASS_LD(dweight + t * k + j);
-        }
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        ce[q] = ck[q] ? expf(rt_value(ck[q]) - top) : 0.f;
+        if (!over_all) sum += ce[q];
+        if (ck[q]) dot += ce[q] * dw[q];
+    }
     sum = group_sum<L>(sum);
     dot = group_sum<L>(dot);
     const float share = sum > 0.f ? 1.0f / sum : 0.f;
@@ -188,14 +223,12 @@ route_topk_backward_kernel(const void *__restrict__ logits, int64_t T, int E, in
         }
     }
     __syncwarp();
-    if (live)
-        for (int j = gl; j < k; j += L) {
-            const uint32_t c = chosen_key(j);
-            if (!c) continue;
-            const float p = expf(rt_value(c) - top) * share;
-            const float g[1] = {p * (DASS_LD(dweight + t * k + j) - s)};
-            row_store<BF16, 1>(dlogits, t * ldd + DASS_LD(expert + t * k + j), g);
-        }
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        if (!ck[q]) continue;
+        const float g[1] = {ce[q] * share * (dw[q] - s)};
+        row_store<BF16, 1>(dlogits, t * ldd + id[q], g);
+    }
 }
 
 struct RouteArgs {
