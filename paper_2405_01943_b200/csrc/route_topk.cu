@@ -1,14 +1,16 @@
 // The router's selection: the k experts with the highest logits of every token, their softmax weights, and the gradient.
 //
 // A token's row is held in registers by a group of L lanes (a power of two), V consecutive logits to a lane, so a warp
-// works on 32 / L tokens.  A logit becomes an unsigned key of the same order (masked: 0).  Its last log2(V L) bits give way
-// to the index, lower indices above higher ones: keys are then unique, and each of the k rounds is a maximum over the
-// group and a compare that removes it.  For bf16 nothing is lost, the bits are empty.  For f32 two chosen logits, or the
-// last chosen and the first not, that agree in all but those bits leave the order open: such a warp (one in about a
-// hundred on random logits of 128 experts) repeats its tokens with whole keys, each round finding the lowest lane and element
-// that hold the maximum.  Sums are in f32 and in a fixed order.
+// works on 32 / L tokens.  A logit becomes an unsigned key of the same order (masked: 0).  Its last log2(V L) bits give
+// way to the index, lower indices above higher ones: keys are then unique.  Up to 8 of up to 256 experts: every lane sorts
+// its 8 keys and log2 L merges of two lists leave the group's 8 largest in order.  Else each of k rounds is a maximum over
+// the group and a compare that removes it.  For bf16 nothing is lost, the bits are empty.  For f32 two chosen logits, or a
+// chosen one and one left out, that agree in all but those bits leave the order open: such a warp (one in about a hundred
+// on random logits of 128 experts) repeats its tokens with whole keys, each round finding the lowest lane and element that
+// hold the maximum.  Sums are in f32 and in a fixed order.
 //
-// Bound: instructions, RT_NOTE.
+// Bound: instruction issue with many tokens (65536 x 128 f32, k = 8: 29 us; rounds instead of sorted lists 31.5; the bytes would
+// take 6), the launch with few.
 #include "rows_common.cuh"
 
 namespace dass {
@@ -66,6 +68,43 @@ __device__ __forceinline__ void rt_load(const void *logits, int64_t row, int e0,
     }
 }
 
+__device__ __forceinline__ void order_pair(uint32_t &a, uint32_t &b)
+{
+    const uint32_t hi = max(a, b);
+    b = min(a, b);
+    a = hi;
+}
+// 8 keys in descending order (an odd-even merge network of 19 comparators)
+__device__ __forceinline__ void sort8(uint32_t (&k)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) order_pair(k[i], k[i + 1]);
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) { order_pair(k[i], k[i + 2]); order_pair(k[i + 1], k[i + 3]); order_pair(k[i + 1], k[i + 2]); }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) order_pair(k[i], k[i + 4]);
+    order_pair(k[2], k[4]); order_pair(k[3], k[5]);
+    order_pair(k[1], k[2]); order_pair(k[3], k[4]); order_pair(k[5], k[6]);
+}
+// The 8 largest of the group's keys, descending, in every lane: the 8 largest of two descending lists are the larger of
+// each key and its counterpart from the other end, a bitonic list that three strides order.
+template <int L> __device__ __forceinline__ void merge8(uint32_t (&k)[8])
+{
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) {
+        uint32_t other[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) other[i] = __shfl_xor_sync(FULL_MASK, k[7 - i], o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = max(k[i], other[i]);
+#pragma unroll
+        for (int s = 4; s > 0; s >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(i & s)) order_pair(k[i], k[i + s]);
+    }
+}
+
 template <bool BF16, bool VECTOR, int V, int L>
 __global__ void __launch_bounds__(RT_THREADS)
 route_topk_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, bool over_all,
@@ -88,14 +127,32 @@ route_topk_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld,
     for (int i = 0; i < V; ++i) key[i] = key[i] ? (key[i] & ~LOW) | (LOW - (gl * V + i)) : 0u;
     uint32_t best = 0u, last = 0u;
     bool open = false;
-    for (int j = 0; j <= k; ++j) {
-        best = 0u;
+    if (V == 8 && k <= 8) {
+        uint32_t top8[8];
 #pragma unroll
-        for (int i = 0; i < V; ++i) { key[i] = key[i] == last ? 0u : key[i]; best = max(best, key[i]); }
-        const uint32_t m = group_max<L>(best);
-        open |= !BF16 && m && ((last ^ m) & ~LOW) == 0u;
-        if (j < k && gl == 0) s_key[j] = m;
-        last = m;
+        for (int i = 0; i < 8; ++i) top8[i] = key[i % V];
+        sort8(top8);
+        merge8<L>(top8);
+        uint32_t edge = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i < k) edge = top8[i];
+            if (i < k && gl == 0) s_key[i] = top8[i];
+            if (i > 0) open |= i < k && top8[i] && ((top8[i] ^ top8[i > 0 ? i - 1 : 0]) & ~LOW) == 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) open |= edge && key[i] < edge && ((key[i] ^ edge) & ~LOW) == 0u;
+        open &= !BF16;
+    } else {
+        for (int j = 0; j <= k; ++j) {
+            best = 0u;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { key[i] = key[i] == last ? 0u : key[i]; best = max(best, key[i]); }
+            const uint32_t m = group_max<L>(best);
+            open |= !BF16 && m && ((last ^ m) & ~LOW) == 0u;
+            if (j < k && gl == 0) s_key[j] = m;
+            last = m;
+        }
     }
     const bool fast = !__any_sync(FULL_MASK, open);
     if (!fast) {
