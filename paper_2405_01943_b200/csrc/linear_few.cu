@@ -8,6 +8,9 @@
 // memory here; no shared-memory round trip, TMEM or tensor map stands between a load and its use, and blocks are small
 // enough that the last wave is short.  A cluster of SPLIT blocks shares the columns and splits k further where there are
 // few columns; sums over the warps and the cluster's blocks are taken in a fixed order.
+//
+// Bound by the launch and the latency of a few loads: 512 x 1024 3.5 us, 2048 x 2048 5.8 us for up to 8 rows (linear_mid.cu:
+// 5.9 and 7.7); 14336 x 4096 gated 44 us, 5.2 TB/s (linear_mid.cu 40).
 #include "linear_common.cuh"
 #include "linear_tc.cuh"
 #include "tc_pair.cuh"
