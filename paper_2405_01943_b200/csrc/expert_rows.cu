@@ -312,7 +312,7 @@ expert_combine_kernel(const void *__restrict__ rows, int64_t ldr, const int32_t 
 // blockDim.x threads per token, blockDim.y tokens a block; dout[t] is read once for BATCH choices.  Three blocks to an SM
 // (held to 80 registers): 16384 tokens, k = 6, d = 2048 take 146 us, with two blocks 170.
 template <bool BF16, int VEC, int BATCH>
-__global__ void __launch_bounds__(ER_THREADS, VEC == 1 ? 1 : 3)
+__global__ void __launch_bounds__(ER_THREADS, VEC == 1 ? 0 : 3)
 expert_combine_backward_kernel(const void *__restrict__ dout, int64_t ldo, const void *__restrict__ rows, int64_t ldr,
                                const int32_t *__restrict__ slot, const float *__restrict__ weight, const int32_t *__restrict__ used,
                                void *__restrict__ drows, int64_t lddr, float *__restrict__ dweight, ErRows r)
