@@ -277,21 +277,6 @@ bool tc_make_map(CUtensorMap *map, const void *ptr, int64_t rows, int64_t cols, 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// `mats` such matrices, mat_stride elements apart, as one map of three dimensions: rows past a matrix's end read as zero,
-// not as the next matrix's.
-bool tc_make_map_3d(CUtensorMap *map, const void *ptr, int64_t mats, int64_t rows, int64_t cols, int64_t ld, int64_t mat_stride, int box_rows)
-{
-    EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)mats};
-    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)(mats > 1 ? mat_stride : rows * ld) * 2};
-    const cuuint32_t box[3] = {(cuuint32_t)TC_BK, (cuuint32_t)box_rows, 1};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Row-major bf16 matrix [rows x cols] with pitch ld, plain (un-swizzled) boxes of box_cols x box_rows elements;
 // out-of-range elements read as zero.  Used by the streaming stage-(b) kernels.
 bool tile_map_bf16(CUtensorMap *map, const void *ptr, int64_t rows, int64_t cols, int64_t ld, int box_cols, int box_rows)

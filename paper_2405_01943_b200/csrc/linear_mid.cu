@@ -265,7 +265,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
 int device_sm_count();                                                                                       // dass_abi.cu
 int *linear_status_word();                                                                                   // linear.cu
 bool tc_make_map(CUtensorMap *map, const void *ptr, int64_t rows, int64_t cols, int64_t ld, int box_rows);   // calib_tc.cu
-bool tc_make_map_3d(CUtensorMap *map, const void *ptr, int64_t mats, int64_t rows, int64_t cols, int64_t ld, int64_t mat_stride, int box_rows);
+bool tc_make_map_3d(CUtensorMap *map, const void *ptr, int64_t mats, int64_t rows, int64_t cols, int64_t ld, int64_t mat_stride, int box_rows);   // linear_tc.cu
 
 template <int NT, bool GLU>
 static dass_status lm_launch(const LinearArgs &a, int split)
