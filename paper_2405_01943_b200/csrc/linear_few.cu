@@ -121,6 +121,7 @@ linear_few_kernel(const LinearArgs a, int col_tiles, int split)
         for (int v = 1; v < LW_WARPS; ++v) s += part[v][o];
         sum[o] = s;
     }
+    __syncwarp();                                            // the cluster barrier wants whole warps
     if (split > 1) cluster_sync_all(); else __syncthreads();
     const int rows = (int)(tile.hi - tile.lo);
     const uint32_t sum_addr = smem_u32(sum);
@@ -149,6 +150,7 @@ linear_few_kernel(const LinearArgs a, int col_tiles, int split)
         if (a.residual) { row_load<true, 1>(a.residual, t * a.ldr + n, b); y[0] += b[0]; }
         row_store<true, 1>(a.Y, t * a.ldy + n, y);
     }
+    __syncwarp();
     if (split > 1) cluster_sync_all();                       // the others may still read this block's sums
 }
 

@@ -189,7 +189,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         bool ok = true;
         const uint64_t pol_w = l2_policy_evict_first(), pol_x = l2_policy_evict_last();
         for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
+            if (!warp_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
             const uint32_t sbase = base + stage * S::STAGE, full = bar_full + 8 * stage;
             if (elect_one()) {
                 mbar_arrive_expect_tx(full, S::STAGE);
@@ -206,7 +206,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         uint32_t stage = 0, phase = 0;
         bool ok = true;
         for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
+            if (!warp_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
             tc_fence_after();
             const uint32_t sbase = base + stage * S::STAGE;
             if (elect_one()) {
@@ -228,7 +228,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     } else {
         // accumulators to shared memory: lane = column of Y, accumulator column = row of X
         const int quad = warp & 3;
-        if (mbar_wait(bar_acc, 0, abort_flag)) {
+        if (warp_wait(bar_acc, 0, abort_flag)) {
             tc_fence_after();
             const uint32_t addr = tmem_base + ((uint32_t)(quad * 32) << 16);
 #pragma unroll 1
@@ -245,6 +245,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
     }
     tc_fence_before();
+    __syncwarp();                                                 // the cluster barrier wants whole warps
     if (p.split > 1) cluster_sync_all(); else __syncthreads();
     if (*abort_flag) {
         for (int i = 0; i < 20; ++i) __nanosleep(1000000);       // failure path: let what was issued land
@@ -254,6 +255,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         if (p.vec) lm_finish<NT, GLU, 1>(p, tile, col, r0, r1, sums);
         else lm_finish<NT, GLU, 16>(p, tile, col, r0, r1, sums);
     }
+    __syncwarp();
     if (p.split > 1) cluster_sync_all(); else __syncthreads();   // sums may still be read by the cluster's other blocks
     if (warp == 1) {
         tc_fence_after();

@@ -168,7 +168,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
             const int a_row = it.row + (int)rank * LT_BM;
             const int b_row = it.col + (GLU ? 0 : (int)rank * (BN / 2));
             for (int kb = 0; kb < p.k_blocks; ++kb) {
-                if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
+                if (!warp_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
                 const uint32_t sbase = base + stage * STAGE_BYTES;
                 const uint32_t fb = leader_full + 8 * stage;
                 if (elect_one()) {
@@ -190,11 +190,11 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
             const int64_t items = (int64_t)first_tile[p.groups] * p.col_tiles;
             for (int64_t idx = pair; ok && idx < items; idx += pairs, ++tile) {
                 const uint32_t as = tile & 1u;
-                if (!mbar_wait(bar_acc_empty + 8 * as, ((tile >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                if (!warp_wait(bar_acc_empty + 8 * as, ((tile >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t acc_addr = tmem_base + as * BN;
                 for (int kb = 0; kb < p.k_blocks; ++kb) {
-                    if (!mbar_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                    if (!warp_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t sbase = base + stage * STAGE_BYTES;
                     if (elect_one()) {
@@ -246,7 +246,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                 }
             };
             if (p.r_vec && c0 < c1) fetch_residual(c0);
-            if (!mbar_wait(bar_acc_full + 8 * as, (tile >> 1) & 1u, abort_flag)) { ok = false; break; }
+            if (!warp_wait(bar_acc_full + 8 * as, (tile >> 1) & 1u, abort_flag)) { ok = false; break; }
             tc_fence_after();
             const uint32_t acc_addr = lane_addr + as * BN;
 #pragma unroll 1

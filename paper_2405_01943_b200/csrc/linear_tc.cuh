@@ -21,6 +21,12 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
     return is != 0;
 }
+// A bounded wait of a whole warp with one answer for all its lanes: where the wait runs out for some of them only, none
+// goes on into an instruction that expects the others.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    return __all_sync(FULL_MASK, mbar_wait(bar, parity, abort_flag));
+}
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
