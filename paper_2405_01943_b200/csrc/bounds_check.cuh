@@ -4,8 +4,9 @@
 // the tensor map in hardware).  In the regular build they are the plain intrinsics.  Built with -DDASS_BOUNDS_CHECK
 // (python -m paper_2405_01943_b200.build --bounds-check: the whole library as ONE translation unit, so that the table
 // below exists once), each entry point first registers the address ranges of the buffers it was given, and every
-// access is tested against them: an access outside all ranges is SKIPPED (a load yields zero) and counted, with the
-// first offender's address, width and source line kept for dass_bounds_report.  Nothing traps and nothing faults.
+// access is tested against them: an access outside all ranges, or at an address that is not a multiple of its width
+// (which the hardware answers with a fault), is SKIPPED (a load yields zero) and counted, with the first offender's
+// address, width and source line kept for dass_bounds_report.  Nothing traps and nothing faults.
 // Internal header.
 #pragma once
 
@@ -30,11 +31,19 @@ struct BoundsReport {
 static __device__ BoundsTable g_bounds;
 static __device__ BoundsReport g_bounds_report;
 
+// Whether an access of nbytes (a power of two) at address a is aligned and lies in one of the ranges.
+__host__ __device__ __forceinline__ bool access_allowed(const BoundsTable &t, unsigned long long a, unsigned nbytes)
+{
+    if (a & (nbytes - 1)) return false;
+    for (int i = 0; i < t.n; ++i)
+        if (a >= t.lo[i] && a + nbytes <= t.hi[i]) return true;
+    return false;
+}
+
 __device__ __forceinline__ bool access_ok(const void *p, unsigned nbytes, unsigned line)
 {
     const unsigned long long a = (unsigned long long)p;
-    for (int i = 0; i < g_bounds.n; ++i)
-        if (a >= g_bounds.lo[i] && a + nbytes <= g_bounds.hi[i]) return true;
+    if (access_allowed(g_bounds, a, nbytes)) return true;
     if (atomicAdd(&g_bounds_report.violations, 1u) == 0u) {
         g_bounds_report.first_addr = a;
         g_bounds_report.first_bytes = nbytes;
