@@ -30,6 +30,15 @@ inline int64_t lin_rows_wanted(const LinearArgs &a)
     return twice < a.T ? twice : a.T;
 }
 
+// Whether 8 bf16 columns of Y, of the residual and of a group's row of either bias are one aligned 16-byte access each.
+// Row g of a bias [groups x N] begins g * N elements in: past the first group N decides, whichever bias is there.
+inline bool lin_wide_ok(const LinearArgs &a)
+{
+    auto whole = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
+    return rows_vec_ok(a.Y, a.ldy, true) && (!a.residual || rows_vec_ok(a.residual, a.ldr, true)) && whole(a.bias) && whole(a.bias_up) &&
+           ((!a.bias && !a.bias_up) || a.groups == 1 || a.N % 8 == 0);
+}
+
 // Rows [lo, hi) of group g, whatever the offsets hold: never outside [0, T).
 __device__ __forceinline__ void lin_group_rows(const int32_t *offsets, int g, int64_t T, int64_t &lo, int64_t &hi)
 {

@@ -288,9 +288,7 @@ static dass_status lm_launch(const LinearArgs &a, int split)
     const int64_t blocks = (int64_t)p.col_tiles * (a.offsets ? groups : p.row_tiles);      // that will have work
     p.split = split < p.k_blocks ? split : 1;
     p.stages = blocks * p.split * 10 <= 8 * device_sm_count() ? S::DEEP : S::SHARED;        // clusters do not fill every SM
-    auto whole = [](const void *q) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0; };
-    p.vec = rows_vec_ok(a.Y, a.ldy, true) && (!a.residual || rows_vec_ok(a.residual, a.ldr, true)) && whole(a.bias) && whole(a.bias_up) &&
-            (!a.bias || a.groups == 1 || a.N % 8 == 0);
+    p.vec = lin_wide_ok(a);
     p.status = linear_status_word();
     if (!p.status) return DASS_ERR_CUDA;
     const int64_t grid = (int64_t)p.col_tiles * p.row_tiles * p.split;
