@@ -193,6 +193,23 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _new(t: torch.Tensor, shape, dtype: Optional[torch.dtype], stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """An uninitialised tensor on t's device for a call on `stream`.
+
+    Memory from the allocator belongs to the stream that was current: it may still be in use by that stream's earlier work,
+    and once released it is handed to that stream's later work, whatever another stream does with it.  So the tensor comes
+    from the pool of the stream that the call runs on, and is also kept until what the caller's current stream has queued
+    by its release is done."""
+    if stream is None:
+        return t.new_empty(shape, dtype=dtype)
+    here = torch.cuda.current_stream(t.device)
+    with torch.cuda.stream(stream):
+        out = t.new_empty(shape, dtype=dtype)
+    if here != stream:
+        out.record_stream(here)
+    return out
+
+
 # ----------------------------------------------------------------------------- stage (a)
 
 def calib_workspace_bytes(T: int, d: int, I: int, dtype: torch.dtype) -> int:
@@ -509,7 +526,7 @@ def mlp_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.T
 # ----------------------------------------------------------------------------- mixture of experts
 #
 # These calls are made once per layer and decode step, so what they do on the host is kept short: one pass over each
-# tensor's shape and strides, outputs from new_empty, the stream by its handle.
+# tensor's shape and strides, the stream by its handle.
 
 _CODES = {torch.bfloat16: BF16, torch.float32: F32}
 
@@ -554,11 +571,11 @@ def route_topk(logits: torch.Tensor, k: int, renormalise: bool = True, expert: O
     T, E, ld = _rows(logits, "logits")
     k, dt = int(k), _code(logits)
     if expert is None:
-        expert = logits.new_empty((T, max(k, 0)), dtype=torch.int32)
+        expert = _new(logits, (T, max(k, 0)), torch.int32, stream)
     else:
         _same(expert, "expert", (T, k), torch.int32, logits.device)
     if weight is None:
-        weight = logits.new_empty((T, max(k, 0)), dtype=torch.float32)
+        weight = _new(logits, (T, max(k, 0)), torch.float32, stream)
     else:
         _same(weight, "weight", (T, k), torch.float32, logits.device)
     if T:
@@ -576,7 +593,7 @@ def route_topk_backward(logits: torch.Tensor, expert: torch.Tensor, dweight: tor
     ids = _same(expert, "expert", (T, k), torch.int32, logits.device)
     dw = _same(dweight, "dweight", (T, k), torch.float32, logits.device)
     if dlogits is None:
-        dlogits, ldd = logits.new_empty((T, E)), E
+        dlogits, ldd = _new(logits, (T, E), None, stream), E
     else:
         ldd = _like(dlogits, "dlogits", T, E, logits)
     if T:
@@ -602,20 +619,20 @@ def expert_sort(expert: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = 
     ids = _same(expert, "expert", (T, k), torch.int32, dev)
     edges = E + 1 if E > 0 else 1
     if offsets is None:
-        offsets = expert.new_empty(edges)
+        offsets = _new(expert, edges, None, stream)
     else:
         _same(offsets, "offsets", (edges,), torch.int32, dev)
     if slot is None:
-        slot = expert.new_empty((T, k))
+        slot = _new(expert, (T, k), None, stream)
     else:
         _same(slot, "slot", (T, k), torch.int32, dev)
     if source is None:
-        source = expert.new_empty(T * k)
+        source = _new(expert, T * k, None, stream)
     else:
         _same(source, "source", (T * k,), torch.int32, dev)
     if workspace is None:
         need = expert_sort_workspace_bytes(T, k, E)
-        workspace = expert.new_empty(need, dtype=torch.uint8) if need else None
+        workspace = _new(expert, need, torch.uint8, stream) if need else None
     _check(load().dass_expert_sort(ids, T, k, E, offsets.data_ptr(), slot.data_ptr(), source.data_ptr(),
                                    _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream_of(expert, stream)),
            "dass_expert_sort")
@@ -649,7 +666,7 @@ def expert_gather(X: torch.Tensor, slot: torch.Tensor, offsets: Optional[torch.T
         raise ValueError("X and slot must have the same number of tokens")
     if Xs is None:
         rows, ldxs = T * k, d
-        Xs = X.new_empty((rows, d))
+        Xs = _new(X, (rows, d), None, stream)
     else:
         rows = Xs.shape[0]
         ldxs = _like(Xs, "Xs", rows, d, X)
@@ -666,7 +683,7 @@ def expert_combine(Ys: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.
     T, k = _slots(slot, weight, Ys.device)
     ldr = _like(residual, "residual", T, d, Ys) if residual is not None else 0
     if Y is None:
-        Y, ldy = Ys.new_empty((T, d)), d
+        Y, ldy = _new(Ys, (T, d), None, stream), d
     else:
         ldy = _like(Y, "Y", T, d, Ys)
     _check(load().dass_expert_combine(Ys.data_ptr(), rows, d, ldys, _code(Ys), slot.data_ptr(), T, k, _ptr(weight),
@@ -696,11 +713,11 @@ def expert_combine_backward(dY: torch.Tensor, Ys: torch.Tensor, slot: torch.Tens
     if dYs is not None:
         lddys = _like(dYs, "dYs", rows, d, dY)
     elif want_rows:
-        dYs = dY.new_empty((rows, d))
+        dYs = _new(dY, (rows, d), None, stream)
     if dweight is not None:
         _same(dweight, "dweight", (T, k), torch.float32, dY.device)
     elif want_weight:
-        dweight = dY.new_empty((T, k), dtype=torch.float32)
+        dweight = _new(dY, (T, k), torch.float32, stream)
     dt = _code(dY)
     if T:
         _check(load().dass_expert_combine_backward(dY.data_ptr(), T, d, lddy, Ys.data_ptr(), rows, ldys, dt, slot.data_ptr(), k,
@@ -739,7 +756,7 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     ldr = _like(residual, "residual", T, N, X) if residual is not None else 0
     dt = _code(X)
     if Y is None:
-        Y, ldy = X.new_empty((T, N)), N
+        Y, ldy = _new(X, (T, N), None, stream), N
     else:
         ldy = _like(Y, "Y", T, N, X)
     if T:

@@ -1,0 +1,111 @@
+"""The memory that a call with `stream=` allocates belongs to that stream: what the caller's current stream allocates next never
+shares it, and it is not reused there while the current stream may still read it.  The library calls are recorded and not
+made, so that nothing runs on memory in doubt."""
+import pytest
+import torch
+
+from paper_2405_01943_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+class Recorder:
+    """The library with its launching calls replaced by notes of the addresses they got."""
+
+    def __init__(self, lib):
+        self.lib, self.addresses = lib, set()
+
+    def __getattr__(self, name):
+        if name.endswith("_bytes") or name in ("dass_status_string",):
+            return getattr(self.lib, name)
+
+        def call(*args):
+            self.addresses |= {a for a in args if isinstance(a, int) and a > 1 << 32}
+            return b.OK
+        return call
+
+
+def _z(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype, device=DEV)
+
+
+T, K, E, D, N = 5000, 2, 8, 64, 96
+CALLS = {
+    "route_topk": lambda z, s: b.route_topk(z["logits"], K, stream=s),
+    "route_topk_backward": lambda z, s: b.route_topk_backward(z["logits"], z["ids"], z["w"], stream=s),
+    "expert_sort": lambda z, s: b.expert_sort(z["ids"], E, stream=s),
+    "expert_gather": lambda z, s: b.expert_gather(z["X"], z["ids"], stream=s),
+    "expert_combine": lambda z, s: b.expert_combine(z["Ys"], z["ids"], stream=s),
+    "expert_combine_backward": lambda z, s: b.expert_combine_backward(z["X"], z["Ys"], z["ids"], stream=s),
+    "linear": lambda z, s: b.linear(z["X"], z["W"], stream=s),
+}
+
+
+@pytest.fixture(scope="module")
+def inputs():
+    z = {"logits": _z(T, E), "ids": _z(T, K, dtype=torch.int32), "w": _z(T, K), "X": _z(T, D), "Ys": _z(T * K, D), "W": _z(N, D)}
+    torch.cuda.synchronize()
+    return z
+
+
+def _spans(tensors):
+    return [(t.untyped_storage().data_ptr(), t.untyped_storage().nbytes()) for t in tensors if t is not None]
+
+
+def _tensors(out):
+    return [] if out is None else [out] if isinstance(out, torch.Tensor) else [t for t in out if t is not None]
+
+
+def _allocated_now(sizes):
+    """Allocations of these sizes on the current stream, several of each, as (address, bytes); all held until the end."""
+    kept = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(8)]
+    return kept, [(t.data_ptr(), t.numel()) for t in kept]
+
+
+def _check(monkeypatch, inputs, call, s):
+    own = {t.untyped_storage().data_ptr() for t in inputs.values()}
+    rec = Recorder(b.load())
+    monkeypatch.setattr(b, "load", lambda: rec)
+    outs = _tensors(call(inputs, s))
+    monkeypatch.undo()
+    made = {a for a in rec.addresses if a not in own}
+    assert made, "the call allocated nothing"
+    sizes = sorted({n for _, n in _spans(outs)} | {1 << 10, 1 << 12, 1 << 14})
+    # the workspace is released already: nothing that the current stream allocates may lie on it
+    kept, now = _allocated_now(sizes)
+    for a in made:
+        assert not any(lo <= a < lo + n for lo, n in now), "memory of a call on another stream was handed to the current stream"
+    # outputs that the current stream still uses are not handed to the call's stream again
+    spans = _spans(outs)
+    if not spans:
+        return
+    torch.cuda._sleep(100_000_000)                                     # tens of milliseconds of work on the current stream
+    del outs
+    with torch.cuda.stream(s):
+        again = [torch.empty(n, dtype=torch.uint8, device=DEV) for _, n in spans]
+    for t in again:
+        assert not any(lo <= t.data_ptr() < lo + n for lo, n in spans), "memory that the current stream may still read was reused"
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_memory_of_a_call_on_another_stream(monkeypatch, inputs, name):
+    _check(monkeypatch, inputs, CALLS[name], torch.cuda.Stream())
+
+
+def test_the_order_on_a_busy_stream_is_right(inputs):
+    """The case in earnest: the call waits behind other work of its stream while the current stream allocates and writes."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    ids = torch.randint(0, 64, (20000, 4), generator=g, device=DEV, dtype=torch.int32)
+    want = b.expert_sort(ids, 64)
+    s = torch.cuda.Stream()
+    need = b.expert_sort_workspace_bytes(20000, 4, 64)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(50_000_000)
+    got = b.expert_sort(ids, 64, stream=s)
+    junk = [torch.full((need,), 0x7f, dtype=torch.uint8, device=DEV) for _ in range(200)]
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and len(junk) == 200
