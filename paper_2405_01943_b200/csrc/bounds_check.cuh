@@ -4,8 +4,8 @@
 // the tensor map in hardware).  In the regular build they are the plain intrinsics.  Built with -DDASS_BOUNDS_CHECK
 // (python -m paper_2405_01943_b200.build --bounds-check: the whole library as ONE translation unit, so that the table
 // below exists once), each entry point first registers the address ranges of the buffers it was given, and every
-// access is tested against them: an access outside all ranges, or at an address that is not a multiple of its width
-// (which the hardware answers with a fault), is SKIPPED (a load yields zero) and counted, with the first offender's
+// access is tested against them: an access outside all ranges, or at an address not aligned
+// for its type (which the hardware answers with a fault), is SKIPPED (a load yields zero) and counted, with the first offender's
 // address, width and source line kept for dass_bounds_report.  Nothing traps and nothing faults.
 // Internal header.
 #pragma once
@@ -31,19 +31,19 @@ struct BoundsReport {
 static __device__ BoundsTable g_bounds;
 static __device__ BoundsReport g_bounds_report;
 
-// Whether an access of nbytes (a power of two) at address a is aligned and lies in one of the ranges.
-__host__ __device__ __forceinline__ bool access_allowed(const BoundsTable &t, unsigned long long a, unsigned nbytes)
+// Whether an access of nbytes at address a is a multiple of `align` (a power of two) and lies in one of the ranges.
+__host__ __device__ __forceinline__ bool access_allowed(const BoundsTable &t, unsigned long long a, unsigned nbytes, unsigned align)
 {
-    if (a & (nbytes - 1)) return false;
+    if (a & (align - 1)) return false;
     for (int i = 0; i < t.n; ++i)
         if (a >= t.lo[i] && a + nbytes <= t.hi[i]) return true;
     return false;
 }
 
-__device__ __forceinline__ bool access_ok(const void *p, unsigned nbytes, unsigned line)
+__device__ __forceinline__ bool access_ok(const void *p, unsigned nbytes, unsigned align, unsigned line)
 {
     const unsigned long long a = (unsigned long long)p;
-    if (access_allowed(g_bounds, a, nbytes)) return true;
+    if (access_allowed(g_bounds, a, nbytes, align)) return true;
     if (atomicAdd(&g_bounds_report.violations, 1u) == 0u) {
         g_bounds_report.first_addr = a;
         g_bounds_report.first_bytes = nbytes;
@@ -100,13 +100,13 @@ template <> __device__ __forceinline__ float4 zero_of<float4>() { return make_fl
     template <typename T> __device__ __forceinline__ T name##_at(const T *p, unsigned line)    \
     {                                                                                           \
         (void)line;                                                                             \
-        return DASS_ACCESS_OK_LINE(p, sizeof(T), line) ? (expr) : zero_of<T>();                 \
+        return DASS_ACCESS_OK_LINE(T, p, line) ? (expr) : zero_of<T>();                 \
     }
 
 #ifdef DASS_BOUNDS_CHECK
-#define DASS_ACCESS_OK_LINE(p, n, line) dass::access_ok((p), (unsigned)(n), (line))
+#define DASS_ACCESS_OK_LINE(T, p, line) dass::access_ok((p), (unsigned)sizeof(T), (unsigned)alignof(T), (line))
 #else
-#define DASS_ACCESS_OK_LINE(p, n, line) true
+#define DASS_ACCESS_OK_LINE(T, p, line) true
 #endif
 
 DASS_DEFINE_LOAD(ld_cs, __ldcs(p))      // streaming load (evict first)
@@ -116,12 +116,12 @@ DASS_DEFINE_LOAD(ld_plain, *p)          // ordinary load
 template <typename T> __device__ __forceinline__ void st_cs_at(T *p, const T &v, unsigned line)
 {
     (void)line;
-    if (DASS_ACCESS_OK_LINE(p, sizeof(T), line)) __stcs(p, v);
+    if (DASS_ACCESS_OK_LINE(T, p, line)) __stcs(p, v);
 }
 template <typename T> __device__ __forceinline__ void st_plain_at(T *p, const T &v, unsigned line)
 {
     (void)line;
-    if (DASS_ACCESS_OK_LINE(p, sizeof(T), line)) *p = v;
+    if (DASS_ACCESS_OK_LINE(T, p, line)) *p = v;
 }
 
 // The forms kernels write: the source line of the access site is recorded with the first violation.

@@ -63,35 +63,39 @@ def _allocated_now(sizes):
     return kept, [(t.data_ptr(), t.numel()) for t in kept]
 
 
-def _check(monkeypatch, inputs, call, s):
+def _recorded(monkeypatch, inputs, call, s):
+    """The outputs of a call on s, and the addresses of all that it allocated."""
     own = {t.untyped_storage().data_ptr() for t in inputs.values()}
     rec = Recorder(b.load())
     monkeypatch.setattr(b, "load", lambda: rec)
     outs = _tensors(call(inputs, s))
     monkeypatch.undo()
-    made = {a for a in rec.addresses if a not in own}
+    return outs, {a for a in rec.addresses if a not in own}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_released_memory_stays_with_the_calls_stream(monkeypatch, inputs, name):
+    outs, made = _recorded(monkeypatch, inputs, CALLS[name], torch.cuda.Stream())
     assert made, "the call allocated nothing"
-    sizes = sorted({n for _, n in _spans(outs)} | {1 << 10, 1 << 12, 1 << 14})
-    # the workspace is released already: nothing that the current stream allocates may lie on it
+    sizes = sorted({n for _, n in _spans(outs)} | {1 << 9, 1 << 12, 1 << 16})
+    outs.clear()                                                       # the workspace is released already
     kept, now = _allocated_now(sizes)
     for a in made:
         assert not any(lo <= a < lo + n for lo, n in now), "memory of a call on another stream was handed to the current stream"
-    # outputs that the current stream still uses are not handed to the call's stream again
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_outputs_outlive_their_use_on_the_current_stream(monkeypatch, inputs, name):
+    s = torch.cuda.Stream()
+    outs, _ = _recorded(monkeypatch, inputs, CALLS[name], s)
     spans = _spans(outs)
-    if not spans:
-        return
     torch.cuda._sleep(100_000_000)                                     # tens of milliseconds of work on the current stream
-    del outs
+    outs.clear()
     with torch.cuda.stream(s):
         again = [torch.empty(n, dtype=torch.uint8, device=DEV) for _, n in spans]
     for t in again:
         assert not any(lo <= t.data_ptr() < lo + n for lo, n in spans), "memory that the current stream may still read was reused"
     torch.cuda.synchronize()
-
-
-@pytest.mark.parametrize("name", CALLS)
-def test_memory_of_a_call_on_another_stream(monkeypatch, inputs, name):
-    _check(monkeypatch, inputs, CALLS[name], torch.cuda.Stream())
 
 
 def test_the_order_on_a_busy_stream_is_right(inputs):
