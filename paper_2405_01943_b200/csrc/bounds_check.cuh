@@ -51,7 +51,7 @@ __device__ __forceinline__ bool access_ok(const void *p, unsigned nbytes, unsign
     }
     return false;
 }
-#define DASS_ACCESS_OK(p, n) dass::access_ok((p), (unsigned)(n), (unsigned)__LINE__)
+#define DASS_ACCESS_OK(p, n) dass::access_ok((p), (unsigned)(n), (unsigned)(n), (unsigned)__LINE__)   // n: a power of two
 
 // Host side: the ranges of one entry-point call, uploaded on the call's stream before its kernels.
 inline size_t &bounds_shrink_next()
