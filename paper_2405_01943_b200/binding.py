@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Callable, Optional, Tuple
 
 import torch
 
@@ -193,21 +193,26 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _new(t: torch.Tensor, shape, dtype: Optional[torch.dtype], stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """An uninitialised tensor on t's device for a call on `stream`.
+def _made(stream: Optional[torch.cuda.Stream], device: torch.device, make: Callable[[], torch.Tensor]) -> torch.Tensor:
+    """make()'s tensor for a call on `stream`.
 
     Memory from the allocator belongs to the stream that was current: it may still be in use by that stream's earlier work,
     and once released it is handed to that stream's later work, whatever another stream does with it.  So the tensor comes
-    from the pool of the stream that the call runs on, and is also kept until what the caller's current stream has queued
-    by its release is done."""
+    from the pool of the stream that the call runs on (where it is filled, if it is), and is also kept until what the
+    caller's current stream has queued by its release is done."""
     if stream is None:
-        return t.new_empty(shape, dtype=dtype)
-    here = torch.cuda.current_stream(t.device)
+        return make()
+    here = torch.cuda.current_stream(device)
     with torch.cuda.stream(stream):
-        out = t.new_empty(shape, dtype=dtype)
+        out = make()
     if here != stream:
         out.record_stream(here)
     return out
+
+
+def _new(t: torch.Tensor, shape, dtype: Optional[torch.dtype], stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """An uninitialised tensor on t's device for a call on `stream`."""
+    return t.new_empty(shape, dtype=dtype) if stream is None else _made(stream, t.device, lambda: t.new_empty(shape, dtype=dtype))
 
 
 # ----------------------------------------------------------------------------- stage (a)
@@ -283,7 +288,7 @@ def norm_finalize(sumsq: torch.Tensor, norm: Optional[torch.Tensor] = None,
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """norm = float32(sqrt(sumsq))."""
     if norm is None:
-        norm = torch.empty(sumsq.numel(), dtype=torch.float32, device=sumsq.device)
+        norm = _new(sumsq, sumsq.numel(), torch.float32, stream)
     code = load().dass_norm_finalize(sumsq.data_ptr(), sumsq.numel(), norm.data_ptr(), _stream(stream))
     _check(code, "dass_norm_finalize")
     return norm
@@ -306,9 +311,9 @@ def score_nm(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alpha: float, 
     if norm.numel() != (rows if norm_axis == AXIS_ROWS else cols):
         raise ValueError("norm has the wrong length for norm_axis")
     if mask_bits is None and want_mask:
-        mask_bits = torch.empty((rows, mask_words_per_row(cols)), dtype=torch.int32, device=W.device)
+        mask_bits = _new(W, (rows, mask_words_per_row(cols)), torch.int32, stream)
     if W_pruned is None and want_pruned:
-        W_pruned = torch.empty_strided((rows, cols), (ld, 1), dtype=W.dtype, device=W.device)
+        W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if W_pruned is not None:
         prow, pcol, pld = _matrix(W_pruned, "W_pruned")
         if (prow, pcol, pld) != (rows, cols, ld) or W_pruned.dtype != W.dtype:
@@ -336,9 +341,9 @@ def compress_nm(W: torch.Tensor, mask_bits: torch.Tensor, n_keep: int, m: int, g
     rows, cols, ld = _matrix(W, "W")
     vshape, mshape = compress_shapes(rows, cols, n_keep, m, group_axis)
     if values is None:
-        values = torch.empty(vshape, dtype=W.dtype, device=W.device)
+        values = _new(W, vshape, None, stream)
     if meta is None:
-        meta = torch.empty(mshape, dtype=torch.int32, device=W.device)
+        meta = _new(W, mshape, torch.int32, stream)
     if tuple(values.shape) != vshape or not values.is_contiguous() or values.dtype != W.dtype:
         raise ValueError(f"values must be a contiguous {vshape} tensor of W's dtype")
     if tuple(meta.shape) != mshape or not meta.is_contiguous() or meta.dtype != torch.int32:
@@ -366,9 +371,9 @@ def prune_nm(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alpha: float, 
     if norm.numel() != (rows if norm_axis == AXIS_ROWS else cols):
         raise ValueError("norm has the wrong length for norm_axis")
     if mask_bits is None and want_mask:
-        mask_bits = torch.empty((rows, mask_words_per_row(cols)), dtype=torch.int32, device=W.device)
+        mask_bits = _new(W, (rows, mask_words_per_row(cols)), torch.int32, stream)
     if W_pruned is None and want_pruned:
-        W_pruned = torch.empty_strided((rows, cols), (ld, 1), dtype=W.dtype, device=W.device)
+        W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if W_pruned is not None:
         prow, pcol, pld = _matrix(W_pruned, "W_pruned")
         if (prow, pcol, pld) != (rows, cols, ld) or W_pruned.dtype != W.dtype:
@@ -379,9 +384,9 @@ def prune_nm(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alpha: float, 
     if want_compressed or values is not None or meta is not None:
         vshape, mshape = compress_shapes(rows, cols, n_keep, m, group_axis)
         if values is None:
-            values = torch.empty(vshape, dtype=W.dtype, device=W.device)
+            values = _new(W, vshape, None, stream)
         if meta is None:
-            meta = torch.empty(mshape, dtype=torch.int32, device=W.device)
+            meta = _new(W, mshape, torch.int32, stream)
         if tuple(values.shape) != vshape or not values.is_contiguous() or values.dtype != W.dtype:
             raise ValueError(f"values must be a contiguous {vshape} tensor of W's dtype")
         if tuple(meta.shape) != mshape or not meta.is_contiguous() or meta.dtype != torch.int32:
@@ -434,11 +439,11 @@ def select_unstructured(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alp
     if norm.numel() != (rows if norm_axis == AXIS_ROWS else cols):
         raise ValueError("norm has the wrong length for norm_axis")
     if mask_bits is None and want_mask:
-        mask_bits = torch.empty((rows, mask_words_per_row(cols)), dtype=torch.int32, device=W.device)
+        mask_bits = _new(W, (rows, mask_words_per_row(cols)), torch.int32, stream)
     if W_pruned is None and want_pruned:
-        W_pruned = torch.empty_strided((rows, cols), (ld, 1), dtype=W.dtype, device=W.device)
+        W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if workspace is None:
-        workspace = select_workspace(rows, cols, norm_axis, W.device)
+        workspace = _made(stream, W.device, lambda: select_workspace(rows, cols, norm_axis, W.device))
     code = load().dass_select_unstructured(W.data_ptr(), rows, cols, ld, _dtype_code(W), norm.data_ptr(), int(norm_axis),
                                            float(alpha), float(sparsity), int(compare_axis), _ptr(mask_bits),
                                            _ptr(W_pruned), workspace.data_ptr(), workspace.numel(), _stream(stream))
@@ -459,13 +464,13 @@ def feature_sumsq(X: torch.Tensor, sumsq: Optional[torch.Tensor] = None, workspa
     """sumsq[j] += sum_t X[t,j]^2 (Eq. 1's squared input-feature norms). Returns sumsq (float64 [d])."""
     T, d, ldx = _matrix(X, "X")
     if sumsq is None:
-        sumsq = torch.zeros(d, dtype=torch.float64, device=X.device)
+        sumsq = _made(stream, X.device, lambda: X.new_zeros(d, dtype=torch.float64))
     if sumsq.dtype != torch.float64 or not sumsq.is_cuda or sumsq.numel() != d or not sumsq.is_contiguous():
         raise ValueError("sumsq must be a contiguous CUDA float64 tensor of d elements")
     need = ctypes.c_size_t(0)
     _check(load().dass_feature_workspace_bytes(T, d, ctypes.byref(need)), "dass_feature_workspace_bytes")
     if workspace is None:
-        workspace = torch.empty(need.value + 16, dtype=torch.uint8, device=X.device)
+        workspace = _new(X, need.value + 16, torch.uint8, stream)
         off = (-workspace.data_ptr()) % 16
         workspace = workspace[off:off + need.value]
     code = load().dass_feature_sumsq(X.data_ptr(), T, d, ldx, _dtype_code(X), sumsq.data_ptr(), workspace.data_ptr(),
@@ -508,12 +513,13 @@ def mlp_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.T
     if not (Wg.dtype == Wu.dtype == Wd.dtype == X.dtype):
         raise ValueError("X, Wg, Wu, Wd must have one dtype")
     if Z is None:
-        Z = torch.empty((T, d), dtype=X.dtype, device=X.device)
+        Z = _new(X, (T, d), None, stream)
     Tz, dz, ldz = _matrix(Z, "Z")
     if (Tz, dz) != (T, d) or Z.dtype != X.dtype:
         raise ValueError("Z must be [T x d] in X's dtype")
     if workspace is None:
-        workspace = mlp_forward_workspace(mlp_forward_workspace_bytes(T, d, I, X.dtype)[1], X.device)
+        nbytes = mlp_forward_workspace_bytes(T, d, I, X.dtype)[1]
+        workspace = _made(stream, X.device, lambda: mlp_forward_workspace(nbytes, X.device))
     if not workspace.is_cuda or workspace.dtype != torch.uint8:
         raise ValueError("workspace must be a CUDA uint8 tensor (see mlp_forward_workspace)")
     code = load().dass_mlp_forward(X.data_ptr(), T, ldx, Wg.data_ptr(), Wu.data_ptr(), I, d, ldw,

@@ -39,12 +39,20 @@ CALLS = {
     "expert_combine": lambda z, s: b.expert_combine(z["Ys"], z["ids"], stream=s),
     "expert_combine_backward": lambda z, s: b.expert_combine_backward(z["X"], z["Ys"], z["ids"], stream=s),
     "linear": lambda z, s: b.linear(z["X"], z["W"], stream=s),
+    "norm_finalize": lambda z, s: b.norm_finalize(z["sumsq"], stream=s),
+    "score_nm": lambda z, s: b.score_nm(z["W"], z["norm"], b.AXIS_ROWS, 0.5, 2, 4, b.AXIS_ROWS, stream=s),
+    "compress_nm": lambda z, s: b.compress_nm(z["W"], z["mask"], 2, 4, b.AXIS_ROWS, stream=s),
+    "prune_nm": lambda z, s: b.prune_nm(z["W"], z["norm"], b.AXIS_ROWS, 0.5, 2, 4, b.AXIS_ROWS, stream=s),
+    "select_unstructured": lambda z, s: b.select_unstructured(z["W"], z["norm"], b.AXIS_ROWS, 0.5, 0.5, b.AXIS_ROWS, stream=s),
+    "feature_sumsq": lambda z, s: b.feature_sumsq(z["X"], stream=s),
+    "mlp_forward": lambda z, s: b.mlp_forward(z["X"], z["W"], z["W"], z["Wd"], b.ACT_SILU, stream=s),
 }
 
 
 @pytest.fixture(scope="module")
 def inputs():
-    z = {"logits": _z(T, E), "ids": _z(T, K, dtype=torch.int32), "w": _z(T, K), "X": _z(T, D), "Ys": _z(T * K, D), "W": _z(N, D)}
+    z = {"logits": _z(T, E), "ids": _z(T, K, dtype=torch.int32), "w": _z(T, K), "X": _z(T, D), "Ys": _z(T * K, D), "W": _z(N, D), "Wd": _z(D, N),
+         "norm": _z(N), "sumsq": _z(N, dtype=torch.float64), "mask": _z(N, b.mask_words_per_row(D), dtype=torch.int32)}
     torch.cuda.synchronize()
     return z
 
@@ -113,3 +121,14 @@ def test_the_order_on_a_busy_stream_is_right(inputs):
     junk = [torch.full((need,), 0x7f, dtype=torch.uint8, device=DEV) for _ in range(200)]
     s.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(got, want)) and len(junk) == 200
+
+
+def test_sums_start_from_zero_on_the_calls_stream(monkeypatch, inputs):
+    """feature_sumsq fills its sums itself: on the stream of the call, not on one that the call does not wait for."""
+    s, where, ones = torch.cuda.Stream(), [], inputs["X"] + 1.0
+    torch.cuda.synchronize()
+    zeros = torch.Tensor.new_zeros
+    monkeypatch.setattr(torch.Tensor, "new_zeros", lambda *a, **k: where.append(torch.cuda.current_stream()) or zeros(*a, **k))
+    got = b.feature_sumsq(ones, stream=s)
+    torch.cuda.synchronize()
+    assert where == [s] and bool((got == T).all())
