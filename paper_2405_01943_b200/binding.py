@@ -659,6 +659,8 @@ def _rows_used(offsets: Optional[torch.Tensor], device: torch.device) -> Optiona
     if offsets is None:
         return None
     n = offsets.numel()
+    if n == 0:
+        raise ValueError("offsets must be the [E + 1] tensor expert_sort returned")
     return _same(offsets, "offsets", (n,), torch.int32, device) + 4 * (n - 1)
 
 
