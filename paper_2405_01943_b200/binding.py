@@ -215,6 +215,12 @@ def _new(t: torch.Tensor, shape, dtype: Optional[torch.dtype], stream: Optional[
     return t.new_empty(shape, dtype=dtype) if stream is None else _made(stream, t.device, lambda: t.new_empty(shape, dtype=dtype))
 
 
+def _workspace(t: torch.Tensor, device: torch.device) -> None:
+    """Checks a caller's workspace: kernels write to its address."""
+    if not t.is_cuda or t.dtype != torch.uint8 or t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+
+
 # ----------------------------------------------------------------------------- stage (a)
 
 def calib_workspace_bytes(T: int, d: int, I: int, dtype: torch.dtype) -> int:
@@ -444,6 +450,8 @@ def select_unstructured(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alp
         W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if workspace is None:
         workspace = _made(stream, W.device, lambda: select_workspace(rows, cols, norm_axis, W.device))
+    else:
+        _workspace(workspace, W.device)
     code = load().dass_select_unstructured(W.data_ptr(), rows, cols, ld, _dtype_code(W), norm.data_ptr(), int(norm_axis),
                                            float(alpha), float(sparsity), int(compare_axis), _ptr(mask_bits),
                                            _ptr(W_pruned), workspace.data_ptr(), workspace.numel(), _stream(stream))
@@ -473,6 +481,8 @@ def feature_sumsq(X: torch.Tensor, sumsq: Optional[torch.Tensor] = None, workspa
         workspace = _new(X, need.value + 16, torch.uint8, stream)
         off = (-workspace.data_ptr()) % 16
         workspace = workspace[off:off + need.value]
+    else:
+        _workspace(workspace, X.device)
     code = load().dass_feature_sumsq(X.data_ptr(), T, d, ldx, _dtype_code(X), sumsq.data_ptr(), workspace.data_ptr(),
                                      workspace.numel(), _stream(stream))
     _check(code, "dass_feature_sumsq")
@@ -639,6 +649,8 @@ def expert_sort(expert: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = 
     if workspace is None:
         need = expert_sort_workspace_bytes(T, k, E)
         workspace = _new(expert, need, torch.uint8, stream) if need else None
+    else:
+        _workspace(workspace, dev)
     _check(load().dass_expert_sort(ids, T, k, E, offsets.data_ptr(), slot.data_ptr(), source.data_ptr(),
                                    _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream_of(expert, stream)),
            "dass_expert_sort")

@@ -16,3 +16,44 @@ def test_rows_used_is_the_last_of_the_offsets():
     for bad in (offsets[:0], offsets.long(), offsets[::2], offsets.view(1, 5)):
         with pytest.raises(ValueError):
             b._rows_used(bad, CPU)
+
+
+class OnDevice(torch.Tensor):
+    """A tensor that passes for a CUDA tensor; the library below notes calls and makes none."""
+    is_cuda = True
+
+
+class Library:
+    def __init__(self, lib):
+        self.lib, self.calls = lib, []
+
+    def __getattr__(self, name):
+        if name.endswith("_bytes"):
+            return getattr(self.lib, name)
+        return lambda *args: self.calls.append(name) or b.OK
+
+
+def _on_device(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnDevice)
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Library(b.load())
+    monkeypatch.setattr(b, "load", lambda: lib)
+    monkeypatch.setattr(b, "_stream_of", lambda t, stream: 0)
+    monkeypatch.setattr(b, "_stream", lambda stream: 0)
+    return lib
+
+
+def test_a_workspace_has_to_be_device_memory(library):
+    calls = [lambda w: b.expert_sort(_on_device(5000, 2, dtype=torch.int32), 8, workspace=w), lambda w: b.feature_sumsq(_on_device(64, 32), workspace=w),
+             lambda w: b.select_unstructured(_on_device(64, 32), _on_device(64), b.AXIS_ROWS, 0.5, 0.5, b.AXIS_ROWS, workspace=w)]
+    for call in calls:
+        library.calls.clear()
+        call(_on_device(1 << 20, dtype=torch.uint8))
+        assert len(library.calls) == 1
+        for bad in (torch.zeros(1 << 20, dtype=torch.uint8), _on_device(1 << 20), _on_device(1 << 20, dtype=torch.uint8)[::2]):
+            with pytest.raises(ValueError):
+                call(bad)
+        assert len(library.calls) == 1
