@@ -170,9 +170,21 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}: the library takes bfloat16 or float32")
 
 
+def _here(t: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
+    """The index of the tensor's device, which has to be the current one: that is where the library launches, and whose
+    streams and records it uses."""
+    device, current = t.get_device(), torch._C._cuda_getDevice()
+    if device != current:
+        raise ValueError(f"a tensor on cuda:{device} while cuda:{current} is current: make the tensor's device current (torch.cuda.device)")
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"a stream of cuda:{stream.device_index} for tensors on cuda:{device}")
+    return device
+
+
 def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
+    _here(t)
     if t.dim() != 2 or t.stride(1) != 1:
         raise ValueError(f"{name} must be a 2-D row-major tensor (unit stride along columns)")
     return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
@@ -186,7 +198,8 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
 def _stream_of(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
     """The given stream, or the current one of the tensor's device (by its raw handle: building a Stream object costs as
     much as the launch of a small kernel)."""
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
+    device = _here(t, stream)
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -293,6 +306,7 @@ def calib_status(workspace: torch.Tensor, stream: Optional[torch.cuda.Stream] = 
 def norm_finalize(sumsq: torch.Tensor, norm: Optional[torch.Tensor] = None,
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """norm = float32(sqrt(sumsq))."""
+    _here(sumsq, stream)
     if norm is None:
         norm = _new(sumsq, sumsq.numel(), torch.float32, stream)
     code = load().dass_norm_finalize(sumsq.data_ptr(), sumsq.numel(), norm.data_ptr(), _stream(stream))
@@ -786,5 +800,6 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
 
 
 def linear_status(stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Waits for the stream and raises if a bounded wait inside a linear kernel ran out since the last query."""
+    """Waits for the stream and raises if a bounded wait inside a linear kernel ran out on the current device since the last
+    query."""
     _check(load().dass_linear_status(_stream(stream)), "dass_linear_status")

@@ -22,6 +22,9 @@ class OnDevice(torch.Tensor):
     """A tensor that passes for a CUDA tensor; the library below notes calls and makes none."""
     is_cuda = True
 
+    def get_device(self):
+        return 0
+
 
 class Library:
     def __init__(self, lib):
@@ -41,7 +44,8 @@ def _on_device(*shape, dtype=torch.float32):
 def library(monkeypatch):
     lib = Library(b.load())
     monkeypatch.setattr(b, "load", lambda: lib)
-    monkeypatch.setattr(b, "_stream_of", lambda t, stream: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
     monkeypatch.setattr(b, "_stream", lambda stream: 0)
     return lib
 
@@ -57,3 +61,36 @@ def test_a_workspace_has_to_be_device_memory(library):
             with pytest.raises(ValueError):
                 call(bad)
         assert len(library.calls) == 1
+
+
+class Stream:
+    cuda_stream, device_index = 1 << 20, 1
+
+
+def test_tensors_of_another_device_than_the_current_one(library, monkeypatch):
+    """The library launches on the current device: a call with another device's tensors, or another device's stream, is refused."""
+    ids, X, Ys, W = _on_device(4, 2, dtype=torch.int32), _on_device(4, 8), _on_device(8, 8), _on_device(8, 8)
+    out = {n: _on_device(*shape, dtype=t) for n, shape, t in (("k", (4, 2), torch.float32), ("off", (9,), torch.int32), ("slot", (4, 2), torch.int32),
+                                                              ("src", (8,), torch.int32), ("X", (4, 8), torch.float32), ("Ys", (8, 8), torch.float32))}
+    calls = [lambda s: b.route_topk(X, 2, expert=ids, weight=out["k"], stream=s), lambda s: b.route_topk_backward(X, ids, out["k"], dlogits=out["X"], stream=s),
+             lambda s: b.expert_sort(ids, 8, offsets=out["off"], slot=out["slot"], source=out["src"], stream=s),
+             lambda s: b.expert_gather(X, ids, Xs=out["Ys"], stream=s), lambda s: b.expert_combine(Ys, ids, Y=out["X"], stream=s),
+             lambda s: b.expert_combine_backward(X, Ys, ids, dYs=out["Ys"], dweight=out["k"], stream=s), lambda s: b.linear(X, W, Y=out["X"], stream=s)]
+    older = [lambda: b.feature_sumsq(X), lambda: b.norm_finalize(_on_device(8, dtype=torch.float64)),
+             lambda: b.score_nm(W, _on_device(8), b.AXIS_ROWS, 0.5, 2, 4, b.AXIS_ROWS)]
+    for call in calls:
+        call(None)
+        with pytest.raises(ValueError):
+            call(Stream())
+    for call in older:
+        call()
+    made = len(library.calls)
+    assert made == len(calls) + len(older)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(None)
+    for call in older:
+        with pytest.raises(ValueError):
+            call()
+    assert len(library.calls) == made
