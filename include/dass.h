@@ -317,7 +317,7 @@ dass_status dass_expert_combine(const void *Ys, int64_t rows, int64_t d, int64_t
                                 int64_t k, const float *weight, const void *residual, int64_t ldr, void *Y, int64_t ldy, void *cuda_stream);
 /* Gradients of the weighted sum: dYs[slot[t,j],:] = weight[t,j] * dY[t,:] (weight null: 1) and, in f32,
  * dweight[t,j] = sum_c dY[t,c] * Ys[slot[t,j],c] (0 for a skipped slot); each nullable, at least one required.
- * rows_used as for dass_expert_gather (applies to dYs; with T = 0 nothing is written).  The residual's gradient is dY. */
+ * rows_used as for dass_expert_gather (applies to dYs, with T = 0 as well).  The residual's gradient is dY. */
 dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, int64_t lddy, const void *Ys, int64_t rows, int64_t ldys,
                                          dass_dtype dt, const int32_t *slot, int64_t k, const float *weight, const int32_t *rows_used,
                                          void *dYs, int64_t lddys, float *dweight, void *cuda_stream);

@@ -753,7 +753,7 @@ def expert_combine_backward(dY: torch.Tensor, Ys: torch.Tensor, slot: torch.Tens
     elif want_weight:
         dweight = _new(dY, (T, k), torch.float32, stream)
     dt = _code(dY)
-    if T:
+    if T or (dYs is not None and offsets is not None):
         _check(load().dass_expert_combine_backward(dY.data_ptr(), T, d, lddy, Ys.data_ptr(), rows, ldys, dt, slot.data_ptr(), k,
                                                    _ptr(weight), _rows_used(offsets, dY.device), _ptr(dYs), lddys, _ptr(dweight),
                                                    _stream_of(dY, stream)), "dass_expert_combine_backward")

@@ -564,7 +564,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     if (!elem_aligned(dY, bf16) || !elem_aligned(Ys, bf16) || !elem_aligned(dYs, bf16) || !elem_aligned(slot, false) ||
         !elem_aligned(weight, false) || !elem_aligned(dweight, false) || !elem_aligned(rows_used, false))
         return DASS_ERR_ALIGN;
-    if (T == 0) return DASS_OK;
+    if (T == 0 && !(dYs && rows_used && rows > 0)) return DASS_OK;    // without tokens dYs still has rows to be zeroed
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const size_t elt = bf16 ? 2 : 4;
     const int vec = bf16 ? 8 : 4;
@@ -572,7 +572,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
                         d % vec == 0;
     const ErRows r{T, rows, (int)k, (int)(k <= 2 ? k : (k + (k + 3) / 4 - 1) / ((k + 3) / 4)), (int)(vector ? d / vec : d)};
     DASS_BOUNDS_SCOPE(bs);
-    DASS_BOUNDS_ADD(bs, dY, ((size_t)(T - 1) * lddy + d) * elt);
+    if (T > 0) DASS_BOUNDS_ADD(bs, dY, ((size_t)(T - 1) * lddy + d) * elt);
     if (rows > 0) DASS_BOUNDS_ADD(bs, Ys, ((size_t)(rows - 1) * ldys + d) * elt);
     if (rows > 0) DASS_BOUNDS_ADD(bs, dYs, ((size_t)(rows - 1) * lddys + d) * elt);
     DASS_BOUNDS_ADD(bs, slot, (size_t)T * k * 4);
@@ -582,7 +582,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
     // few threads a token keep its sums inside a warp; a whole block where there are few tokens
-    ErGrid g = er_grid(T, r, er_sum_cols(vector, k), T >= 148 * 32 ? 64 : ER_THREADS);
+    ErGrid g = er_grid(T > 0 ? T : rows, r, er_sum_cols(vector, k), T >= 148 * 32 ? 64 : ER_THREADS);
     g.grid.y = 1;                                                     // a token's threads walk its whole row
     const dim3 grid = g.grid, block = g.block;
     auto launch = [&](auto kernel) { kernel<<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r); };
