@@ -344,7 +344,7 @@ extern "C" {
 dass_status dass_route_topk(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, int k, dass_route_norm norm,
                             int32_t *expert, float *weight, void *cuda_stream)
 {
-    if (!logits || !expert || !weight) return DASS_ERR_NULL;
+    if (T > 0 && (!logits || !expert || !weight)) return DASS_ERR_NULL;
     const dass_status cs = rt_check(T, E, ld, (int)dt, k, (int)norm);
     if (cs != DASS_OK) return cs;
     const bool bf16 = dt == DASS_BF16;
@@ -366,7 +366,7 @@ dass_status dass_route_topk(const void *logits, int64_t T, int64_t E, int64_t ld
 dass_status dass_route_topk_backward(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, int k, dass_route_norm norm,
                                      const int32_t *expert, const float *dweight, void *dlogits, int64_t ldd, void *cuda_stream)
 {
-    if (!logits || !expert || !dweight || !dlogits) return DASS_ERR_NULL;
+    if (T > 0 && (!logits || !expert || !dweight || !dlogits)) return DASS_ERR_NULL;
     const dass_status cs = rt_check(T, E, ld, (int)dt, k, (int)norm);
     if (cs != DASS_OK) return cs;
     if (ldd < E) return DASS_ERR_SHAPE;

@@ -94,3 +94,14 @@ def test_tensors_of_another_device_than_the_current_one(library, monkeypatch):
         with pytest.raises(ValueError):
             call()
     assert len(library.calls) == made
+
+
+def test_no_tokens_need_no_buffers():
+    """T = 0 is a valid request: an empty tensor has no address."""
+    lib = b.load()
+    assert lib.dass_route_topk(None, 0, 8, 8, b.BF16, 2, b.ROUTE_CHOSEN, None, None, None) == b.OK
+    assert lib.dass_route_topk_backward(None, 0, 8, 8, b.BF16, 2, b.ROUTE_ALL, None, None, None, 8, None) == b.OK
+    assert lib.dass_expert_gather(None, 0, 16, 16, b.BF16, None, 2, None, None, None, 0, 16, None) == b.OK
+    assert lib.dass_expert_combine(None, 0, 16, 16, b.BF16, None, 0, 2, None, None, 0, None, 16, None) == b.OK
+    assert lib.dass_linear(None, 0, 64, 64, 1 << 20, None, 32, 64, 0, None, None, b.ACT_NONE, None, 0, None, 32, b.BF16, None, 1, None) == b.OK
+    assert lib.dass_route_topk(None, 0, 8, 7, b.BF16, 2, b.ROUTE_CHOSEN, None, None, None) == 2     # sizes are still looked at
