@@ -325,7 +325,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
 /* Matrix product with its epilogue, dense or per expert:
  *     Y = act(X W^T + bias) [ * (X W_up^T + bias_up) ] + residual          one rounding to `dt`, at Y
  * X [T x K, ldx], W (and W_up, nullable: the GLU form) [N x K, ldw], bias / bias_up [N] in `dt`, nullable, residual
- * [T x N, ldr], nullable, Y [T x N, ldy].  act: any dass_act.  Y may be the residual itself (same pitch).
+ * [T x N, ldr], nullable, Y [T x N, ldy].  act: any dass_act (a NaN stays one).  Y may be the residual itself (same pitch).
  * offsets (device, groups + 1 values, nullable): rows offsets[g] .. offsets[g+1] - 1 use group g's matrices W + g *
  * group_stride (elements), W_up + g * group_stride and row g of bias / bias_up [groups x N]; rows of no group are
  * written as zeros.  Null: groups = 1, all rows.

@@ -79,13 +79,21 @@ __device__ __forceinline__ LinTile lin_find_tile(const int32_t *offsets, int gro
     return r;
 }
 
+// max(x, 0) that keeps NaN, as the other activations do (fmaxf gives the number where one side is NaN).
+__device__ __forceinline__ float lin_relu(float x)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // The activation in f32, from accurate functions.
 __device__ __forceinline__ float lin_act(float x, int act)
 {
     switch (act) {
     case DASS_ACT_SILU: return x / (1.0f + expf(-x));
     case DASS_ACT_GELU_TANH: return 0.5f * x * (1.0f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
-    case DASS_ACT_RELU: return fmaxf(x, 0.0f);
+    case DASS_ACT_RELU: return lin_relu(x);
     default: return x;
     }
 }

@@ -78,7 +78,7 @@ __device__ __forceinline__ float lt_act(float x)
     if constexpr (ACT == DASS_ACT_SILU) return x * rcp_approx(1.0f + ex2_approx(-LOG2E * x));
     else if constexpr (ACT == DASS_ACT_GELU_TANH)           // 0.5 (1 + tanh z) = sigmoid(2 z), z = sqrt(2 / pi) (x + 0.044715 x^3)
         return x * rcp_approx(1.0f + ex2_approx(-1.5957691216057308f * LOG2E * x * fmaf(0.044715f * x, x, 1.0f)));
-    else if constexpr (ACT == DASS_ACT_RELU) return fmaxf(x, 0.0f);
+    else if constexpr (ACT == DASS_ACT_RELU) return lin_relu(x);
     else return x;
 }
 template <int ACT, int V> __device__ __forceinline__ void lt_act_each(float (&x)[V])

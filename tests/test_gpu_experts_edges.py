@@ -44,3 +44,28 @@ def test_gradient_rows_without_tokens_stay_inside(dtype):
         _no_tokens(dtype, 33, 71)
         rep = b.bounds_report()
     assert rep["violations"] == 0, rep
+
+
+ACTS = {"none": b.ACT_NONE, **b.ACT_BY_NAME}
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("glu", [False, True], ids=["plain", "glu"])
+@pytest.mark.parametrize("T,K,N,dtype", [(4, 64, 72, BF16), (64, 2048, 4096, BF16), (1100, 128, 136, BF16), (4, 64, 72, F32), (70, 64, 72, F32)],
+                         ids=["few", "mid", "many", "f32-few", "f32"])
+def test_nan_stays_nan_through_every_activation(T, K, N, dtype, act, glu):
+    """A NaN among the inputs of an output makes that output NaN, and no other one."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    rand = lambda *s: torch.randn(s, generator=g, device=DEV).to(dtype)                 # noqa: E731
+    X, W, V, bias = rand(T, K), rand(N, K), rand(N, K) if glu else None, rand(N)
+    Y = b.linear(X, W, bias=bias, act=ACTS[act], W_up=V)
+    assert bool(torch.isfinite(Y).all())
+    want = torch.zeros((T, N), dtype=torch.bool, device=DEV)
+    X, bias = X.clone(), bias.clone()
+    X[1, 3], bias[5] = float("nan"), float("nan")
+    want[1], want[:, 5] = True, True
+    Y2 = b.linear(X, W, bias=bias, act=ACTS[act], W_up=V)
+    b.linear_status()
+    assert torch.equal(torch.isnan(Y2), want)
+    assert torch.equal(Y2[~want], Y[~want])
