@@ -332,8 +332,8 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
  * bf16: tensor cores, f32 accumulators; f32: f32 FMAs.  X, W and W_up 16-byte aligned with pitches (and group_stride) of
  * whole 16 bytes, as everywhere in this header; bias, residual and Y need element alignment only.
  * Waits inside the tensor-core kernels are bounded (2 s); dass_linear_status waits for `cuda_stream` and returns
- * DASS_ERR_TIMEOUT if one ran out on the current device since the last query (outputs of that call are then
- * incomplete; the context stays usable), else DASS_OK, and clears the record.
+ * DASS_ERR_TIMEOUT if one ran out on the current device that no query has reported yet (outputs of that call are then
+ * incomplete; the context stays usable), else DASS_OK.  What runs out on another stream meanwhile is left for the next query.
  * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (more than 2^28 rows, K or N beyond 32-bit coordinates, groups > 1024) / CUDA. */
 dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const void *W, const void *W_up, int64_t N, int64_t ldw,
                         int64_t group_stride, const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,

@@ -78,10 +78,12 @@ LinPlan lin_plan(const LinearArgs &a)
     return best;
 }
 
-__device__ int g_linear_status = 0;      // DASS_OK or DASS_ERR_TIMEOUT; read and cleared through dass_linear_status
+// Bounded waits that ran out on this device, counted and never cleared: a query that cleared it could lose what a kernel on
+// another stream records meanwhile.  dass_linear_status remembers how many have been reported.
+__device__ int g_linear_timeouts = 0;
 
-// Address of the record on the current device (looked up once per device).
-int *linear_status_word()
+// Address of the count on the current device (looked up once per device).
+int *linear_timeouts()
 {
     static std::atomic<int *> cached[64];
     int dev = 0;
@@ -89,7 +91,7 @@ int *linear_status_word()
     int *p = dev < 64 ? cached[dev].load(std::memory_order_relaxed) : nullptr;
     if (p) return p;
     void *addr = nullptr;
-    if (cudaGetSymbolAddress(&addr, g_linear_status) != cudaSuccess) return nullptr;
+    if (cudaGetSymbolAddress(&addr, g_linear_timeouts) != cudaSuccess) return nullptr;
     p = static_cast<int *>(addr);
     if (dev < 64) cached[dev].store(p, std::memory_order_relaxed);
     return p;
@@ -145,13 +147,18 @@ dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const 
 
 dass_status dass_linear_status(void *cuda_stream)
 {
+    static std::atomic<int> reported[64];
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    int *word = linear_status_word();
-    int host = 0;
-    if (!word || cudaMemcpyAsync(&host, word, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-        cudaMemsetAsync(word, 0, sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+    int *word = linear_timeouts();
+    int count = 0, dev = 0;
+    if (!word || cudaGetDevice(&dev) != cudaSuccess ||
+        cudaMemcpyAsync(&count, word, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
         return DASS_ERR_CUDA;
-    return host == 0 ? DASS_OK : DASS_ERR_TIMEOUT;
+    if (dev >= 64) return count ? DASS_ERR_TIMEOUT : DASS_OK;          // not remembered past 64 devices: reported every time
+    // the remembered count only grows, whichever of several queries comes first (differences: the count may wrap)
+    int before = reported[dev].load();
+    while (count - before > 0 && !reported[dev].compare_exchange_weak(before, count)) {}
+    return count - before > 0 ? DASS_ERR_TIMEOUT : DASS_OK;
 }
 
 }  // extern "C"

@@ -41,7 +41,7 @@ struct LmParams {
     LinearArgs a;
     int col_tiles, row_tiles, k_blocks, split, stages;
     int vec;                // Y, R and the biases allow 16-byte accesses
-    int *status;
+    int *timeouts;
 };
 
 // 8 values of a bf16 row: columns n .. n + 7 (STEP 1), or n, n + 16 .. n + 112 (STEP 16); columns past N are zero.
@@ -200,7 +200,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             __syncwarp();
             if ((int)++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
-        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, (int)DASS_ERR_TIMEOUT); }
+        if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }
     } else if (warp == 1) {
         constexpr uint32_t idesc = idesc_bf16_f32(LM_COLS, NT);
         uint32_t stage = 0, phase = 0;
@@ -224,7 +224,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             __syncwarp();
             if ((int)++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
-        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, (int)DASS_ERR_TIMEOUT); }
+        if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }
     } else {
         // accumulators to shared memory: lane = column of Y, accumulator column = row of X
         const int quad = warp & 3;
@@ -241,7 +241,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             }
         } else if (lane == 0) {
             *abort_flag = 1;
-            atomicExch(p.status, (int)DASS_ERR_TIMEOUT);
+            atomicAdd(p.timeouts, 1);
         }
     }
     tc_fence_before();
@@ -265,7 +265,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
 
 // ------------------------------------------------------------------ host side
 int device_sm_count();                                                                                       // dass_abi.cu
-int *linear_status_word();                                                                                   // linear.cu
+int *linear_timeouts();                                                                                      // linear.cu
 bool tc_make_map(CUtensorMap *map, const void *ptr, int64_t rows, int64_t cols, int64_t ld, int box_rows);   // calib_tc.cu
 bool tc_make_map_3d(CUtensorMap *map, const void *ptr, int64_t mats, int64_t rows, int64_t cols, int64_t ld, int64_t mat_stride, int box_rows);   // linear_tc.cu
 
@@ -289,8 +289,8 @@ static dass_status lm_launch(const LinearArgs &a, int split)
     p.split = split < p.k_blocks ? split : 1;
     p.stages = blocks * p.split * 10 <= 8 * device_sm_count() ? S::DEEP : S::SHARED;        // clusters do not fill every SM
     p.vec = lin_wide_ok(a);
-    p.status = linear_status_word();
-    if (!p.status) return DASS_ERR_CUDA;
+    p.timeouts = linear_timeouts();
+    if (!p.timeouts) return DASS_ERR_CUDA;
     const int64_t grid = (int64_t)p.col_tiles * p.row_tiles * p.split;
     if (grid > 0x7fffffffll) return DASS_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};

@@ -18,7 +18,7 @@
 // a library product without them 784 to 801), 705 us as a single burst; 16384 rows of 8 experts 4096 -> 14336 gated 3.03
 // ms, 14336 -> 4096 1.60 ms.  With short contractions the epilogue bounds (16384 x 512 -> 2048: 35 us).
 //
-// Every wait is bounded: when one runs out the CTA raises an abort flag, records DASS_ERR_TIMEOUT for
+// Every wait is bounded: when one runs out the CTA raises an abort flag, counts it for
 // dass_linear_status, lets its roles drain and frees its TMEM before it returns.
 #include "linear_common.cuh"
 #include "linear_tc.cuh"
@@ -49,7 +49,7 @@ struct LtParams {
     int64_t ldr, ldy, T;
     int N, groups, col_tiles, k_blocks, cols_per_tile;
     int y_vec, r_vec;               // whole 16-byte accesses
-    int *status;
+    int *timeouts;
 };
 
 struct LtItem { int g; int row, row_end, col; };
@@ -180,7 +180,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
         }
-        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, (int)DASS_ERR_TIMEOUT); }
+        if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (leader CTA only)
         if (rank == 0) {
@@ -210,7 +210,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, (int)DASS_ERR_TIMEOUT); }
+            if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }
         }
     } else {
         // ------------------------------------------------------------ epilogue (this CTA's 128 rows)
@@ -334,7 +334,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                 else mbar_arrive_cluster(leader_acc_empty + 8 * as);
             }
         }
-        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, (int)DASS_ERR_TIMEOUT); }
+        if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }
     }
 
     // ---------------------------------------------------------------- teardown
@@ -376,7 +376,7 @@ static cudaError_t lt_pick(int act, const CUtensorMap &mx, const CUtensorMap &mw
     }
 }
 
-int *linear_status_word();                                                                                   // linear.cu
+int *linear_timeouts();                                                                                      // linear.cu
 bool tc_make_map(CUtensorMap *map, const void *ptr, int64_t rows, int64_t cols, int64_t ld, int box_rows);   // calib_tc.cu
 
 typedef CUresult (*LinEncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -427,8 +427,8 @@ dass_status linear_tc_launch(const LinearArgs &a, int bn)
     p.k_blocks = (int)((a.K + LT_BK - 1) / LT_BK);
     p.y_vec = rows_vec_ok(a.Y, a.ldy, true);
     p.r_vec = a.residual && rows_vec_ok(a.residual, a.ldr, true);
-    p.status = linear_status_word();
-    if (!p.status) return DASS_ERR_CUDA;
+    p.timeouts = linear_timeouts();
+    if (!p.timeouts) return DASS_ERR_CUDA;
     const int64_t items = ((a.T + 2 * LT_BM - 1) / (2 * LT_BM) + (a.offsets ? a.groups : 0)) * p.col_tiles;   // at most
     const int pairs = device_sm_count() / 2;
     const int grid = 2 * (int)(items < pairs ? items : pairs);

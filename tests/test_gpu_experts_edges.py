@@ -1,9 +1,9 @@
 """Mixture-of-experts calls at the edges of their contracts."""
-import numpy as np
+import ctypes
+
 import pytest
 import torch
 
-import expert_reference as ref
 from paper_2405_01943_b200 import binding as b
 from paper_2405_01943_b200 import build
 
@@ -69,3 +69,40 @@ def test_nan_stays_nan_through_every_activation(T, K, N, dtype, act, glu):
     b.linear_status()
     assert torch.equal(torch.isnan(Y2), want)
     assert torch.equal(Y2[~want], Y[~want])
+
+
+class _Word:
+    """An int32 of device memory at an address, as a tensor's memory."""
+
+    def __init__(self, address):
+        self.__cuda_array_interface__ = {"shape": (1,), "typestr": "<i4", "data": (address, False), "version": 2}
+
+
+def test_a_timeout_is_reported_once_and_none_is_lost():
+    """Every bounded wait that runs out is counted on the device; a query reports what no query has reported and leaves the
+    count alone, so that what another stream records beside it is there for the next one."""
+    address = b.load()._ZN4dass15linear_timeoutsEv
+    address.restype, address.argtypes = ctypes.c_void_p, []
+    b.linear_status()
+    count = torch.as_tensor(_Word(address()), device=DEV)
+    start = int(count)
+    for times in (1, 3):
+        count += times
+        with pytest.raises(b.DassError) as e:
+            b.linear_status()
+        assert e.value.code == 8
+        b.linear_status()
+    assert int(count) == start + 4
+    s = torch.cuda.Stream()                                              # recorded on another stream, after this query's answer
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        count += 1
+    b.linear_status(torch.cuda.current_stream())
+    s.synchronize()
+    with pytest.raises(b.DassError):
+        b.linear_status()
+    b.linear_status()
+    X = torch.ones((70, 2048), dtype=BF16, device=DEV)
+    W = torch.ones((4096, 2048), dtype=BF16, device=DEV)
+    assert bool((b.linear(X, W) == 2048).all())
+    b.linear_status()
