@@ -49,6 +49,7 @@ class ExpertLayer:
         self.sumsq = torch.zeros((E, I), dtype=torch.float64, device=Wg.device)
         self.norm = torch.zeros((E, I), dtype=torch.float32, device=Wg.device)
         self._calib_ws: Optional[torch.Tensor] = None
+        self._calib_status = torch.zeros(1, dtype=torch.int32, device=Wg.device)     # the worst of all calibration calls since reset()
 
     # ------------------------------------------------------------------ forward
     def route(self, X: torch.Tensor, among: Optional[torch.Tensor] = None) -> Routed:
@@ -79,6 +80,7 @@ class ExpertLayer:
     # ------------------------------------------------------------------ calibration and pruning
     def reset(self) -> None:
         self.sumsq.zero_()
+        self._calib_status.zero_()
 
     def calibrate(self, X: torch.Tensor, routed: Optional[Routed] = None) -> list:
         """Adds a batch of tokens to every expert's neuron sums: the tokens routed to an expert are its calibration set.
@@ -92,6 +94,8 @@ class ExpertLayer:
         for e, (lo, hi) in enumerate(zip(edges, edges[1:])):
             if hi > lo:
                 b.calib_accumulate(Xs[lo:hi], self.Wg[e], self.Wu[e], self.act, self.sumsq[e], self._calib_ws)
+                # the next call clears the workspace's status word, and a larger workspace may replace it
+                torch.maximum(self._calib_status, self._calib_ws[:4].view(torch.int32), out=self._calib_status)
         return [hi - lo for lo, hi in zip(edges, edges[1:])]
 
     def finalize(self) -> torch.Tensor:
@@ -112,8 +116,8 @@ class ExpertLayer:
         return out
 
     def check(self) -> None:
-        """Raises if a bounded device-side wait gave up in any call so far (synchronises the stream)."""
-        if self._calib_ws is not None:
-            b.calib_status(self._calib_ws)
+        """Raises if a bounded device-side wait gave up in any calibration call since reset(), or in any pruning or product
+        that has not been reported yet (synchronises the stream)."""
+        b.calib_status(self._calib_status)
         b.prune_status()
         b.linear_status()
