@@ -48,6 +48,7 @@ class ExpertLayer:
         self.act, self.renormalise = b.ACT_BY_NAME[act], bool(renormalise)
         self.sumsq = torch.zeros((E, I), dtype=torch.float64, device=Wg.device)
         self.norm = torch.zeros((E, I), dtype=torch.float32, device=Wg.device)
+        self._finalized = False
         self._calib_ws: Optional[torch.Tensor] = None
         self._calib_status = torch.zeros(1, dtype=torch.int32, device=Wg.device)     # the worst of all calibration calls since reset()
 
@@ -100,15 +101,19 @@ class ExpertLayer:
 
     def finalize(self) -> torch.Tensor:
         """norm[e, i]: neuron i's norm over expert e's tokens (0 for an expert that none reached)."""
-        return b.norm_finalize(self.sumsq.view(-1), self.norm.view(-1)).view(self.E, self.I)
+        b.norm_finalize(self.sumsq.view(-1), self.norm.view(-1))
+        self._finalized = True
+        return self.norm
 
     def prune(self, alpha: float = 0.5, n_keep: int = 2, m: int = 4) -> "ExpertLayer":
         """A layer with every expert's projections pruned N:M by the norms of the last finalize(): Eq. 4 with ``alpha`` on
-        gate and up, Eq. 5 on down.  An expert without tokens has no norms: it is pruned by magnitude alone."""
+        gate and up, Eq. 5 on down.  An expert that had no tokens then has no norms: it is pruned by magnitude alone."""
+        if not self._finalized:
+            raise RuntimeError("prune() needs the norms of a finalize()")
         out = ExpertLayer(self.Wr, torch.empty_like(self.Wg), torch.empty_like(self.Wu), torch.empty_like(self.Wd), self.k,
                           renormalise=self.renormalise, router_bias=self.router_bias)
         out.act = self.act
-        seen = (self.sumsq > 0).any(dim=1, keepdim=True)
+        seen = (self.norm > 0).any(dim=1, keepdim=True)
         norm = torch.where(seen, self.norm, torch.ones_like(self.norm))
         for e in range(self.E):
             for W, P, axis, power in ((self.Wg, out.Wg, b.AXIS_ROWS, alpha), (self.Wu, out.Wu, b.AXIS_ROWS, alpha), (self.Wd, out.Wd, b.AXIS_COLS, 1.0)):

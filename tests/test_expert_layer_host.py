@@ -55,3 +55,31 @@ def test_check_sees_a_timeout_in_any_calibration_call(calibration):
         layer.check()
         layer.calibrate(X, routed=_routed([1, 0, 2, 0]))
         layer.check()
+
+
+def test_prune_goes_by_the_last_finalize_alone(calibration, monkeypatch):
+    used = []
+    monkeypatch.setattr(b, "norm_finalize", lambda sumsq, norm: norm.copy_(sumsq.sqrt()))
+    monkeypatch.setattr(b, "prune_nm", lambda W, norm, *a, **k: used.append(norm.clone()))
+    X, layer = torch.zeros(16, D), _layer()
+    with pytest.raises(RuntimeError):
+        layer.prune()                                                         # no norms yet
+    layer.calibrate(X, routed=_routed([2, 0, 3, 0]))
+    with pytest.raises(RuntimeError):
+        layer.prune()                                                         # sums, but still no norms
+    assert not used
+    norm = layer.finalize()
+    assert norm.shape == (E, I) and bool((norm[0] == 1).all()) and bool((norm[1] == 0).all())
+
+    def norms_of_prune():
+        used.clear()
+        layer.prune()
+        assert len(used) == 3 * E
+        return torch.stack(used[::3])
+    one = torch.ones(E, I)                                                    # experts 1 and 3 had no tokens: magnitude alone
+    layer.norm[0], one[0] = 0.5, 0.5
+    assert torch.equal(norms_of_prune(), one)
+    layer.calibrate(X, routed=_routed([0, 4, 0, 0]))                          # sums of a later batch are not the last finalize's norms
+    assert torch.equal(norms_of_prune(), one)
+    layer.reset()                                                             # nor does clearing them change those
+    assert torch.equal(norms_of_prune(), one)
