@@ -582,7 +582,7 @@ dass_status dass_expert_combine_backward(const void *dY, int64_t T, int64_t d, i
     DASS_BOUNDS_COMMIT(bs, st);
     (void)elt;
     // few threads a token keep its sums inside a warp; a whole block where there are few tokens
-    ErGrid g = er_grid(T > 0 ? T : rows, r, er_sum_cols(vector, k), T >= 148 * 32 ? 64 : ER_THREADS);
+    ErGrid g = er_grid(T > 0 ? T : rows, r, er_sum_cols(vector, k), T >= (int64_t)device_sm_count() * 32 ? 64 : ER_THREADS);
     g.grid.y = 1;                                                     // a token's threads walk its whole row
     const dim3 grid = g.grid, block = g.block;
     auto launch = [&](auto kernel) { kernel<<<grid, block, 0, st>>>(dY, lddy, Ys, ldys, slot, weight, rows_used, dYs, lddys, dweight, r); };
