@@ -275,7 +275,8 @@ dass_status dass_mlp_forward(const void *X, int64_t T, int64_t ldx,
  * nothing past a row's last element is read or written; sums and softmax are in f32, in a fixed order (equal inputs give
  * bit-equal results), with one rounding to `dt` at the end; inputs and outputs must not overlap except where stated.
  * Device-side integers are not trusted: ids, slots and offsets out of range never lead outside a buffer.
- * The first dass_linear on each device looks up an address and configures its kernel; make it before a stream capture.
+ * dass_linear looks up an address on its first call on a device and configures each of its kernels at that kernel's first
+ * launch there: make a call that is to be captured (the same sizes and options) once before the capture.
  */
 typedef enum { DASS_ROUTE_CHOSEN = 0, DASS_ROUTE_ALL = 1 } dass_route_norm;   /* what the weights' softmax runs over */
 

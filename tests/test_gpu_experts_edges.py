@@ -106,3 +106,22 @@ def test_a_timeout_is_reported_once_and_none_is_lost():
     W = torch.ones((4096, 2048), dtype=BF16, device=DEV)
     assert bool((b.linear(X, W) == 2048).all())
     b.linear_status()
+
+
+def test_a_call_that_was_made_once_can_be_captured():
+    """The same call replayed from a graph on new inputs; one size for each of the bf16 kernels."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(7)
+    for T, K, N in ((4, 64, 72), (64, 2048, 4096), (1100, 128, 136)):
+        X, W, Y = (torch.randn(s, generator=g, device=DEV).to(BF16) for s in ((T, K), (N, K), (T, N)))
+        b.linear(X, W, Y=Y)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.linear(X, W, Y=Y)
+        X.copy_(torch.randn((T, K), generator=g, device=DEV).to(BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, b.linear(X, W))
+        del graph
+    b.linear_status()
