@@ -242,11 +242,7 @@ calib_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 }
 
 // ------------------------------------------------------------------ host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_tiled_fn()
+EncodeTiledFn encode_tiled_fn()
 {
     static std::atomic<EncodeTiledFn> cached{nullptr};      // the same value whichever host thread resolves it first
     EncodeTiledFn fn = cached.load(std::memory_order_acquire);

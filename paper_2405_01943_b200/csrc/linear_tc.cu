@@ -379,25 +379,12 @@ static cudaError_t lt_pick(int act, const CUtensorMap &mx, const CUtensorMap &mw
 int *linear_timeouts();                                                                                      // linear.cu
 bool tc_make_map(CUtensorMap *map, const void *ptr, int64_t rows, int64_t cols, int64_t ld, int box_rows);   // calib_tc.cu
 
-typedef CUresult (*LinEncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                CUtensorMapFloatOOBfill);
-
 // `mats` row-major bf16 matrices [rows x cols] with pitch ld, mat_stride elements apart, as one map of three dimensions: boxes of
 // 64 x box_rows elements with the 128-byte swizzle; rows past a matrix's end read as zero, not as the next matrix's.
 bool tc_make_map_3d(CUtensorMap *map, const void *ptr, int64_t mats, int64_t rows, int64_t cols, int64_t ld, int64_t mat_stride, int box_rows)
 {
-    static std::atomic<LinEncodeFn> cached{nullptr};        // the same value whichever host thread resolves it first
-    LinEncodeFn fn = cached.load(std::memory_order_acquire);
-    if (!fn) {
-        void *entry = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &entry, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            return false;
-        fn = reinterpret_cast<LinEncodeFn>(entry);
-        cached.store(fn, std::memory_order_release);
-    }
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)mats};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)(mats > 1 ? mat_stride : rows * ld) * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};

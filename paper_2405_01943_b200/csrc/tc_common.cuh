@@ -133,6 +133,12 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int m, int n)
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+// The driver's tensor-map encoder, looked up once (calib_tc.cu); null where it is not found.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn();
+
 // Raises a kernel's dynamic shared-memory limit once per device (the attribute belongs to the device's copy of
 // the kernel).  `done` holds one bit per device ordinal; ordinals past 63 are configured on every call.  Safe to
 // call from several host threads: the mask is atomic, and setting the attribute twice is harmless.
