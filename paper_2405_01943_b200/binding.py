@@ -198,8 +198,12 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
 def _stream_of(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
     """The given stream, or the current one of the tensor's device (by its raw handle: building a Stream object costs as
     much as the launch of a small kernel)."""
-    device = _here(t, stream)
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+    if stream is None:
+        device = t.get_device()
+        if device == torch._C._cuda_getDevice():
+            return torch._C._cuda_getCurrentRawStream(device)
+    _here(t, stream)
+    return stream.cuda_stream
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -223,9 +227,9 @@ def _made(stream: Optional[torch.cuda.Stream], device: torch.device, make: Calla
     return out
 
 
-def _new(t: torch.Tensor, shape, dtype: Optional[torch.dtype], stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """An uninitialised tensor on t's device for a call on `stream`."""
-    return t.new_empty(shape, dtype=dtype) if stream is None else _made(stream, t.device, lambda: t.new_empty(shape, dtype=dtype))
+def _new(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> Callable[..., torch.Tensor]:
+    """t.new_empty for a call on `stream`."""
+    return t.new_empty if stream is None else lambda shape, dtype=None: _made(stream, t.device, lambda: t.new_empty(shape, dtype=dtype))
 
 
 def _workspace(t: torch.Tensor, device: torch.device) -> None:
@@ -308,7 +312,7 @@ def norm_finalize(sumsq: torch.Tensor, norm: Optional[torch.Tensor] = None,
     """norm = float32(sqrt(sumsq))."""
     _here(sumsq, stream)
     if norm is None:
-        norm = _new(sumsq, sumsq.numel(), torch.float32, stream)
+        norm = _new(sumsq, stream)(sumsq.numel(), dtype=torch.float32)
     code = load().dass_norm_finalize(sumsq.data_ptr(), sumsq.numel(), norm.data_ptr(), _stream(stream))
     _check(code, "dass_norm_finalize")
     return norm
@@ -331,7 +335,7 @@ def score_nm(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alpha: float, 
     if norm.numel() != (rows if norm_axis == AXIS_ROWS else cols):
         raise ValueError("norm has the wrong length for norm_axis")
     if mask_bits is None and want_mask:
-        mask_bits = _new(W, (rows, mask_words_per_row(cols)), torch.int32, stream)
+        mask_bits = _new(W, stream)((rows, mask_words_per_row(cols)), dtype=torch.int32)
     if W_pruned is None and want_pruned:
         W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if W_pruned is not None:
@@ -361,9 +365,9 @@ def compress_nm(W: torch.Tensor, mask_bits: torch.Tensor, n_keep: int, m: int, g
     rows, cols, ld = _matrix(W, "W")
     vshape, mshape = compress_shapes(rows, cols, n_keep, m, group_axis)
     if values is None:
-        values = _new(W, vshape, None, stream)
+        values = _new(W, stream)(vshape)
     if meta is None:
-        meta = _new(W, mshape, torch.int32, stream)
+        meta = _new(W, stream)(mshape, dtype=torch.int32)
     if tuple(values.shape) != vshape or not values.is_contiguous() or values.dtype != W.dtype:
         raise ValueError(f"values must be a contiguous {vshape} tensor of W's dtype")
     if tuple(meta.shape) != mshape or not meta.is_contiguous() or meta.dtype != torch.int32:
@@ -391,7 +395,7 @@ def prune_nm(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alpha: float, 
     if norm.numel() != (rows if norm_axis == AXIS_ROWS else cols):
         raise ValueError("norm has the wrong length for norm_axis")
     if mask_bits is None and want_mask:
-        mask_bits = _new(W, (rows, mask_words_per_row(cols)), torch.int32, stream)
+        mask_bits = _new(W, stream)((rows, mask_words_per_row(cols)), dtype=torch.int32)
     if W_pruned is None and want_pruned:
         W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if W_pruned is not None:
@@ -404,9 +408,9 @@ def prune_nm(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alpha: float, 
     if want_compressed or values is not None or meta is not None:
         vshape, mshape = compress_shapes(rows, cols, n_keep, m, group_axis)
         if values is None:
-            values = _new(W, vshape, None, stream)
+            values = _new(W, stream)(vshape)
         if meta is None:
-            meta = _new(W, mshape, torch.int32, stream)
+            meta = _new(W, stream)(mshape, dtype=torch.int32)
         if tuple(values.shape) != vshape or not values.is_contiguous() or values.dtype != W.dtype:
             raise ValueError(f"values must be a contiguous {vshape} tensor of W's dtype")
         if tuple(meta.shape) != mshape or not meta.is_contiguous() or meta.dtype != torch.int32:
@@ -459,7 +463,7 @@ def select_unstructured(W: torch.Tensor, norm: torch.Tensor, norm_axis: int, alp
     if norm.numel() != (rows if norm_axis == AXIS_ROWS else cols):
         raise ValueError("norm has the wrong length for norm_axis")
     if mask_bits is None and want_mask:
-        mask_bits = _new(W, (rows, mask_words_per_row(cols)), torch.int32, stream)
+        mask_bits = _new(W, stream)((rows, mask_words_per_row(cols)), dtype=torch.int32)
     if W_pruned is None and want_pruned:
         W_pruned = _made(stream, W.device, lambda: W.new_empty_strided((rows, cols), (ld, 1)))
     if workspace is None:
@@ -492,7 +496,7 @@ def feature_sumsq(X: torch.Tensor, sumsq: Optional[torch.Tensor] = None, workspa
     need = ctypes.c_size_t(0)
     _check(load().dass_feature_workspace_bytes(T, d, ctypes.byref(need)), "dass_feature_workspace_bytes")
     if workspace is None:
-        workspace = _new(X, need.value + 16, torch.uint8, stream)
+        workspace = _new(X, stream)(need.value + 16, dtype=torch.uint8)
         off = (-workspace.data_ptr()) % 16
         workspace = workspace[off:off + need.value]
     else:
@@ -537,7 +541,7 @@ def mlp_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.T
     if not (Wg.dtype == Wu.dtype == Wd.dtype == X.dtype):
         raise ValueError("X, Wg, Wu, Wd must have one dtype")
     if Z is None:
-        Z = _new(X, (T, d), None, stream)
+        Z = _new(X, stream)((T, d))
     Tz, dz, ldz = _matrix(Z, "Z")
     if (Tz, dz) != (T, d) or Z.dtype != X.dtype:
         raise ValueError("Z must be [T x d] in X's dtype")
@@ -556,7 +560,7 @@ def mlp_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.T
 # ----------------------------------------------------------------------------- mixture of experts
 #
 # These calls are made once per layer and decode step, so what they do on the host is kept short: one pass over each
-# tensor's shape and strides, the stream by its handle.
+# tensor's shape and strides, outputs from new_empty, the stream by its handle.
 
 _CODES = {torch.bfloat16: BF16, torch.float32: F32}
 
@@ -600,12 +604,13 @@ def route_topk(logits: torch.Tensor, k: int, renormalise: bool = True, expert: O
     (``renormalise``) or over all experts.  logits [T x E]; returns (expert int32 [T x k], weight float32 [T x k])."""
     T, E, ld = _rows(logits, "logits")
     k, dt = int(k), _code(logits)
+    new = _new(logits, stream)
     if expert is None:
-        expert = _new(logits, (T, max(k, 0)), torch.int32, stream)
+        expert = new((T, max(k, 0)), dtype=torch.int32)
     else:
         _same(expert, "expert", (T, k), torch.int32, logits.device)
     if weight is None:
-        weight = _new(logits, (T, max(k, 0)), torch.float32, stream)
+        weight = new((T, max(k, 0)), dtype=torch.float32)
     else:
         _same(weight, "weight", (T, k), torch.float32, logits.device)
     if T:
@@ -623,7 +628,7 @@ def route_topk_backward(logits: torch.Tensor, expert: torch.Tensor, dweight: tor
     ids = _same(expert, "expert", (T, k), torch.int32, logits.device)
     dw = _same(dweight, "dweight", (T, k), torch.float32, logits.device)
     if dlogits is None:
-        dlogits, ldd = _new(logits, (T, E), None, stream), E
+        dlogits, ldd = _new(logits, stream)((T, E)), E
     else:
         ldd = _like(dlogits, "dlogits", T, E, logits)
     if T:
@@ -648,21 +653,22 @@ def expert_sort(expert: torch.Tensor, E: int, offsets: Optional[torch.Tensor] = 
     (T, k), E, dev = expert.shape, int(E), expert.device
     ids = _same(expert, "expert", (T, k), torch.int32, dev)
     edges = E + 1 if E > 0 else 1
+    new = _new(expert, stream)
     if offsets is None:
-        offsets = _new(expert, edges, None, stream)
+        offsets = new(edges)
     else:
         _same(offsets, "offsets", (edges,), torch.int32, dev)
     if slot is None:
-        slot = _new(expert, (T, k), None, stream)
+        slot = new((T, k))
     else:
         _same(slot, "slot", (T, k), torch.int32, dev)
     if source is None:
-        source = _new(expert, T * k, None, stream)
+        source = new(T * k)
     else:
         _same(source, "source", (T * k,), torch.int32, dev)
     if workspace is None:
         need = expert_sort_workspace_bytes(T, k, E)
-        workspace = _new(expert, need, torch.uint8, stream) if need else None
+        workspace = new(need, dtype=torch.uint8) if need else None
     else:
         _workspace(workspace, dev)
     _check(load().dass_expert_sort(ids, T, k, E, offsets.data_ptr(), slot.data_ptr(), source.data_ptr(),
@@ -700,7 +706,7 @@ def expert_gather(X: torch.Tensor, slot: torch.Tensor, offsets: Optional[torch.T
         raise ValueError("X and slot must have the same number of tokens")
     if Xs is None:
         rows, ldxs = T * k, d
-        Xs = _new(X, (rows, d), None, stream)
+        Xs = _new(X, stream)((rows, d))
     else:
         rows = Xs.shape[0]
         ldxs = _like(Xs, "Xs", rows, d, X)
@@ -717,7 +723,7 @@ def expert_combine(Ys: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.
     T, k = _slots(slot, weight, Ys.device)
     ldr = _like(residual, "residual", T, d, Ys) if residual is not None else 0
     if Y is None:
-        Y, ldy = _new(Ys, (T, d), None, stream), d
+        Y, ldy = _new(Ys, stream)((T, d)), d
     else:
         ldy = _like(Y, "Y", T, d, Ys)
     _check(load().dass_expert_combine(Ys.data_ptr(), rows, d, ldys, _code(Ys), slot.data_ptr(), T, k, _ptr(weight),
@@ -744,14 +750,15 @@ def expert_combine_backward(dY: torch.Tensor, Ys: torch.Tensor, slot: torch.Tens
     if Ty != T:
         raise ValueError("dY and slot must have the same number of tokens")
     lddys = d
+    new = _new(dY, stream)
     if dYs is not None:
         lddys = _like(dYs, "dYs", rows, d, dY)
     elif want_rows:
-        dYs = _new(dY, (rows, d), None, stream)
+        dYs = new((rows, d))
     if dweight is not None:
         _same(dweight, "dweight", (T, k), torch.float32, dY.device)
     elif want_weight:
-        dweight = _new(dY, (T, k), torch.float32, stream)
+        dweight = new((T, k), dtype=torch.float32)
     dt = _code(dY)
     if T or (dYs is not None and offsets is not None):
         _check(load().dass_expert_combine_backward(dY.data_ptr(), T, d, lddy, Ys.data_ptr(), rows, ldys, dt, slot.data_ptr(), k,
@@ -790,7 +797,7 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     ldr = _like(residual, "residual", T, N, X) if residual is not None else 0
     dt = _code(X)
     if Y is None:
-        Y, ldy = _new(X, (T, N), None, stream), N
+        Y, ldy = _new(X, stream)((T, N)), N
     else:
         ldy = _like(Y, "Y", T, N, X)
     if T:
