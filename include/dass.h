@@ -58,7 +58,7 @@ typedef enum {
     DASS_ERR_UNSUPPORTED = 5,  /* a valid request the library has no kernel for */
     DASS_ERR_WORKSPACE = 6,    /* workspace NULL or smaller than the query says */
     DASS_ERR_CUDA = 7,         /* a CUDA runtime / driver call failed */
-    DASS_ERR_TIMEOUT = 8,      /* a bounded device-side wait ran out (reported by dass_calib_status / dass_prune_status) */
+    DASS_ERR_TIMEOUT = 8,      /* a bounded device-side wait ran out (reported by dass_calib_status / dass_prune_status / dass_linear_status) */
     DASS_ERR_INTERNAL = 9      /* a consistency check between two passes of a kernel chain failed (dass_prune_status) */
 } dass_status;
 

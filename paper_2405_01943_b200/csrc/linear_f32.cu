@@ -273,7 +273,7 @@ dass_status linear_f32_launch(const LinearArgs &a)
     const int64_t rows = a.offsets ? (a.T + a.groups - 1) / a.groups : a.T, groups = lin_active_groups(a);
     const int64_t cols = a.W_up ? 2 * a.N : a.N;
     auto tiles = [&](int64_t bt, int64_t bn) { return ((a.T + bt - 1) / bt + (a.offsets ? groups / 2 : 0)) * ((cols + bn - 1) / bn); };
-    // The largest tile that still gives most SMs one (1024 rows, 4096 x 4096: 763 us with 128 x 128, 938 with 64 x 64, 1250
+    // The largest tile that still gives most SMs one (1024 rows, 4096 x 4096: 763 to 822 us with 128 x 128, 938 with 64 x 64, 1250
     // with 32 x 32; 128 rows: 422, 191, 192); few rows, while reading them again and again costs less than a tile's start
     // (4096 x 4096: 4 rows 32 against 66 us, 16 rows 86 against 63; 700 x 200 gated, 16 rows 5 against 12).
     const double products = (double)a.T * cols * a.K;

@@ -14,12 +14,12 @@
 // operands, are 2 to 10 % slower).
 //
 // Tiles of 256 columns, or of 128 where those fill the machine better (512 rows, 4096 x 4096: 21 against 30 us).  Bound by
-// the tensor pipe and, run back to back, by the power it draws: 8192^3 with bias and residual takes 871 us (1263 TFLOP/s;
-// a library product without them 784 to 801), 705 us as a single burst; 16384 rows of 8 experts 4096 -> 14336 gated 3.03
+// the tensor pipe and, run back to back, by the power it draws: 8192^3 with bias and residual takes 868 to 906 us (1267 to
+// 1213 TFLOP/s; 865 without them on the card of 890, a library product 806 there), 705 us as a single burst; 16384 rows of 8 experts 4096 -> 14336 gated 3.03
 // ms, 14336 -> 4096 1.60 ms.  With short contractions the epilogue bounds (16384 x 512 -> 2048: 35 us).
 //
-// Every wait is bounded: when one runs out the CTA raises an abort flag, counts it for
-// dass_linear_status, lets its roles drain and frees its TMEM before it returns.
+// Every wait is bounded: when one runs out the CTA raises an abort flag, counts it for dass_linear_status, lets its roles
+// drain and frees its TMEM before it returns.
 #include "linear_common.cuh"
 #include "linear_tc.cuh"
 #include "tc_common.cuh"

@@ -70,7 +70,8 @@ __device__ __forceinline__ float ex2_approx(float x)
 
 // The activation before a rounding to bf16 (8 bits): an exponential and a reciprocal of the special-function unit, a few
 // units of f32's last place off, are exact enough by 2^10 and keep the epilogue at two such instructions per element.
-// x / (1 + e^-x) holds at the ends too: e^-x = inf gives a reciprocal of 0.
+// x / (1 + e^-x) holds at the ends too: e^-x = inf gives a reciprocal of 0.  Both instructions flush subnormals, so that
+// results below 1e-36 in size (SiLU of x < -87.3) come out as zero.
 template <int ACT>
 __device__ __forceinline__ float lt_act(float x)
 {

@@ -54,7 +54,10 @@ class ExpertLayer:
 
     # ------------------------------------------------------------------ forward
     def route(self, X: torch.Tensor, among: Optional[torch.Tensor] = None) -> Routed:
-        """The router's choice; with ``among`` (truth values [T x E]) only among the experts it names."""
+        """The router's choice; with ``among`` (truth values [T x E]) only among the experts it names.
+
+        The logits are stored in X's dtype, as a projection's output is: for a bf16 layer two experts closer than one part in
+        256 can tie, and then the lower index is chosen."""
         logits = b.linear(X, self.Wr, bias=self.router_bias)
         if among is not None:
             logits = logits.masked_fill(~among, float("-inf"))
@@ -62,7 +65,10 @@ class ExpertLayer:
         return Routed(logits, expert, weight, *b.expert_sort(expert, self.E))
 
     def forward(self, X: torch.Tensor, residual: Optional[torch.Tensor] = None, routed: Optional[Routed] = None, keep: bool = False):
-        """Y[t] = residual[t] + sum_j weight[t,j] * expert_j(X[t]).  With ``keep`` also what router_gradient needs."""
+        """Y[t] = residual[t] + sum_j weight[t,j] * expert_j(X[t]).  With ``keep`` also what router_gradient needs.
+
+        An expert's intermediate H and its output are rounded to X's dtype between the calls, as a dense layer's are: in bf16
+        an expert's output is 2.3e-3 off the exact one, of which the last rounding alone is 1.7e-3."""
         r = routed if routed is not None else self.route(X)
         Xs = b.expert_gather(X, r.slot, r.offsets)
         H = b.linear(Xs, self.Wg, act=self.act, W_up=self.Wu, offsets=r.offsets)
