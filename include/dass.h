@@ -341,6 +341,63 @@ dass_status dass_linear(const void *X, int64_t T, int64_t K, int64_t ldx, const 
                         void *Y, int64_t ldy, dass_dtype dt, const int32_t *offsets, int64_t groups, void *cuda_stream);
 dass_status dass_linear_status(void *cuda_stream);
 
+/* The balance of a router's choices: how many each expert got, and a loss that grows as loads and probabilities gather on
+ * the same experts.  A token counts if it has a choice inside [0, E) (a padding token, all -1, does not); with n such tokens,
+ * c_e choices of expert e (entries of `expert` outside [0, E) are skipped) and p_t the softmax of token t's unmasked logits
+ * (-inf and NaN mask, +inf is the largest finite f32, as in dass_route_topk; p_t = 0 where all are masked):
+ *     counts[e] = c_e, counts[E] = n;   share[e] = P_e = 1/n sum_t p_te;   f_e = c_e / (n k);   *loss = E sum_e f_e P_e
+ * which is 1 for even loads and E for one expert alone; all zero for n = 0.
+ * logits [T x E, ld] in `dt`, expert [T x k] int32; loss one f32, counts [E + 1] int32, share [E] f32.  E <= 1024, k <= 32,
+ * T k < 2^31.  workspace: dass_route_balance_workspace_bytes(T, E) bytes (may be 0), 16-byte aligned.
+ * Errors: NULL / DTYPE / SHAPE / UNSUPPORTED / ALIGN / WORKSPACE / CUDA. */
+dass_status dass_route_balance_workspace_bytes(int64_t T, int64_t E, size_t *bytes /* HOST */);
+dass_status dass_route_balance(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, const int32_t *expert, int64_t k,
+                               float *loss, int32_t *counts, float *share, void *workspace, size_t workspace_bytes, void *cuda_stream);
+/* dlogits[t,e] = add[t,e] + dloss E/n p_te (f_e - sum_i f_i p_ti)   (the second term 0 for tokens that do not count).
+ * counts [E + 1]: dass_route_balance's, or their sums over several batches or ranks (n and c_e alike): f and n then are those of
+ * all of them.  dloss (device, one f32, nullable: 1).  add [T x E, lda] in `dt`, nullable, e.g. dass_route_topk_backward's
+ * result; dlogits [T x E, ldd] in `dt`, written in full, may be `add` itself (same pitch). */
+dass_status dass_route_balance_backward(const void *logits, int64_t T, int64_t E, int64_t ld, dass_dtype dt, const int32_t *expert, int64_t k,
+                                        const int32_t *counts, const float *dloss, const void *add, int64_t lda,
+                                        void *dlogits, int64_t ldd, void *cuda_stream);
+
+/* ------------------------------------------------------------------ microscaled 4-bit values
+ * (No counterpart in the paper.)  What a pruned matrix still holds, in 4.25 bits a value: blocks of 32 consecutive values of
+ * a row share a power-of-two scale, each value is a 4-bit float (1 sign, 2 exponent, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6).  Zeros stay zeros, so a pruned matrix keeps its mask.
+ *
+ * codes:  [rows x ceil(K/32) * 16] bytes, dense; value k of a row is the low (even k) or high (odd k) half of byte k / 2: sign
+ *         (8), then the index into the eight sizes above.
+ * scales: tiles of 128 rows x 4 blocks (512 bytes), [ceil(rows/128) x ceil(K/128)] of them, row-major: the scale of row r, block b
+ *         is byte (r % 32) * 16 + r % 128 / 32 * 4 + b % 4 of tile (r / 128, b / 4), the order the tensor cores read.  A byte s
+ *         stands for 2^(s - 127), 255 for NaN (the whole block).
+ * Both 16-byte aligned.  Codes past K and scales past the last row or block are zero; products count on that.
+ * dass_mx4_bytes gives the sizes for one matrix; `groups` matrices (experts) lie one after the other.
+ *
+ * Quantisation: s = max(0, floor(log2 max|x|) - 2 + 127) over the block, code = x / 2^(s - 127) rounded to nearest, ties to the
+ * even code, sizes beyond 6 to 6.  A block that holds a NaN or an infinity becomes NaN.  X: `groups` matrices [rows x K, ldx],
+ * group_stride elements apart, in `dt`, of any element-aligned pointer and pitch.  rows = 0 is a valid request.
+ * Dequantisation gives the exact values (all of them are bf16 numbers; those of scales above 2^125, which quantisation does
+ * not produce, may overflow to infinity) in Y [rows x K, ldy].
+ * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (dimensions beyond 32-bit coordinates) / CUDA. */
+dass_status dass_mx4_bytes(int64_t rows, int64_t K, size_t *codes /* HOST, nullable */, size_t *scales /* HOST, nullable */);
+dass_status dass_mx4_quantize(const void *X, int64_t groups, int64_t rows, int64_t K, int64_t ldx, int64_t group_stride, dass_dtype dt,
+                              uint8_t *codes, uint8_t *scales, void *cuda_stream);
+dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K,
+                                void *Y, int64_t ldy, int64_t group_stride, dass_dtype dt, void *cuda_stream);
+
+/* dass_linear with weights in 4 bits:
+ *     Y = act(X W^T + bias) [ * (X W_up^T + bias_up) ] + residual          one rounding to bf16, at Y
+ * X [T x K] is given in bf16 (X, ldx; 16-byte aligned, pitch of whole 16 bytes) or in 4 bits (x_codes, x_scales), not both.
+ * W (w_codes, w_scales) and W_up (nullable: the GLU form) are `groups` matrices [N x K].  Products of the values that codes and
+ * scales stand for, in f32 accumulators.  bias, bias_up, residual, Y in bf16, offsets and groups, alignment and what else is
+ * not said here: as for dass_linear, whose dass_linear_status reports this call's bounded waits too.
+ * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (X in both forms; limits of dass_linear) / CUDA. */
+dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, const uint8_t *x_scales, int64_t T, int64_t K,
+                            const uint8_t *w_codes, const uint8_t *w_scales, const uint8_t *up_codes, const uint8_t *up_scales, int64_t N,
+                            const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,
+                            void *Y, int64_t ldy, const int32_t *offsets, int64_t groups, void *cuda_stream);
+
 /* ------------------------------------------------------------------ checked-access build
  * (No counterpart in the paper: the stand-in for a memory sanitizer.)  libdass_check.so is this library compiled with
  * -DDASS_BOUNDS_CHECK (python -m paper_2405_01943_b200.build --bounds-check).  In it every entry point registers the

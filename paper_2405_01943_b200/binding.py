@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Callable, Optional, Tuple
+from typing import Callable, NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -32,6 +32,8 @@ EXPORTS = (
     "dass_mlp_forward_workspace_bytes", "dass_mlp_forward",
     "dass_route_topk", "dass_route_topk_backward", "dass_expert_sort_workspace_bytes", "dass_expert_sort",
     "dass_expert_gather", "dass_expert_combine", "dass_expert_combine_backward", "dass_linear", "dass_linear_status",
+    "dass_route_balance_workspace_bytes", "dass_route_balance", "dass_route_balance_backward",
+    "dass_mx4_bytes", "dass_mx4_quantize", "dass_mx4_dequantize", "dass_linear_mx4",
     "dass_bounds_report", "dass_bounds_shrink_next",
     "dass_status_string", "dass_version",
 )
@@ -137,6 +139,20 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.dass_linear.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, i64, vp, vp, ci, vp, i64, vp, i64, ci, vp, i64, vp]
     lib.dass_linear_status.restype = ci
     lib.dass_linear_status.argtypes = [vp]
+    lib.dass_route_balance_workspace_bytes.restype = ci
+    lib.dass_route_balance_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.dass_route_balance.restype = ci
+    lib.dass_route_balance.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.dass_route_balance_backward.restype = ci
+    lib.dass_route_balance_backward.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+    lib.dass_mx4_bytes.restype = ci
+    lib.dass_mx4_bytes.argtypes = [i64, i64, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.dass_mx4_quantize.restype = ci
+    lib.dass_mx4_quantize.argtypes = [vp, i64, i64, i64, i64, i64, ci, vp, vp, vp]
+    lib.dass_mx4_dequantize.restype = ci
+    lib.dass_mx4_dequantize.argtypes = [vp, vp, i64, i64, i64, vp, i64, i64, ci, vp]
+    lib.dass_linear_mx4.restype = ci
+    lib.dass_linear_mx4.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp, ci, vp, i64, vp, i64, vp, i64, vp]
     lib.dass_status_string.restype = ctypes.c_char_p
     lib.dass_status_string.argtypes = [ctypes.c_int]
     lib.dass_version.restype = ctypes.c_int
@@ -810,3 +826,202 @@ def linear_status(stream: Optional[torch.cuda.Stream] = None) -> None:
     """Waits for the stream and raises if a bounded wait inside a linear kernel ran out on the current device since the last
     query."""
     _check(load().dass_linear_status(_stream(stream)), "dass_linear_status")
+
+
+# ----------------------------------------------------------------------------- the router's balance
+
+def route_balance_workspace_bytes(T: int, E: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().dass_route_balance_workspace_bytes(int(T), int(E), ctypes.byref(out)), "dass_route_balance_workspace_bytes")
+    return int(out.value)
+
+
+def route_balance(logits: torch.Tensor, expert: torch.Tensor, loss: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+                  share: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """The balance loss of a router's choices and the loads behind it.  logits [T x E], expert int32 [T x k] (route_topk's;
+    entries outside [0, E) are no choices).  Returns (loss float32 [], counts int32 [E + 1], share float32 [E]): counts[:E]
+    choices per expert, counts[E] the tokens with a choice, share the mean probability of each expert over those."""
+    T, E, ld = _rows(logits, "logits")
+    dt, dev = _code(logits), logits.device
+    k = expert.shape[1] if expert.dim() == 2 else -1
+    ids = _same(expert, "expert", (T, k), torch.int32, dev)
+    new = _new(logits, stream)
+    if loss is None:
+        loss = new((), dtype=torch.float32)
+    else:
+        _same(loss, "loss", (), torch.float32, dev)
+    if counts is None:
+        counts = new(E + 1, dtype=torch.int32)
+    else:
+        _same(counts, "counts", (E + 1,), torch.int32, dev)
+    if share is None:
+        share = new(E, dtype=torch.float32)
+    else:
+        _same(share, "share", (E,), torch.float32, dev)
+    if workspace is None:
+        need = route_balance_workspace_bytes(T, E)
+        workspace = new(need, dtype=torch.uint8) if need else None
+    else:
+        _workspace(workspace, dev)
+    _check(load().dass_route_balance(logits.data_ptr(), T, E, ld, dt, ids, k, loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
+                                     _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream_of(logits, stream)),
+           "dass_route_balance")
+    return loss, counts, share
+
+
+def route_balance_backward(logits: torch.Tensor, expert: torch.Tensor, counts: torch.Tensor, dloss: Optional[torch.Tensor] = None,
+                           add: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The logits' gradient [T x E] of route_balance's loss, times ``dloss`` (a float32 scalar on the device; 1 without it),
+    plus ``add`` (another gradient of the logits).  ``counts`` as route_balance returned it, or summed over batches."""
+    T, E, ld = _rows(logits, "logits")
+    dt, dev = _code(logits), logits.device
+    k = expert.shape[1] if expert.dim() == 2 else -1
+    ids = _same(expert, "expert", (T, k), torch.int32, dev)
+    load_ = _same(counts, "counts", (E + 1,), torch.int32, dev)
+    scale = _same(dloss, "dloss", (), torch.float32, dev) if dloss is not None else None
+    lda = _like(add, "add", T, E, logits) if add is not None else 0
+    if dlogits is None:
+        dlogits, ldd = _new(logits, stream)((T, E)), E
+    else:
+        ldd = _like(dlogits, "dlogits", T, E, logits)
+    _check(load().dass_route_balance_backward(logits.data_ptr(), T, E, ld, dt, ids, k, load_, scale, _ptr(add), lda, dlogits.data_ptr(),
+                                              ldd, _stream_of(logits, stream)), "dass_route_balance_backward")
+    return dlogits
+
+
+# ----------------------------------------------------------------------------- microscaled 4-bit values
+
+class MX4(NamedTuple):
+    """A matrix [rows x cols], or a stack of them, in 4 bits: ``codes`` uint8 [(G x) rows x 16 ceil(cols / 32)] and ``scales``
+    uint8 [(G x) ceil(rows / 128) x ceil(cols / 128) x 512], in the layout of include/dass.h."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+
+    @property
+    def shape(self) -> Tuple[int, ...]:
+        return (*self.codes.shape[:-1], self.cols)
+
+    @property
+    def device(self) -> torch.device:
+        return self.codes.device
+
+
+def _mx4_shapes(lead: Tuple[int, ...], cols: int) -> Tuple[Tuple[int, ...], Tuple[int, ...]]:
+    return (*lead, (cols + 31) // 32 * 16), (*lead[:-1], (lead[-1] + 127) // 128, (cols + 127) // 128, 512)
+
+
+def _mx4(q: MX4, name: str, device: torch.device) -> Tuple[int, int]:
+    """Checks a 4-bit matrix and returns its addresses."""
+    codes, scales, cols = q
+    lead = codes.shape[:-1]
+    if len(lead) not in (1, 2) or cols < 1:
+        raise ValueError(f"{name} must be an MX4 of [rows x cols] or [G x rows x cols]")
+    want = _mx4_shapes(lead, cols)
+    return _same(codes, f"{name}.codes", want[0], torch.uint8, device), _same(scales, f"{name}.scales", want[1], torch.uint8, device)
+
+
+def mx4_quantize(X: torch.Tensor, out: Optional[MX4] = None, stream: Optional[torch.cuda.Stream] = None) -> MX4:
+    """X [rows x cols] or [G x rows x cols] (bfloat16 or float32, unit stride along columns) in microscaled 4-bit values."""
+    if X.dim() not in (2, 3) or not X.is_cuda:
+        raise ValueError("X must be a 2-D or 3-D CUDA tensor")
+    _here(X, stream)
+    shape, strides = X.shape, X.stride()
+    G, rows, cols = shape if len(shape) == 3 else (1, *shape)
+    if strides[-1] != 1 and cols > 1:
+        raise ValueError("X must have unit stride along its columns")
+    dt = _code(X)
+    if cols < 1 or G < 1:
+        raise ValueError("X must have columns (and, as a stack, matrices)")
+    ld = strides[-2] if rows > 1 or strides[-2] > cols else cols
+    if out is None:
+        want, new = _mx4_shapes(shape[:-1], cols), _new(X, stream)
+        out = MX4(new(want[0], dtype=torch.uint8), new(want[1], dtype=torch.uint8), cols)
+    elif out.shape != shape:
+        raise ValueError("out must be an MX4 of X's shape")
+    codes, scales = _mx4(out, "out", X.device)
+    if rows:
+        _check(load().dass_mx4_quantize(X.data_ptr(), G, rows, cols, ld, strides[0] if len(shape) == 3 else 0, dt, codes, scales,
+                                        _stream_of(X, stream)), "dass_mx4_quantize")
+    return out
+
+
+def mx4_dequantize(Q: MX4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The values an MX4 stands for, exactly."""
+    if not Q.codes.is_cuda:
+        raise ValueError("Q must be on a CUDA device")
+    _here(Q.codes, stream)
+    codes, scales = _mx4(Q, "Q", Q.codes.device)
+    shape = Q.shape
+    G, rows, cols = shape if len(shape) == 3 else (1, *shape)
+    if out is None:
+        out = _new(Q.codes, stream)(shape, dtype=dtype)
+    elif out.shape != shape or out.dtype != dtype or out.device != Q.codes.device or (out.stride(-1) != 1 and cols > 1):
+        raise ValueError("out must be a tensor of Q's shape and device and of the dtype asked for, with unit stride along its columns")
+    strides, dt = out.stride(), _code(out)
+    ld = strides[-2] if rows > 1 or strides[-2] > cols else cols
+    if rows:
+        _check(load().dass_mx4_dequantize(codes, scales, G, rows, cols, out.data_ptr(), ld, strides[0] if len(shape) == 3 else 0, dt,
+                                          _stream_of(Q.codes, stream)), "dass_mx4_dequantize")
+    return out
+
+
+def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, W_up: Optional[MX4] = None,
+               bias_up: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+               Y: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """linear() with weights in 4 bits: Y = act(X W^T + bias) [* (X W_up^T + bias_up)] + residual in bfloat16.
+
+    X [T x K] is a bfloat16 matrix or an MX4 (mx4_quantize's).  Dense: W (and W_up) [N x K]; per expert, with ``offsets``:
+    [G x N x K], as for linear().  ``Y`` may be the residual itself."""
+    quantized = isinstance(X, MX4)
+    if quantized:
+        first = X.codes
+        if first.dim() != 2 or not first.is_cuda:
+            raise ValueError("X must be an MX4 of [T x K] on a CUDA device")
+        (T, K), ldx, x = X.shape, 0, None
+        xc, xs = _mx4(X, "X", first.device)
+    else:
+        first = X
+        T, K, ldx = _rows(X, "X")
+        if X.dtype != torch.bfloat16:
+            raise TypeError(f"unsupported dtype {X.dtype}: linear_mx4 takes bfloat16 rows or an MX4")
+        x, xc, xs = X.data_ptr(), None, None
+    device, dtype = first.device, torch.bfloat16
+    shape = W.shape
+    if len(shape) != (2 if offsets is None else 3) or shape[-1] != K:
+        raise ValueError(f"W must be an MX4 of {'[N x K]' if offsets is None else '[G x N x K]'}")
+    wc, ws = _mx4(W, "W", device)
+    uc = us = None
+    if W_up is not None:
+        if W_up.shape != shape:
+            raise ValueError("W_up must have W's shape")
+        uc, us = _mx4(W_up, "W_up", device)
+    N = shape[-2]
+    if offsets is None:
+        groups, edges, per = 1, None, (N,)
+    else:
+        groups = shape[0]
+        edges, per = _same(offsets, "offsets", (groups + 1,), torch.int32, device), (groups, N)
+    b = _same(bias, "bias", per, dtype, device) if bias is not None else None
+    if bias_up is not None and W_up is None:
+        raise ValueError("bias_up goes with W_up")
+    bu = _same(bias_up, "bias_up", per, dtype, device) if bias_up is not None else None
+
+    def like(t: torch.Tensor, name: str) -> int:
+        r, c, ld = _rows(t, name)
+        if r != T or c != N or t.dtype != dtype or t.device != device:
+            raise ValueError(f"{name} must be a {dtype} matrix of shape {(T, N)} on {device}")
+        return ld
+
+    ldr = like(residual, "residual") if residual is not None else 0
+    if Y is None:
+        Y, ldy = _new(first, stream)((T, N), dtype=dtype), N
+    else:
+        ldy = like(Y, "Y")
+    if T:
+        _check(load().dass_linear_mx4(x, ldx, xc, xs, T, K, wc, ws, uc, us, N, b, bu, act, _ptr(residual), ldr, Y.data_ptr(), ldy, edges,
+                                      groups, _stream_of(first, stream)), "dass_linear_mx4")
+    return Y
