@@ -4,6 +4,7 @@
 namespace dass {
 
 dass_status mx4_few_launch(const Mx4Args &p, int eights, int sixteens, int split);     // mx4_few.cu
+dass_status mx4_tc_launch(const Mx4Args &p, int columns);                              // mx4_tc.cu
 int device_sm_count();                                                                 // dass_abi.cu
 
 }  // namespace dass
@@ -55,6 +56,7 @@ dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, 
     DASS_BOUNDS_ADD(bs, Y, ((size_t)(T - 1) * ldy + N) * 2);
     DASS_BOUNDS_ADD(bs, offsets, (size_t)(groups + 1) * 4);
     DASS_BOUNDS_COMMIT(bs, p.a.st);
+    if (x_codes && T > 32) return mx4_tc_launch(p, 256);
     const int64_t want = lin_rows_wanted(p.a), blocks = (N + 31) / 32 * lin_active_groups(p.a);
     const int nt = want <= 8 ? 1 : want <= 16 ? 2 : 4;
     int split = 1;
