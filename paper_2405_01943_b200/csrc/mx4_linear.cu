@@ -5,6 +5,7 @@ namespace dass {
 
 dass_status mx4_few_launch(const Mx4Args &p, int eights, int sixteens, int split);     // mx4_few.cu
 dass_status mx4_tc_launch(const Mx4Args &p, int columns);                              // mx4_tc.cu
+dass_status mx4_wide_launch(const Mx4Args &p, int rows);                               // mx4_wide.cu
 int device_sm_count();                                                                 // dass_abi.cu
 
 }  // namespace dass
@@ -57,6 +58,7 @@ dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, 
     DASS_BOUNDS_ADD(bs, offsets, (size_t)(groups + 1) * 4);
     DASS_BOUNDS_COMMIT(bs, p.a.st);
     if (x_codes && T > 32) return mx4_tc_launch(p, 256);
+    if (!x_codes && T > 64) return mx4_wide_launch(p, up_codes ? 128 : 256);
     const int64_t want = lin_rows_wanted(p.a), blocks = (N + 31) / 32 * lin_active_groups(p.a);
     const int nt = want <= 8 ? 1 : want <= 16 ? 2 : 4;
     int split = 1;

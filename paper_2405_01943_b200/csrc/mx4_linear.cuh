@@ -1,8 +1,10 @@
-// What the kernels of dass_linear_mx4 share: the arguments.  Internal header.
+// What the kernels of dass_linear_mx4 share: the arguments, the tensor maps, the walk of the persistent kernels over groups
+// of rows.  Internal header.
 #pragma once
 
 #include "linear_common.cuh"
 #include "mx4_common.cuh"
+#include "tc_common.cuh"
 
 namespace dass {
 
@@ -17,6 +19,102 @@ struct Mx4Args {
 __host__ __device__ __forceinline__ Mx4Matrix mx4_group(const Mx4Matrix &m, int64_t g, int64_t N, int64_t K)
 {
     return {m.codes + g * N * mx4_pitch(K), m.scales + g * ((N + MX4_TILE_ROWS - 1) / MX4_TILE_ROWS) * mx4_k_tiles(K) * MX4_TILE_BYTES};
+}
+
+// ------------------------------------------------------------------ the persistent kernels' walk
+// Every group's rows are cut into tiles by themselves, of ROWS rows from the multiple of ALIGN at or below the group's first
+// one.  The host does not know the offsets, so every CTA builds the prefix sums of the groups' tile counts once (in `table`:
+// first tiles, then first rows, then ends) and finds its items in them.  Inside a group the items run over MX4_BAND row
+// tiles before they step to the next columns, so that the CTAs at work at one time share a patch of tiles through L2.
+constexpr int MX4_BAND = 8;
+constexpr uint32_t MX4_TABLE_BYTES = (3 * LIN_MAX_GROUPS + 4) * 4;
+
+struct Mx4Item { int g; int row, row_lo, row_hi, col; };   // the tile's first row, the group's rows, the first column
+
+template <int ALIGN, int ROWS>
+__device__ __forceinline__ void mx4_count_tiles(int *table, const int32_t *offsets, int groups, int64_t T, int threads)
+{
+    for (int g = threadIdx.x; g < groups; g += threads) {
+        int64_t lo, hi;
+        lin_group_rows(offsets, g, T, lo, hi);
+        table[g + 1] = hi > lo ? (int)((hi - (lo & ~(int64_t)(ALIGN - 1)) + ROWS - 1) / ROWS) : 0;
+        table[LIN_MAX_GROUPS + 4 + g] = (int)lo;
+        table[2 * LIN_MAX_GROUPS + 4 + g] = (int)hi;
+    }
+}
+// Inclusive prefix sums over the groups, by one warp.
+__device__ __forceinline__ void mx4_sum_tiles(int *table, int groups)
+{
+    const int lane = threadIdx.x & 31;
+    int carry = 0;
+    for (int g0 = 0; g0 < groups; g0 += 32) {
+        int v = g0 + lane < groups ? table[g0 + lane + 1] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(FULL_MASK, v, o);
+            v += lane >= o ? up : 0;
+        }
+        v += carry;
+        if (g0 + lane < groups) table[g0 + lane + 1] = v;
+        carry = __shfl_sync(FULL_MASK, v, 31);
+    }
+    if (lane == 0) table[0] = 0;
+}
+// The idx-th item of the walk; false past the last one.
+template <int ALIGN, int ROWS>
+__device__ __forceinline__ bool mx4_item(const int *table, int groups, int col_tiles, int cols_per_tile, int64_t idx, Mx4Item &it)
+{
+    const int *lo = table + LIN_MAX_GROUPS + 4, *hi = lo + LIN_MAX_GROUPS;
+    if (idx >= (int64_t)table[groups] * col_tiles) return false;
+    int a = 0, b = groups;                                           // table[a] * col_tiles <= idx < table[b] * col_tiles
+    while (b - a > 1) {
+        const int m = (a + b) >> 1;
+        if ((int64_t)table[m] * col_tiles <= idx) a = m; else b = m;
+    }
+    const int tiles = table[a + 1] - table[a];
+    const int64_t rem = idx - (int64_t)table[a] * col_tiles;
+    const int band = (int)(rem / ((int64_t)MX4_BAND * col_tiles));
+    const int r2 = (int)(rem - (int64_t)band * MX4_BAND * col_tiles);
+    const int left = tiles - band * MX4_BAND;
+    const int nb = left < MX4_BAND ? left : MX4_BAND;
+    const int ct = r2 / nb;
+    it.g = a;
+    it.row_lo = lo[a];
+    it.row_hi = hi[a];
+    it.row = (lo[a] & ~(ALIGN - 1)) + (band * MX4_BAND + (r2 - ct * nb)) * ROWS;
+    it.col = ct * cols_per_tile;
+    return true;
+}
+
+// ------------------------------------------------------------------ tensor maps
+// `mats` matrices of codes [rows x pitch bytes], one after the other: boxes of 128 bytes x box_rows with the 128-byte swizzle;
+// rows past a matrix's end read as zero.
+inline bool mx4_codes_map(CUtensorMap *map, const void *codes, int64_t mats, int64_t rows, int64_t K, int box_rows)
+{
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const int64_t pitch = mx4_pitch(K);
+    const cuuint64_t dims[3] = {(cuuint64_t)pitch, (cuuint64_t)rows, (cuuint64_t)mats};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch, (cuuint64_t)(rows * pitch)};
+    const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(codes), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Scale tiles [tiles along the rows x tiles along k x 512 bytes]: boxes of two k tiles.
+inline bool mx4_scales_map(CUtensorMap *map, const void *scales, int64_t row_tiles, int64_t K)
+{
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const int64_t k_tiles = mx4_k_tiles(K);
+    const cuuint64_t dims[3] = {MX4_TILE_BYTES / 4, (cuuint64_t)k_tiles, (cuuint64_t)row_tiles};
+    const cuuint64_t strides[2] = {MX4_TILE_BYTES, (cuuint64_t)k_tiles * MX4_TILE_BYTES};
+    const cuuint32_t box[3] = {MX4_TILE_BYTES / 4, 2, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(scales), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace dass

@@ -15,9 +15,14 @@
 
 namespace dass {
 
-constexpr int MQ_THREADS = 128;
+constexpr int MQ_WARPS = 4;
+constexpr int MQ_THREADS = MQ_WARPS * 32;
 constexpr int MQ_ROWS = 4;           // rows of a warp
 constexpr int MQ_COLS = 256;         // columns of a warp
+
+// A block's warps lie side by side along the columns, or, where a row is shorter, over each other: `across` (1, 2 or 4) of
+// them side by side.  grid.x columns, grid.y rows, grid.z matrices; the last two wrap around.
+struct MqGrid { int across; int64_t row_groups, groups; };
 
 // Two floats to two codes each, four pairs: v[0] in the lowest bits.
 __device__ __forceinline__ uint32_t mx4_encode8(const float (&v)[8])
@@ -33,122 +38,163 @@ __device__ __forceinline__ uint32_t mx4_encode8(const float (&v)[8])
     return r;
 }
 
-// 8 values of a row from column c on; absent ones are zero.
+// 8 values of a lane as they lie in memory: 16-byte pieces where rows allow them; else single elements, 32 consecutive ones to
+// an access of the warp, that change lanes through shared memory (mq_turn).
+template <bool BF16, bool VECTOR> struct MqRaw { RowRaw<BF16, VECTOR ? ROW_VEC<BF16> : 1> piece[VECTOR ? 8 / ROW_VEC<BF16> : 8]; };
+
 template <bool BF16, bool VECTOR>
-__device__ __forceinline__ void mq_load8(const void *X, int64_t row, int64_t c, int64_t K, float (&v)[8])
+__device__ __forceinline__ void mq_load(MqRaw<BF16, VECTOR> &r, const void *X, int64_t row, int64_t c0, int lane, int64_t K)
 {
-    if (VECTOR && c + 8 <= K) {
-        if constexpr (BF16) {
-            row_load<true, 8>(X, row + c, v);
-        } else {
-            float a[4], b[4];
-            row_load<false, 4>(X, row + c, a);
-            row_load<false, 4>(X, row + c + 4, b);
+    constexpr int W = VECTOR ? ROW_VEC<BF16> : 1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    for (int i = 0; i < 8 / W; ++i) {
+        const int64_t c = VECTOR ? c0 + lane * 8 + i * W : c0 + i * 32 + lane;
+        if (c + W <= K) {
+            raw_load<BF16, W, true>(r.piece[i], X, row + c);
+        } else if constexpr (W == 1) {
+            r.piece[i].w = 0;
+        } else {                                                       // a row that ends inside the piece
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                if (c + j >= K) continue;
+                if constexpr (BF16) w[j / 2] |= (uint32_t)DASS_LD(static_cast<const uint16_t *>(X) + row + c + j) << (16 * (j & 1));
+                else w[j] = DASS_LD(static_cast<const uint32_t *>(X) + row + c + j);
+            }
+            r.piece[i].w = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        return;
     }
+}
+// The lane's 8 consecutive values.
+template <bool BF16, bool VECTOR>
+__device__ __forceinline__ void mq_floats(const MqRaw<BF16, VECTOR> &r, float *turn, int lane, float (&v)[8])
+{
+    constexpr int W = VECTOR ? ROW_VEC<BF16> : 1;
+    if constexpr (VECTOR) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float x[1] = {0.f};
-        if (c + i < K) row_load<BF16, 1>(X, row + c + i, x);
-        v[i] = x[0];
+        for (int i = 0; i < 8 / W; ++i) {
+            float x[W];
+            raw_floats<BF16, W>(r.piece[i], x);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[i * W + j] = x[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x[1];
+            raw_floats<BF16, 1>(r.piece[i], x);
+            turn[i * 32 + lane] = x[0];
+        }
+        __syncwarp();
+        const float4 a = *reinterpret_cast<const float4 *>(turn + lane * 8), b = *reinterpret_cast<const float4 *>(turn + lane * 8 + 4);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        __syncwarp();
     }
 }
 
 template <bool BF16, bool VECTOR>
 __global__ void __launch_bounds__(MQ_THREADS)
 mx4_quantize_kernel(const void *__restrict__ X, int64_t rows, int64_t K, int64_t ldx, int64_t group_stride,
-                    uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int col_chunks, int64_t row_chunks, int64_t chunks)
+                    uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, const MqGrid q)
 {
-    const int64_t chunk = (int64_t)blockIdx.x * (MQ_THREADS / 32) + (threadIdx.x >> 5);
-    if (chunk >= chunks) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t across = chunk / col_chunks;
-    const int64_t g = across / row_chunks, r0 = (across - g * row_chunks) * MQ_ROWS;
-    const int64_t c = (chunk - across * col_chunks) * MQ_COLS + lane * 8;
+    __shared__ float turn[VECTOR ? 1 : MQ_WARPS][VECTOR ? 4 : MQ_COLS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t c0 = ((int64_t)blockIdx.x * q.across + (warp & (q.across - 1))) * MQ_COLS, c = c0 + lane * 8;
     const int64_t pitch = mx4_pitch(K), k_tiles = mx4_k_tiles(K);
-    uint8_t *const gcodes = codes + g * rows * pitch;
-    uint8_t *const gscales = scales + g * mx4_row_tiles(rows) * k_tiles * MX4_TILE_BYTES;
-    float v[MQ_ROWS][8];
+    const int64_t first = (int64_t)blockIdx.y * (MQ_WARPS / q.across) + warp / q.across;
+    for (int64_t g = blockIdx.z; g < q.groups; g += gridDim.z)
+        for (int64_t rg = first; rg < q.row_groups; rg += (int64_t)gridDim.y * (MQ_WARPS / q.across)) {
+            const int64_t r0 = rg * MQ_ROWS;
+            uint8_t *const gcodes = codes + (g * rows + r0) * pitch + c / 2;
+            uint8_t *const gscales = scales + g * mx4_row_tiles(rows) * k_tiles * MX4_TILE_BYTES + mx4_scale_word(r0, c / MX4_TILE_K, k_tiles);
+            MqRaw<BF16, VECTOR> raw[MQ_ROWS];
 #pragma unroll
-    for (int i = 0; i < MQ_ROWS; ++i) {
-        if (r0 + i < rows) {
-            mq_load8<BF16, VECTOR>(X, g * group_stride + (r0 + i) * ldx, c, K, v[i]);
-        } else {
+            for (int i = 0; i < MQ_ROWS; ++i)
+                mq_load<BF16, VECTOR>(raw[i], X, g * group_stride + (r0 + i) * ldx, c0, lane, r0 + i < rows ? K : 0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            for (int i = 0; i < MQ_ROWS; ++i) {
+                float v[8];
+                mq_floats<BF16, VECTOR>(raw[i], turn[VECTOR ? 0 : warp], lane, v);
+                uint32_t most = 0u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
+                most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
+                most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
+                const uint32_t e = most >> 23;
+                const uint32_t s = e == 255u ? 255u : e > 2u ? e - 2u : 0u;
+                const float up = __uint_as_float((254u - s) << 23);
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = v[j] * up;
+                const uint32_t packed = e == 255u ? 0u : mx4_encode8(y);
+                if (r0 + i < rows && c < pitch * 2) DASS_ST_CS(reinterpret_cast<uint32_t *>(gcodes + i * pitch), packed);
+                uint32_t word = s << (8 * ((lane >> 2) & 3));
+                word |= __shfl_xor_sync(FULL_MASK, word, 4);
+                word |= __shfl_xor_sync(FULL_MASK, word, 8);
+                if ((lane & 15) == 0 && c < k_tiles * MX4_TILE_K) DASS_ST(reinterpret_cast<uint32_t *>(gscales + i * 16), word);   // the four rows' slots are neighbours
+            }
         }
-    }
-#pragma unroll
-    for (int i = 0; i < MQ_ROWS; ++i) {
-        const int64_t r = r0 + i;
-        uint32_t most = 0u;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[i][j]) & 0x7fffffffu);
-        most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
-        most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
-        const uint32_t e = most >> 23;
-        const uint32_t s = e == 255u ? 255u : e > 2u ? e - 2u : 0u;
-        const float up = s == 255u ? 0.f : __uint_as_float((254u - s) << 23);
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = s == 255u ? 0.f : v[i][j] * up;
-        const uint32_t packed = mx4_encode8(y);
-        if (r < rows && c < pitch * 2) DASS_ST(reinterpret_cast<uint32_t *>(gcodes + r * pitch + c / 2), packed);
-        uint32_t word = s << (8 * ((lane >> 2) & 3));
-        word |= __shfl_xor_sync(FULL_MASK, word, 4);
-        word |= __shfl_xor_sync(FULL_MASK, word, 8);
-        if ((lane & 15) == 0 && c < k_tiles * MX4_TILE_K)
-            DASS_ST(reinterpret_cast<uint32_t *>(gscales + mx4_scale_word(r, c / MX4_TILE_K, k_tiles)), word);
-    }
 }
 
 template <bool BF16, bool VECTOR>
 __global__ void __launch_bounds__(MQ_THREADS)
 mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int64_t K,
-                      void *__restrict__ Y, int64_t ldy, int64_t group_stride, int col_chunks, int64_t row_chunks, int64_t chunks)
+                      void *__restrict__ Y, int64_t ldy, int64_t group_stride, const MqGrid q)
 {
-    const int64_t chunk = (int64_t)blockIdx.x * (MQ_THREADS / 32) + (threadIdx.x >> 5);
-    if (chunk >= chunks) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t across = chunk / col_chunks;
-    const int64_t g = across / row_chunks, r0 = (across - g * row_chunks) * MQ_ROWS;
-    const int64_t c = (chunk - across * col_chunks) * MQ_COLS + lane * 8;
+    __shared__ float turn[VECTOR ? 1 : MQ_WARPS][VECTOR ? 4 : MQ_COLS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t c0 = ((int64_t)blockIdx.x * q.across + (warp & (q.across - 1))) * MQ_COLS, c = c0 + lane * 8;
     const int64_t pitch = mx4_pitch(K), k_tiles = mx4_k_tiles(K);
-    const uint8_t *const gcodes = codes + g * rows * pitch;
-    const uint8_t *const gscales = scales + g * mx4_row_tiles(rows) * k_tiles * MX4_TILE_BYTES;
-    if (c >= K) return;
-    uint32_t x[MQ_ROWS], s[MQ_ROWS];
+    const int64_t first = (int64_t)blockIdx.y * (MQ_WARPS / q.across) + warp / q.across;
+    for (int64_t g = blockIdx.z; g < q.groups; g += gridDim.z)
+        for (int64_t rg = first; rg < q.row_groups; rg += (int64_t)gridDim.y * (MQ_WARPS / q.across)) {
+            const int64_t r0 = rg * MQ_ROWS;
+            const uint8_t *const gcodes = codes + (g * rows + r0) * pitch + c / 2;
+            const uint8_t *const gscales = scales + g * mx4_row_tiles(rows) * k_tiles * MX4_TILE_BYTES + mx4_scale_word(r0, c / MX4_TILE_K, k_tiles) +
+                                           ((c / MX4_BLOCK) & 3);
+            uint32_t x[MQ_ROWS], s[MQ_ROWS];
 #pragma unroll
-    for (int i = 0; i < MQ_ROWS; ++i) {
-        const int64_t r = r0 + i;
-        x[i] = r < rows ? DASS_LD_CS(reinterpret_cast<const uint32_t *>(gcodes + r * pitch + c / 2)) : 0u;
-        s[i] = r < rows ? DASS_LD(gscales + mx4_scale_word(r, c / MX4_TILE_K, k_tiles) + ((c / MX4_BLOCK) & 3)) : 0u;
-    }
-#pragma unroll
-    for (int i = 0; i < MQ_ROWS; ++i) {
-        const int64_t r = r0 + i, at = g * group_stride + r * ldy + c;
-        if (r >= rows) break;
-        float v[8];
-        mx4_decode8_f32(x[i], mx4_scale(s[i]), v);
-        if (VECTOR && c + 8 <= K) {
-            if constexpr (BF16) {
-                row_store<true, 8>(Y, at, v);
-            } else {
-                const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-                row_store<false, 4>(Y, at, a);
-                row_store<false, 4>(Y, at + 4, b);
+            for (int i = 0; i < MQ_ROWS; ++i) {
+                const bool in = r0 + i < rows && c < K;
+                x[i] = in ? DASS_LD_CS(reinterpret_cast<const uint32_t *>(gcodes + i * pitch)) : 0u;
+                s[i] = in ? DASS_LD(gscales + i * 16) : 0u;
             }
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float one[1] = {v[j]};
-                if (c + j < K) row_store<BF16, 1>(Y, at + j, one);
+            for (int i = 0; i < MQ_ROWS; ++i) {
+                if (r0 + i >= rows) break;
+                const int64_t at = g * group_stride + (r0 + i) * ldy;
+                float v[8];
+                mx4_decode8_f32(x[i], mx4_scale(s[i]), v);
+                if constexpr (VECTOR) {
+                    if (c + 8 <= K) {
+                        if constexpr (BF16) {
+                            row_store<true, 8>(Y, at + c, v);
+                        } else {
+                            const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+                            row_store<false, 4>(Y, at + c, a);
+                            row_store<false, 4>(Y, at + c + 4, b);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float one[1] = {v[j]};
+                            if (c + j < K) row_store<BF16, 1>(Y, at + c + j, one);
+                        }
+                    }
+                } else {
+                    float *const mine = turn[warp];
+                    *reinterpret_cast<float4 *>(mine + lane * 8) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4 *>(mine + lane * 8 + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float one[1] = {mine[j * 32 + lane]};
+                        if (c0 + j * 32 + lane < K) row_store<BF16, 1>(Y, at + c0 + j * 32 + lane, one);
+                    }
+                    __syncwarp();
+                }
             }
         }
-    }
 }
 
 static dass_status mq_check(int64_t groups, int64_t rows, int64_t K, int64_t ld, int64_t group_stride, int dt)
@@ -156,20 +202,18 @@ static dass_status mq_check(int64_t groups, int64_t rows, int64_t K, int64_t ld,
     if (dt != DASS_BF16 && dt != DASS_F32) return DASS_ERR_DTYPE;
     if (groups < 1 || rows < 0 || K < 1 || ld < K || (groups > 1 && rows > 0 && group_stride < (rows - 1) * ld + K)) return DASS_ERR_SHAPE;
     const int64_t lim = 0x7fffffffll - 512;
-    if (rows > lim || K > lim || groups > lim) return DASS_ERR_UNSUPPORTED;
+    if (rows > lim || K > lim || groups > lim || rows > (1ll << 48) / K / groups) return DASS_ERR_UNSUPPORTED;   // more than any memory holds
     return DASS_OK;
 }
 
-struct MqGrid { int col_chunks; int64_t row_chunks, chunks; unsigned blocks; };
-// False where there are more warps than a grid holds.
-static bool mq_grid(int64_t groups, int64_t padded_rows, int64_t K, MqGrid &q)
+static dim3 mq_grid(int64_t groups, int64_t padded_rows, int64_t K, MqGrid &q)
 {
-    q.col_chunks = (int)((K + MQ_COLS - 1) / MQ_COLS);
-    q.row_chunks = (padded_rows + MQ_ROWS - 1) / MQ_ROWS;
-    if (q.row_chunks > (int64_t)0x7fffffff * (MQ_THREADS / 32) / q.col_chunks / groups) return false;
-    q.chunks = groups * q.row_chunks * q.col_chunks;
-    q.blocks = (unsigned)((q.chunks + MQ_THREADS / 32 - 1) / (MQ_THREADS / 32));
-    return true;
+    const int64_t chunks = (K + MQ_COLS - 1) / MQ_COLS;
+    q.across = chunks >= 4 ? 4 : chunks >= 2 ? 2 : 1;
+    q.row_groups = (padded_rows + MQ_ROWS - 1) / MQ_ROWS;
+    q.groups = groups;
+    const int64_t y = (q.row_groups + MQ_WARPS / q.across - 1) / (MQ_WARPS / q.across);
+    return dim3((unsigned)((chunks + q.across - 1) / q.across), (unsigned)(y < 65535 ? y : 65535), (unsigned)(groups < 65535 ? groups : 65535));
 }
 
 }  // namespace dass
@@ -199,7 +243,7 @@ dass_status dass_mx4_quantize(const void *X, int64_t groups, int64_t rows, int64
     if (!elem_aligned(X, bf16) || (reinterpret_cast<uintptr_t>(codes) & 15u) || (reinterpret_cast<uintptr_t>(scales) & 15u)) return DASS_ERR_ALIGN;
     if (rows == 0) return DASS_OK;
     MqGrid q;
-    if (!mq_grid(groups, mx4_row_tiles(rows) * MX4_TILE_ROWS, K, q)) return DASS_ERR_UNSUPPORTED;
+    const dim3 grid = mq_grid(groups, mx4_row_tiles(rows) * MX4_TILE_ROWS, K, q);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const int64_t stride = groups > 1 ? group_stride : 0;
     DASS_BOUNDS_SCOPE(bs);
@@ -208,7 +252,7 @@ dass_status dass_mx4_quantize(const void *X, int64_t groups, int64_t rows, int64
     DASS_BOUNDS_ADD(bs, scales, (size_t)groups * mx4_scales_bytes(rows, K));
     DASS_BOUNDS_COMMIT(bs, st);
     const bool vec = rows_vec_ok(X, ldx, bf16) && (groups == 1 || stride % (bf16 ? 8 : 4) == 0);
-    auto go = [&](auto kernel) { kernel<<<q.blocks, MQ_THREADS, 0, st>>>(X, rows, K, ldx, stride, codes, scales, q.col_chunks, q.row_chunks, q.chunks); };
+    auto go = [&](auto kernel) { kernel<<<grid, MQ_THREADS, 0, st>>>(X, rows, K, ldx, stride, codes, scales, q); };
     if (bf16) vec ? go(mx4_quantize_kernel<true, true>) : go(mx4_quantize_kernel<true, false>);
     else vec ? go(mx4_quantize_kernel<false, true>) : go(mx4_quantize_kernel<false, false>);
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;
@@ -224,7 +268,7 @@ dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int
     if (!elem_aligned(Y, bf16) || (reinterpret_cast<uintptr_t>(codes) & 15u) || (reinterpret_cast<uintptr_t>(scales) & 15u)) return DASS_ERR_ALIGN;
     if (rows == 0) return DASS_OK;
     MqGrid q;
-    if (!mq_grid(groups, rows, K, q)) return DASS_ERR_UNSUPPORTED;
+    const dim3 grid = mq_grid(groups, rows, K, q);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const int64_t stride = groups > 1 ? group_stride : 0;
     DASS_BOUNDS_SCOPE(bs);
@@ -233,7 +277,7 @@ dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int
     DASS_BOUNDS_ADD(bs, scales, (size_t)groups * mx4_scales_bytes(rows, K));
     DASS_BOUNDS_COMMIT(bs, st);
     const bool vec = rows_vec_ok(Y, ldy, bf16) && (groups == 1 || stride % (bf16 ? 8 : 4) == 0);
-    auto go = [&](auto kernel) { kernel<<<q.blocks, MQ_THREADS, 0, st>>>(codes, scales, rows, K, Y, ldy, stride, q.col_chunks, q.row_chunks, q.chunks); };
+    auto go = [&](auto kernel) { kernel<<<grid, MQ_THREADS, 0, st>>>(codes, scales, rows, K, Y, ldy, stride, q); };
     if (bf16) vec ? go(mx4_dequantize_kernel<true, true>) : go(mx4_dequantize_kernel<true, false>);
     else vec ? go(mx4_dequantize_kernel<false, true>) : go(mx4_dequantize_kernel<false, false>);
     return cudaGetLastError() == cudaSuccess ? DASS_OK : DASS_ERR_CUDA;

@@ -27,11 +27,9 @@ constexpr int MT_BM = 128;          // rows per CTA
 constexpr int MT_BK = 256;          // k per stage: one 128-byte swizzle row of codes, two scale tiles
 constexpr int MT_EPI_WARPS = 8;     // two to a quarter of the TMEM lanes, each with half of the columns
 constexpr int MT_THREADS = 64 + 32 * MT_EPI_WARPS;
-constexpr int MT_BAND = 8;          // row tiles that are walked before the next columns
 constexpr uint32_t MT_ROW_BYTES = MT_BK / 2;
 constexpr uint32_t MT_A_BYTES = MT_BM * MT_ROW_BYTES;
 constexpr uint32_t MT_SCALES = 2 * MX4_TILE_BYTES;                   // 128 rows' scales of a stage
-constexpr uint32_t MT_TABLE_BYTES = (3 * LIN_MAX_GROUPS + 4) * 4;   // a group's first tile, first row and end
 constexpr int MT_TURN_PITCH = 20;                                     // words from row to row of 32 bf16
 constexpr uint32_t MT_TURN_BYTES = MT_EPI_WARPS * 32 * MT_TURN_PITCH * 4;
 constexpr uint32_t MT_SF_COL = 256;                                   // TMEM columns from here on hold scales
@@ -41,7 +39,7 @@ template <int BN> struct MtShape {  // BN: accumulator columns; each CTA of the 
     static constexpr int STAGES = BN == 256 ? 5 : 6;
     static constexpr int ACCS = 256 / BN;                             // accumulators
     static constexpr uint32_t SF_COLS = 8 + BN / 16;                  // TMEM columns of a stage's scales
-    static constexpr uint32_t BYTES = STAGES * STAGE + 1024 /* alignment slack */ + 256 /* barriers */ + MT_TABLE_BYTES + MT_TURN_BYTES;
+    static constexpr uint32_t BYTES = STAGES * STAGE + 1024 /* alignment slack */ + 256 /* barriers */ + MX4_TABLE_BYTES + MT_TURN_BYTES;
     static_assert(BYTES <= 227 * 1024 && MT_SF_COL + STAGES * SF_COLS <= 512 && STAGE % 1024 == 0, "");
 };
 
@@ -55,8 +53,6 @@ struct MtParams {
     int y_vec, r_vec;               // whole 16-byte accesses
     int *timeouts;
 };
-
-struct MtItem { int g; int row, row_lo, row_hi, col; };
 
 // ------------------------------------------------------------------ PTX wrappers
 // Descriptor of 32 rows of 16 bytes, one after the other, for tcgen05.cp: 8-row groups 128 bytes apart, no swizzle.
@@ -81,31 +77,6 @@ __device__ __forceinline__ void umma_mxf4_pair(uint32_t d_tmem, uint64_t adesc, 
                  "setp.ne.b32 p, %4, 0;\n\t"
                  "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
                  ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
-}
-
-// The idx-th item of the grid's walk; false past the last one.
-__device__ __forceinline__ bool mt_item(const MtParams &p, const int *first_tile, int64_t idx, MtItem &it)
-{
-    const int *lo = first_tile + LIN_MAX_GROUPS + 4, *hi = lo + LIN_MAX_GROUPS;
-    if (idx >= (int64_t)first_tile[p.groups] * p.col_tiles) return false;
-    int a = 0, b = p.groups;                                         // first_tile[a] * col_tiles <= idx < first_tile[b] * col_tiles
-    while (b - a > 1) {
-        const int m = (a + b) >> 1;
-        if ((int64_t)first_tile[m] * p.col_tiles <= idx) a = m; else b = m;
-    }
-    const int tiles = first_tile[a + 1] - first_tile[a];
-    const int64_t rem = idx - (int64_t)first_tile[a] * p.col_tiles;
-    const int band = (int)(rem / ((int64_t)MT_BAND * p.col_tiles));
-    const int r2 = (int)(rem - (int64_t)band * MT_BAND * p.col_tiles);
-    const int left = tiles - band * MT_BAND;
-    const int nb = left < MT_BAND ? left : MT_BAND;
-    const int ct = r2 / nb;
-    it.g = a;
-    it.row_lo = lo[a];
-    it.row_hi = hi[a];
-    it.row = (lo[a] & ~(MT_BM - 1)) + (band * MT_BAND + (r2 - ct * nb)) * 2 * MT_BM;
-    it.col = ct * p.cols_per_tile;
-    return true;
 }
 
 // A column's bias for the lanes of a warp: lane l holds column n + l.
@@ -154,35 +125,14 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    for (int g = threadIdx.x; g < p.groups; g += MT_THREADS) {
-        int64_t lo, hi;
-        lin_group_rows(p.offsets, g, p.T, lo, hi);
-        const int64_t from = lo & ~(int64_t)(MT_BM - 1);
-        first_tile[g + 1] = hi > lo ? (int)((hi - from + 2 * MT_BM - 1) / (2 * MT_BM)) : 0;
-        first_tile[LIN_MAX_GROUPS + 4 + g] = (int)lo;
-        first_tile[2 * LIN_MAX_GROUPS + 4 + g] = (int)hi;
-    }
+    mx4_count_tiles<MT_BM, 2 * MT_BM>(first_tile, p.offsets, p.groups, p.T, MT_THREADS);
     if (warp == 1) {
         tmem_alloc_pair(smem_u32(tmem_slot), 512);
         tmem_relinquish_pair();
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 0) {                                              // inclusive prefix sums over the groups
-        int carry = 0;
-        for (int g0 = 0; g0 < p.groups; g0 += 32) {
-            int v = g0 + lane < p.groups ? first_tile[g0 + lane + 1] : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int up = __shfl_up_sync(FULL_MASK, v, o);
-                v += lane >= o ? up : 0;
-            }
-            v += carry;
-            if (g0 + lane < p.groups) first_tile[g0 + lane + 1] = v;
-            carry = __shfl_sync(FULL_MASK, v, 31);
-        }
-        if (lane == 0) first_tile[0] = 0;
-    }
+    if (warp == 0) mx4_sum_tiles(first_tile, p.groups);
     __syncthreads();
     cluster_sync_all();            // both CTAs' barriers are initialised and both TMEM allocations exist
     tc_fence_after();
@@ -196,8 +146,8 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         const uint32_t leader_full = map_to_cta(bar_full, 0);
         const uint64_t pol = l2_policy_evict_last();
         const CUtensorMap *map_b = GLU && rank ? &map_up : &map_w;
-        MtItem it;
-        for (int64_t idx = pair; ok && mt_item(p, first_tile, idx, it); idx += pairs) {
+        Mx4Item it;
+        for (int64_t idx = pair; ok && mx4_item<MT_BM, 2 * MT_BM>(first_tile, p.groups, p.col_tiles, p.cols_per_tile, idx, it); idx += pairs) {
             const int a_row = it.row + (int)rank * MT_BM;
             const int b_row = it.col + (GLU ? 0 : (int)rank * (BN / 2));
             const int a_tile = a_row / MX4_TILE_ROWS < p.x_tiles ? a_row / MX4_TILE_ROWS : p.x_tiles - 1;      // absent rows are not stored
@@ -209,7 +159,7 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 const uint32_t fb = leader_full + 8 * stage;
                 if (elect_one()) {
                     if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * stage, 2 * S::STAGE);   // both CTAs' bytes
-                    tma_load_2d_pair(sbase, &map_x, fb, kb * (int)MT_ROW_BYTES, a_row, pol);
+                    tma_load_3d_pair(sbase, &map_x, fb, kb * (int)MT_ROW_BYTES, a_row, 0, pol);
                     tma_load_3d_pair(sbase + MT_A_BYTES, map_b, fb, kb * (int)MT_ROW_BYTES, b_row, it.g, pol);
                     tma_load_3d_pair(scales, &map_xs, fb, 0, kb * 2, a_tile, pol);
                     tma_load_3d_pair(scales + MT_SCALES, &map_ws, fb, 0, kb * 2, w_tile, pol);
@@ -272,13 +222,13 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
         const uint32_t leader_acc_empty = map_to_cta(bar_acc_empty, 0);
         // Blocks of 32 rows x 32 columns are turned through shared memory, so that an access moves runs of a row (linear_tc.cu).
-        uint32_t *turn = reinterpret_cast<uint32_t *>(first_tile) + MT_TABLE_BYTES / 4 + (warp - 2) * 32 * MT_TURN_PITCH;
+        uint32_t *turn = reinterpret_cast<uint32_t *>(first_tile) + MX4_TABLE_BYTES / 4 + (warp - 2) * 32 * MT_TURN_PITCH;
         uint16_t *turn16 = reinterpret_cast<uint16_t *>(turn);
         const int vr = lane >> 2, vc = (lane & 3) * 8;           // this lane's row and column in an access of 8 rows
         uint32_t tile = 0;
         bool ok = true;
-        MtItem it;
-        for (int64_t idx = pair; ok && mt_item(p, first_tile, idx, it); idx += pairs, ++tile) {
+        Mx4Item it;
+        for (int64_t idx = pair; ok && mx4_item<MT_BM, 2 * MT_BM>(first_tile, p.groups, p.col_tiles, p.cols_per_tile, idx, it); idx += pairs, ++tile) {
             const uint32_t as = tile % S::ACCS;
             const int64_t t0 = (int64_t)it.row + rank * MT_BM + quad * 32;                  // the warp's first row
             const int r_lo = it.row_lo > t0 ? (int)(it.row_lo - t0 < 32 ? it.row_lo - t0 : 32) : 0;
@@ -395,36 +345,6 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 int device_sm_count();                                                                                       // dass_abi.cu
 int *linear_timeouts();                                                                                      // linear.cu
 
-// `mats` matrices of codes [rows x pitch bytes], one after the other: boxes of 128 bytes x box_rows with the 128-byte swizzle;
-// rows past a matrix's end read as zero.
-static bool mx4_codes_map(CUtensorMap *map, const void *codes, int64_t mats, int64_t rows, int64_t K, int box_rows, bool flat)
-{
-    const EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const int64_t pitch = mx4_pitch(K);
-    const cuuint64_t dims[3] = {(cuuint64_t)pitch, (cuuint64_t)rows, (cuuint64_t)mats};
-    const cuuint64_t strides[2] = {(cuuint64_t)pitch, (cuuint64_t)(rows * pitch)};
-    const cuuint32_t box[3] = {MT_ROW_BYTES, (cuuint32_t)box_rows, 1};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, flat ? 2 : 3, const_cast<void *>(codes), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// Scale tiles [tiles along the rows x tiles along k x 512 bytes]: boxes of two k tiles.
-static bool mx4_scales_map(CUtensorMap *map, const void *scales, int64_t row_tiles, int64_t K)
-{
-    const EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const int64_t k_tiles = mx4_k_tiles(K);
-    const cuuint64_t dims[3] = {MX4_TILE_BYTES / 4, (cuuint64_t)k_tiles, (cuuint64_t)row_tiles};
-    const cuuint64_t strides[2] = {MX4_TILE_BYTES, (cuuint64_t)k_tiles * MX4_TILE_BYTES};
-    const cuuint32_t box[3] = {MX4_TILE_BYTES / 4, 2, 1};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(scales), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 struct MtMaps { CUtensorMap x, w, up, xs, ws, us; };
 
 template <int BN, bool GLU, int ACT>
@@ -455,8 +375,8 @@ dass_status mx4_tc_launch(const Mx4Args &q, int bn)
     const int64_t w_tiles = mx4_row_tiles(a.N);
     const Mx4Matrix &second = glu ? q.up : q.w;
     MtMaps m;
-    if (!mx4_codes_map(&m.x, q.x.codes, 1, a.T, a.K, MT_BM, true) || !mx4_codes_map(&m.w, q.w.codes, a.groups, a.N, a.K, bn / 2, false) ||
-        !mx4_codes_map(&m.up, second.codes, a.groups, a.N, a.K, bn / 2, false) || !mx4_scales_map(&m.xs, q.x.scales, mx4_row_tiles(a.T), a.K) ||
+    if (!mx4_codes_map(&m.x, q.x.codes, 1, a.T, a.K, MT_BM) || !mx4_codes_map(&m.w, q.w.codes, a.groups, a.N, a.K, bn / 2) ||
+        !mx4_codes_map(&m.up, second.codes, a.groups, a.N, a.K, bn / 2) || !mx4_scales_map(&m.xs, q.x.scales, mx4_row_tiles(a.T), a.K) ||
         !mx4_scales_map(&m.ws, q.w.scales, a.groups * w_tiles, a.K) || !mx4_scales_map(&m.us, second.scales, a.groups * w_tiles, a.K))
         return DASS_ERR_CUDA;
     MtParams p;

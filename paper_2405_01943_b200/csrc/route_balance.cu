@@ -9,13 +9,15 @@
 // second kernel adds the rows in a fixed order.  Small calls are one block and one launch.  Choices are counted in shared
 // memory; integer sums do not depend on their order.
 #include "rows_common.cuh"
+#include "tc_common.cuh"
 
 namespace dass {
 
-constexpr int RB_THREADS = 256;
+constexpr int RB_THREADS = 512;            // of the loss
+constexpr int RB_BACK_THREADS = 256;       // of the gradient
 constexpr int RB_MAX_E = 1024;
 constexpr int RB_MAX_K = 32;
-constexpr int RB_BLOCKS = 592;             // partial rows at most: four blocks to each of 148 SMs
+constexpr int RB_BLOCKS = 296;             // partial rows at most: two blocks to each of 148 SMs
 constexpr int RB_ONE_BLOCK = 1 << 14;      // logits that one block takes alone
 
 // -inf and NaN are masked; +inf counts as the largest finite value.
@@ -37,26 +39,43 @@ template <int L> __device__ __forceinline__ float rb_sum(float v)
 // The column of a lane's element i * W + c.
 template <int L, int W> __device__ __forceinline__ int rb_col(int gl, int i) { return (i * L + gl) * W; }
 
-// A row of masked logits; absent columns are -inf.
+// A row as it lies in memory, all of its loads in flight before the first is used; absent columns hold bits that
+// rb_floats does not look at.
+template <bool BF16, int W, int V> struct RbRow { RowRaw<BF16, W> piece[V / W]; RowRaw<BF16, 1> tail[W > 1 ? W : 1]; };
+
 template <bool BF16, int W, int V, int L>
-__device__ __forceinline__ void rb_load(const void *logits, int64_t row, int gl, int E, float (&x)[V])
+__device__ __forceinline__ void rb_load(RbRow<BF16, W, V> &r, const void *logits, int64_t row, int gl, int E)
 {
 #pragma unroll
     for (int i = 0; i < V / W; ++i) {
         const int e = rb_col<L, W>(gl, i);
-        if (e + W <= E) {
-            float v[W];
-            row_load<BF16, W>(logits, row + e, v);
+        if (e + W <= E) raw_load<BF16, W>(r.piece[i], logits, row + e);
+        else if (W > 1 && e < E) {                                     // the one ragged piece of the row
 #pragma unroll
-            for (int c = 0; c < W; ++c) x[i * W + c] = rb_logit(v[c]);
-        } else {
+            for (int c = 0; c < W; ++c)
+                if (e + c < E) raw_load<BF16, 1>(r.tail[W > 1 ? c : 0], logits, row + e + c);
+        }
+    }
+}
+// The row's masked logits; absent columns are -inf.
+template <bool BF16, int W, int V, int L>
+__device__ __forceinline__ void rb_floats(const RbRow<BF16, W, V> &r, int gl, int E, float (&x)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V / W; ++i) {
+        const int e = rb_col<L, W>(gl, i);
+        float v[W];
+        raw_floats<BF16, W>(r.piece[i], v);
+        if (W > 1 && e < E && e + W > E) {
 #pragma unroll
             for (int c = 0; c < W; ++c) {
-                float v[1] = {-INFINITY};
-                if (e + c < E) row_load<BF16, 1>(logits, row + e + c, v);
-                x[i * W + c] = rb_logit(v[0]);
+                float one[1];
+                raw_floats<BF16, 1>(r.tail[W > 1 ? c : 0], one);
+                v[c] = one[0];
             }
         }
+#pragma unroll
+        for (int c = 0; c < W; ++c) x[i * W + c] = e + c < E ? rb_logit(v[c]) : -INFINITY;
     }
 }
 
@@ -78,18 +97,29 @@ __device__ __forceinline__ float rb_softmax(float (&x)[V])
     return sum > 0.f ? 1.0f / sum : 0.f;
 }
 
+// A lane's choices of a token: j = gl, gl + L, ...
+template <int L> constexpr int RB_IDS = L >= 8 ? RB_MAX_K / L : 4;     // held in registers; the others (of few lanes' tokens) are read when they are looked at
+template <int L>
+__device__ __forceinline__ void rb_load_ids(int (&id)[RB_IDS<L>], const int32_t *expert, int64_t t, int k, int gl, bool live)
+{
+#pragma unroll
+    for (int i = 0; i < RB_IDS<L>; ++i) id[i] = live && gl + i * L < k ? DASS_LD(expert + t * k + gl + i * L) : -1;
+}
 // Whether the token has a choice inside [0, E), for all lanes of its group; COUNT: the choices are counted too.
 template <int L, bool COUNT>
-__device__ __forceinline__ bool rb_chosen(const int32_t *expert, int64_t t, int k, int E, int gl, bool live, int *count)
+__device__ __forceinline__ bool rb_chosen(const int (&id)[RB_IDS<L>], const int32_t *expert, int64_t t, int k, int E, int gl, bool live, int *count)
 {
     int any = 0;
-    for (int j = gl; j < k; j += L) {
-        const int id = live ? DASS_LD(expert + t * k + j) : -1;
-        if (id >= 0 && id < E) {
+    auto look = [&](int e) {
+        if (e >= 0 && e < E) {
             any = 1;
-            if (COUNT) atomicAdd(count + id, 1);
+            if (COUNT) atomicAdd(count + e, 1);
         }
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < RB_IDS<L>; ++i) look(id[i]);
+    if (live)
+        for (int j = gl + RB_IDS<L> * L; j < k; j += L) look(DASS_LD(expert + t * k + j));
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) any |= __shfl_xor_sync(FULL_MASK, any, o);
     return any != 0;
@@ -137,12 +167,25 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
     int seen = 0;
     const int64_t rounds = (T + TOKENS - 1) / TOKENS;               // every lane takes part in every round of its warp
+    RbRow<BF16, W, V> next;
+    int next_id[RB_IDS<L>];
+    auto fetch = [&](int64_t r) {                                   // the next round's loads run under this one's arithmetic
+        const int64_t t = r * TOKENS + threadIdx.x / L;
+        const bool live = r < rounds && t < T;
+        rb_load<BF16, W, V, L>(next, logits, (live ? t : 0) * ld, gl, live ? E : 0);
+        rb_load_ids<L>(next_id, expert, t, k, gl, live);
+    };
+    fetch(blockIdx.x);
     for (int64_t r = blockIdx.x; r < rounds; r += gridDim.x) {
         const int64_t t = r * TOKENS + threadIdx.x / L;
         const bool live = t < T;
         float x[V];
-        rb_load<BF16, W, V, L>(logits, (live ? t : 0) * ld, gl, live ? E : 0, x);
-        const bool in = rb_chosen<L, true>(expert, t, k, E, gl, live, count);
+        int id[RB_IDS<L>];
+        rb_floats<BF16, W, V, L>(next, gl, live ? E : 0, x);
+#pragma unroll
+        for (int i = 0; i < RB_IDS<L>; ++i) id[i] = next_id[i];
+        fetch(r + gridDim.x);
+        const bool in = rb_chosen<L, true>(id, expert, t, k, E, gl, live, count);
         const float inv = rb_softmax<V, L>(x) * (in ? 1.f : 0.f);
         seen += in && gl == 0;
 #pragma unroll
@@ -192,7 +235,7 @@ route_balance_finish_kernel(const float *__restrict__ partial, const int32_t *__
     if (d < deep) {
         float s = 0.f;
         int c = 0, n = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (int r = d; r < rows; r += deep) {
             s += DASS_LD(partial + (int64_t)r * E + e);
             c += DASS_LD(partial_counts + (int64_t)r * (E + 1) + e);
@@ -214,12 +257,12 @@ route_balance_finish_kernel(const float *__restrict__ partial, const int32_t *__
 
 // dlogits = add + dloss * E/n p (f - sum f p); 0 + add for tokens without a choice.
 template <bool BF16, int W, int V, int L>
-__global__ void __launch_bounds__(RB_THREADS)
+__global__ void __launch_bounds__(RB_BACK_THREADS)
 route_balance_backward_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, const int32_t *__restrict__ expert,
                               const int32_t *__restrict__ counts, const float *__restrict__ dloss, const void *add, int64_t lda,
                               void *dlogits, int64_t ldd)
 {
-    constexpr int TOKENS = RB_THREADS / L;
+    constexpr int TOKENS = RB_BACK_THREADS / L;
     const int gl = threadIdx.x & (L - 1);
     const int n = DASS_LD(counts + E);
     const float inverse = n > 0 ? 1.0f / (float)n : 0.f;
@@ -234,9 +277,13 @@ route_balance_backward_kernel(const void *__restrict__ logits, int64_t T, int E,
     for (int64_t r = blockIdx.x; r < rounds; r += gridDim.x) {
         const int64_t t = r * TOKENS + threadIdx.x / L;
         const bool live = t < T;
+        RbRow<BF16, W, V> row;
+        int id[RB_IDS<L>];
         float x[V];
-        rb_load<BF16, W, V, L>(logits, (live ? t : 0) * ld, gl, live ? E : 0, x);
-        const bool in = rb_chosen<L, false>(expert, t, k, E, gl, live, nullptr);
+        rb_load<BF16, W, V, L>(row, logits, (live ? t : 0) * ld, gl, live ? E : 0);
+        rb_load_ids<L>(id, expert, t, k, gl, live);
+        rb_floats<BF16, W, V, L>(row, gl, live ? E : 0, x);
+        const bool in = rb_chosen<L, false>(id, expert, t, k, E, gl, live, nullptr);
         const float inv = rb_softmax<V, L>(x);
         float dot = 0.f;
 #pragma unroll
@@ -294,13 +341,18 @@ template <bool BF16, int W, int V, int L>
 static cudaError_t rb_launch(const BalanceArgs &a)
 {
     if (a.dlogits) {
-        constexpr int TOKENS = RB_THREADS / L;
+        constexpr int TOKENS = RB_BACK_THREADS / L;
         const int64_t rounds = (a.T + TOKENS - 1) / TOKENS, most = 8 * (int64_t)device_sm_count();
-        route_balance_backward_kernel<BF16, W, V, L><<<(unsigned)(rounds < most ? rounds : most), RB_THREADS, 0, a.st>>>(
+        route_balance_backward_kernel<BF16, W, V, L><<<(unsigned)(rounds < most ? rounds : most), RB_BACK_THREADS, 0, a.st>>>(
             a.logits, a.T, a.E, a.ld, a.k, a.expert, a.load, a.dloss, a.add, a.lda, a.dlogits, a.ldd);
         return cudaGetLastError();
     }
-    const size_t smem = ((size_t)(RB_THREADS / 32) * a.E + a.E + 1) * 4;       // at most 36 KB
+    const size_t smem = ((size_t)(RB_THREADS / 32) * a.E + a.E + 1) * 4;       // at most 68 KB
+    if (smem > 48 * 1024) {                                                      // E above 722
+        static DeviceMask configured{0ull};                                      // per device
+        const cudaError_t e = ensure_dynamic_smem(route_balance_kernel<BF16, W, V, L>, 68 * 1024 + 8, configured);
+        if (e != cudaSuccess) return e;
+    }
     route_balance_kernel<BF16, W, V, L><<<a.blocks, RB_THREADS, smem, a.st>>>(a.logits, a.T, a.E, a.ld, a.k, a.expert, a.partial,
                                                                              a.partial_counts, a.loss, a.counts, a.share);
     return cudaGetLastError();
