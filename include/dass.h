@@ -392,11 +392,17 @@ dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int
  * W (w_codes, w_scales) and W_up (nullable: the GLU form) are `groups` matrices [N x K].  Products of the values that codes and
  * scales stand for, in f32 accumulators.  bias, bias_up, residual, Y in bf16, offsets and groups, alignment and what else is
  * not said here: as for dass_linear, whose dass_linear_status reports this call's bounded waits too.
- * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (X in both forms; limits of dass_linear) / CUDA. */
+ * bf16 rows meet the weights as they are, or, where few of them meet many weights, as sums of 4-bit rows that hold every
+ * value of a block of 32 to 2^-24 of the largest in it; those rows go to the workspace: dass_linear_mx4_workspace_bytes(..)
+ * bytes (may be 0), 16-byte aligned.  groups = 1 and has_offsets = 0 for a dense product.
+ * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (X in both forms; limits of dass_linear) / WORKSPACE / CUDA. */
+dass_status dass_linear_mx4_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t groups, int has_offsets, int has_up, int x_in_4_bits,
+                                            size_t *bytes /* HOST */);
 dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, const uint8_t *x_scales, int64_t T, int64_t K,
                             const uint8_t *w_codes, const uint8_t *w_scales, const uint8_t *up_codes, const uint8_t *up_scales, int64_t N,
                             const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,
-                            void *Y, int64_t ldy, const int32_t *offsets, int64_t groups, void *cuda_stream);
+                            void *Y, int64_t ldy, const int32_t *offsets, int64_t groups,
+                            void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* ------------------------------------------------------------------ checked-access build
  * (No counterpart in the paper: the stand-in for a memory sanitizer.)  libdass_check.so is this library compiled with

@@ -33,7 +33,7 @@ EXPORTS = (
     "dass_route_topk", "dass_route_topk_backward", "dass_expert_sort_workspace_bytes", "dass_expert_sort",
     "dass_expert_gather", "dass_expert_combine", "dass_expert_combine_backward", "dass_linear", "dass_linear_status",
     "dass_route_balance_workspace_bytes", "dass_route_balance", "dass_route_balance_backward",
-    "dass_mx4_bytes", "dass_mx4_quantize", "dass_mx4_dequantize", "dass_linear_mx4",
+    "dass_mx4_bytes", "dass_mx4_quantize", "dass_mx4_dequantize", "dass_linear_mx4_workspace_bytes", "dass_linear_mx4",
     "dass_bounds_report", "dass_bounds_shrink_next",
     "dass_status_string", "dass_version",
 )
@@ -152,7 +152,9 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.dass_mx4_dequantize.restype = ci
     lib.dass_mx4_dequantize.argtypes = [vp, vp, i64, i64, i64, vp, i64, i64, ci, vp]
     lib.dass_linear_mx4.restype = ci
-    lib.dass_linear_mx4.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp, ci, vp, i64, vp, i64, vp, i64, vp]
+    lib.dass_linear_mx4_workspace_bytes.restype = ci
+    lib.dass_linear_mx4_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci, ci, ctypes.POINTER(sz)]
+    lib.dass_linear_mx4.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp, ci, vp, i64, vp, i64, vp, i64, vp, sz, vp]
     lib.dass_status_string.restype = ctypes.c_char_p
     lib.dass_status_string.argtypes = [ctypes.c_int]
     lib.dass_version.restype = ctypes.c_int
@@ -969,9 +971,18 @@ def mx4_dequantize(Q: MX4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     return out
 
 
+def linear_mx4_workspace_bytes(T: int, K: int, N: int, groups: int = 1, has_offsets: bool = False, has_up: bool = False,
+                               x_in_4_bits: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().dass_linear_mx4_workspace_bytes(int(T), int(K), int(N), int(groups), int(has_offsets), int(has_up), int(x_in_4_bits),
+                                                  ctypes.byref(out)), "dass_linear_mx4_workspace_bytes")
+    return int(out.value)
+
+
 def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, W_up: Optional[MX4] = None,
                bias_up: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
-               Y: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+               Y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """linear() with weights in 4 bits: Y = act(X W^T + bias) [* (X W_up^T + bias_up)] + residual in bfloat16.
 
     X [T x K] is a bfloat16 matrix or an MX4 (mx4_quantize's).  Dense: W (and W_up) [N x K]; per expert, with ``offsets``:
@@ -1022,6 +1033,12 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
     else:
         ldy = like(Y, "Y")
     if T:
+        if workspace is None:
+            need = linear_mx4_workspace_bytes(T, K, N, groups, offsets is not None, W_up is not None, quantized)
+            workspace = _new(first, stream)(need, dtype=torch.uint8) if need else None
+        else:
+            _workspace(workspace, device)
         _check(load().dass_linear_mx4(x, ldx, xc, xs, T, K, wc, ws, uc, us, N, b, bu, act, _ptr(residual), ldr, Y.data_ptr(), ldy, edges,
-                                      groups, _stream_of(first, stream)), "dass_linear_mx4")
+                                      groups, _ptr(workspace), workspace.numel() if workspace is not None else 0,
+                                      _stream_of(first, stream)), "dass_linear_mx4")
     return Y

@@ -65,6 +65,20 @@ __device__ __forceinline__ void mx4_decode8(uint32_t x, const Mx4Factor &f, bool
     }
 }
 
+// Two floats to two codes each, four pairs: v[0] in the lowest bits.
+__device__ __forceinline__ uint32_t mx4_encode8(const float (&v)[8])
+{
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+
 // 8 codes as floats times `scale`, in order.
 __device__ __forceinline__ void mx4_decode8_f32(uint32_t x, float scale, float (&v)[8])
 {

@@ -21,23 +21,34 @@ __host__ __device__ __forceinline__ Mx4Matrix mx4_group(const Mx4Matrix &m, int6
     return {m.codes + g * N * mx4_pitch(K), m.scales + g * ((N + MX4_TILE_ROWS - 1) / MX4_TILE_ROWS) * mx4_k_tiles(K) * MX4_TILE_BYTES};
 }
 
+// ------------------------------------------------------------------ descriptors of the block-scaled products
+// Descriptor of 32 rows of 16 bytes, one after the other, for tcgen05.cp: 8-row groups 128 bytes apart, no swizzle.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+}
+// Instruction descriptor of kind::mxf4: A = B = e2m1, both K-major, scales ue8m0, D = f32; sf: which half of a scale word.
+__host__ __device__ constexpr uint32_t idesc_mxf4(int m, int n, int sf)
+{
+    return ((uint32_t)sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 7) << 27) | ((uint32_t)sf << 29);
+}
+
 // ------------------------------------------------------------------ the persistent kernels' walk
-// Every group's rows are cut into tiles by themselves, of ROWS rows from the multiple of ALIGN at or below the group's first
+// Every group's rows are cut into tiles by themselves, of `rows` rows from the multiple of `align` at or below the group's first
 // one.  The host does not know the offsets, so every CTA builds the prefix sums of the groups' tile counts once (in `table`:
 // first tiles, then first rows, then ends) and finds its items in them.  Inside a group the items run over MX4_BAND row
 // tiles before they step to the next columns, so that the CTAs at work at one time share a patch of tiles through L2.
 constexpr int MX4_BAND = 8;
 constexpr uint32_t MX4_TABLE_BYTES = (3 * LIN_MAX_GROUPS + 4) * 4;
 
-struct Mx4Item { int g; int row, row_lo, row_hi, col; };   // the tile's first row, the group's rows, the first column
+struct Mx4Item { int g; int tile, row, row_lo, row_hi, col; };   // the row tile, counted over all groups, its first row, the group's rows, the first column
 
-template <int ALIGN, int ROWS>
-__device__ __forceinline__ void mx4_count_tiles(int *table, const int32_t *offsets, int groups, int64_t T, int threads)
+__device__ __forceinline__ void mx4_count_tiles(int *table, const int32_t *offsets, int groups, int64_t T, int align, int rows, int threads)
 {
     for (int g = threadIdx.x; g < groups; g += threads) {
         int64_t lo, hi;
         lin_group_rows(offsets, g, T, lo, hi);
-        table[g + 1] = hi > lo ? (int)((hi - (lo & ~(int64_t)(ALIGN - 1)) + ROWS - 1) / ROWS) : 0;
+        table[g + 1] = hi > lo ? (int)((hi - (lo & ~(int64_t)(align - 1)) + rows - 1) / rows) : 0;
         table[LIN_MAX_GROUPS + 4 + g] = (int)lo;
         table[2 * LIN_MAX_GROUPS + 4 + g] = (int)hi;
     }
@@ -61,8 +72,7 @@ __device__ __forceinline__ void mx4_sum_tiles(int *table, int groups)
     if (lane == 0) table[0] = 0;
 }
 // The idx-th item of the walk; false past the last one.
-template <int ALIGN, int ROWS>
-__device__ __forceinline__ bool mx4_item(const int *table, int groups, int col_tiles, int cols_per_tile, int64_t idx, Mx4Item &it)
+__device__ __forceinline__ bool mx4_item(const int *table, int groups, int align, int rows, int col_tiles, int cols_per_tile, int64_t idx, Mx4Item &it)
 {
     const int *lo = table + LIN_MAX_GROUPS + 4, *hi = lo + LIN_MAX_GROUPS;
     if (idx >= (int64_t)table[groups] * col_tiles) return false;
@@ -81,9 +91,62 @@ __device__ __forceinline__ bool mx4_item(const int *table, int groups, int col_t
     it.g = a;
     it.row_lo = lo[a];
     it.row_hi = hi[a];
-    it.row = (lo[a] & ~(ALIGN - 1)) + (band * MX4_BAND + (r2 - ct * nb)) * ROWS;
+    const int nth = band * MX4_BAND + (r2 - ct * nb);
+    it.tile = table[a] + nth;
+    it.row = (lo[a] & ~(align - 1)) + nth * rows;
     it.col = ct * cols_per_tile;
     return true;
+}
+
+// ------------------------------------------------------------------ blocks of Y whose columns are lanes
+// Where a TMEM lane is a column of Y a thread holds one column, and a store from there would move 2 bytes.  A warp's block of
+// rows x 32 columns therefore passes through shared memory (64 bytes a row), where the residual waits before it.
+// Rows lo .. hi - 1 exist, and `left` columns (32 or more: all).  Called by a whole warp; ends with a warp barrier.
+__device__ __forceinline__ void mx4_block_in(uint16_t *block, const uint16_t *from, int64_t ld, bool vec, int lo, int hi, int left)
+{
+    const int lane = threadIdx.x & 31;
+    if (vec && left >= 32) {
+#pragma unroll 4
+        for (int r = lo + (lane >> 2); r < hi; r += 8)
+            *reinterpret_cast<uint4 *>(block + r * 32 + (lane & 3) * 8) = DASS_LD(reinterpret_cast<const uint4 *>(from + r * ld + (lane & 3) * 8));
+    } else {
+#pragma unroll 4
+        for (int r = lo; r < hi; ++r)
+            if (lane < left) block[r * 32 + lane] = DASS_LD(from + r * ld + lane);
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void mx4_block_out(const uint16_t *block, uint16_t *to, int64_t ld, bool vec, int lo, int hi, int left)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    if (vec && left >= 32) {
+#pragma unroll 4
+        for (int r = lo + (lane >> 2); r < hi; r += 8)
+            DASS_ST(reinterpret_cast<uint4 *>(to + r * ld + (lane & 3) * 8), *reinterpret_cast<const uint4 *>(block + r * 32 + (lane & 3) * 8));
+    } else {
+#pragma unroll 4
+        for (int r = lo; r < hi; ++r)
+            if (lane < left) DASS_ST(to + r * ld + lane, block[r * 32 + lane]);
+    }
+    __syncwarp();
+}
+// V results of this lane's column, rows r0 .. r0 + V - 1 of the block: plus what the block holds there, if it does, rounded.
+template <int V>
+__device__ __forceinline__ void mx4_block_set(uint16_t *block, int r0, const float (&y)[V], bool add)
+{
+    uint16_t *at = block + r0 * 32 + (threadIdx.x & 31);
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+        float a = y[i], b = y[i + 1];
+        if (add) {
+            a += __uint_as_float((uint32_t)at[i * 32] << 16);
+            b += __uint_as_float((uint32_t)at[i * 32 + 32] << 16);
+        }
+        const uint32_t w = pack_bf16x2(a, b);
+        at[i * 32] = (uint16_t)w;
+        at[i * 32 + 32] = (uint16_t)(w >> 16);
+    }
 }
 
 // ------------------------------------------------------------------ tensor maps

@@ -24,20 +24,6 @@ constexpr int MQ_COLS = 256;         // columns of a warp
 // them side by side.  grid.x columns, grid.y rows, grid.z matrices; the last two wrap around.
 struct MqGrid { int across; int64_t row_groups, groups; };
 
-// Two floats to two codes each, four pairs: v[0] in the lowest bits.
-__device__ __forceinline__ uint32_t mx4_encode8(const float (&v)[8])
-{
-    uint32_t r;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-        "mov.b32 %0, {a, b, c, d};\n\t}"
-        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return r;
-}
-
 // 8 values of a lane as they lie in memory: 16-byte pieces where rows allow them; else single elements, 32 consecutive ones to
 // an access of the warp, that change lanes through shared memory (mq_turn).
 template <bool BF16, bool VECTOR> struct MqRaw { RowRaw<BF16, VECTOR ? ROW_VEC<BF16> : 1> piece[VECTOR ? 8 / ROW_VEC<BF16> : 8]; };

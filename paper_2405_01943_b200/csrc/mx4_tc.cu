@@ -55,21 +55,11 @@ struct MtParams {
 };
 
 // ------------------------------------------------------------------ PTX wrappers
-// Descriptor of 32 rows of 16 bytes, one after the other, for tcgen05.cp: 8-row groups 128 bytes apart, no swizzle.
-__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr)
-{
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-}
 // 32 rows of 16 bytes to 4 TMEM columns of lanes 0 .. 31, and to the other three quarters of the lanes; in both CTAs, each
 // from its own shared memory.
 __device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t desc)
 {
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-// Instruction descriptor of kind::mxf4: A = B = e2m1, both K-major, scales ue8m0, D = f32; sf: which half of a scale word.
-__host__ __device__ constexpr uint32_t idesc_mxf4(int m, int n, int sf)
-{
-    return ((uint32_t)sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 7) << 27) | ((uint32_t)sf << 29);
 }
 __device__ __forceinline__ void umma_mxf4_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
 {
@@ -125,7 +115,7 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    mx4_count_tiles<MT_BM, 2 * MT_BM>(first_tile, p.offsets, p.groups, p.T, MT_THREADS);
+    mx4_count_tiles(first_tile, p.offsets, p.groups, p.T, MT_BM, 2 * MT_BM, MT_THREADS);
     if (warp == 1) {
         tmem_alloc_pair(smem_u32(tmem_slot), 512);
         tmem_relinquish_pair();
@@ -147,7 +137,7 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         const uint64_t pol = l2_policy_evict_last();
         const CUtensorMap *map_b = GLU && rank ? &map_up : &map_w;
         Mx4Item it;
-        for (int64_t idx = pair; ok && mx4_item<MT_BM, 2 * MT_BM>(first_tile, p.groups, p.col_tiles, p.cols_per_tile, idx, it); idx += pairs) {
+        for (int64_t idx = pair; ok && mx4_item(first_tile, p.groups, MT_BM, 2 * MT_BM, p.col_tiles, p.cols_per_tile, idx, it); idx += pairs) {
             const int a_row = it.row + (int)rank * MT_BM;
             const int b_row = it.col + (GLU ? 0 : (int)rank * (BN / 2));
             const int a_tile = a_row / MX4_TILE_ROWS < p.x_tiles ? a_row / MX4_TILE_ROWS : p.x_tiles - 1;      // absent rows are not stored
@@ -228,7 +218,7 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         uint32_t tile = 0;
         bool ok = true;
         Mx4Item it;
-        for (int64_t idx = pair; ok && mx4_item<MT_BM, 2 * MT_BM>(first_tile, p.groups, p.col_tiles, p.cols_per_tile, idx, it); idx += pairs, ++tile) {
+        for (int64_t idx = pair; ok && mx4_item(first_tile, p.groups, MT_BM, 2 * MT_BM, p.col_tiles, p.cols_per_tile, idx, it); idx += pairs, ++tile) {
             const uint32_t as = tile % S::ACCS;
             const int64_t t0 = (int64_t)it.row + rank * MT_BM + quad * 32;                  // the warp's first row
             const int r_lo = it.row_lo > t0 ? (int)(it.row_lo - t0 < 32 ? it.row_lo - t0 : 32) : 0;

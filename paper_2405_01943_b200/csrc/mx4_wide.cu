@@ -11,8 +11,8 @@
 //                 the GLU form, a block of one matrix of every slab
 //   warps 20..27  epilogue: a TMEM lane is a column of Y, a thread has one column of half of the tile's rows
 // The accumulator (NT columns, in the GLU form NT of each product) leaves TMEM room for a ring of decoded slabs and for no
-// second accumulator.  So the epilogue has the residual in registers before the accumulator is complete, turns it into
-// packed bf16 results there, hands it back, and stores under the next tile's products.
+// second accumulator.  So the epilogue has the residual in shared memory before the accumulator is complete, turns it into
+// bf16 results there, hands it back, and stores under the next tile's products.
 // A decoded slab takes 200 to 400 cycles of the integer pipe, its products 512 at NT = 256 (gated: 128).
 //
 // Every wait is bounded, as in linear_tc.cu.
@@ -39,7 +39,8 @@ template <int NT, bool GLU> struct MwShape {
     static constexpr int W_STAGES = 3;
     static constexpr int A_STAGES = 8 / M;                            // of 32 TMEM columns for each matrix
     static constexpr uint32_t W_AT = X_STAGES * X_BYTES;
-    static constexpr uint32_t BYTES = W_AT + W_STAGES * W_BYTES + 1024 /* alignment slack */ + 512 /* barriers */ + MX4_TABLE_BYTES;
+    static constexpr int ROWS = NT / 2;                               // rows of Y of an epilogue warp, which has 32 columns
+    static constexpr uint32_t BYTES = W_AT + W_STAGES * W_BYTES + 8 * ROWS * 64 + 1024 /* alignment slack */ + 512 /* barriers */ + MX4_TABLE_BYTES;
     static_assert(M * NT <= 256 && BYTES <= 227 * 1024 && X_BYTES % 1024 == 0 && (MW_CODES + MW_SCALES) % 1024 == 0, "");
 };
 
@@ -48,7 +49,7 @@ struct MwParams {
     const uint16_t *bias, *bias_up, *residual;
     uint16_t *Y;
     int64_t ldr, ldy, T;
-    int N, groups, col_tiles, slabs, w_tiles, y_vec;
+    int N, groups, col_tiles, slabs, w_tiles, y_vec, r_vec;
     int *timeouts;
 };
 
@@ -108,7 +109,7 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;                 // swizzled tiles need 1024-byte alignment
     uint8_t *aligned = smem_raw + (base - raw);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + S::W_AT + WS * S::W_BYTES);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + S::W_AT + WS * S::W_BYTES + 8 * S::ROWS * 64);
     const uint32_t x_full = smem_u32(bars), x_empty = x_full + 8 * XS;        // full: leader; empty: per CTA
     const uint32_t w_full = x_empty + 8 * XS, w_empty = w_full + 8 * WS;      // per CTA
     const uint32_t a_full = w_empty + 8 * WS, a_empty = a_full + 8 * AS;      // full: leader, both CTAs' warps arrive; empty: per CTA
@@ -138,7 +139,7 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    mx4_count_tiles<1, NT>(table, p.offsets, p.groups, p.T, MW_THREADS);
+    mx4_count_tiles(table, p.offsets, p.groups, p.T, 1, NT, MW_THREADS);
     if (warp == 1) {
         tmem_alloc_pair(smem_u32(tmem_slot), 512);
         tmem_relinquish_pair();
@@ -162,7 +163,7 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             uint32_t stage = 0, phase = 0;
             const uint32_t leader_full = map_to_cta(x_full, 0);
             const uint64_t pol = l2_policy_evict_last();
-            for (int64_t idx = pair; ok && mx4_item<1, NT>(table, p.groups, p.col_tiles, 2 * MW_ROWS, idx, it); idx += pairs) {
+            for (int64_t idx = pair; ok && mx4_item(table, p.groups, 1, NT, p.col_tiles, 2 * MW_ROWS, idx, it); idx += pairs) {
                 const int row = it.row + (int)rank * (NT / 2);
                 for (int s = 0; s < p.slabs; ++s) {
                     if (!warp_wait(x_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
@@ -178,7 +179,7 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             // -------------------------------------------------------- TMA of codes and scales (one per CTA)
             uint32_t stage = 0, phase = 0;
             const uint64_t pol = l2_policy_evict_last();
-            for (int64_t idx = pair; ok && mx4_item<1, NT>(table, p.groups, p.col_tiles, 2 * MW_ROWS, idx, it); idx += pairs) {
+            for (int64_t idx = pair; ok && mx4_item(table, p.groups, 1, NT, p.col_tiles, 2 * MW_ROWS, idx, it); idx += pairs) {
                 const int row = it.col + (int)rank * MW_ROWS;
                 const int of = row / MX4_TILE_ROWS, tile = it.g * p.w_tiles + (of < p.w_tiles ? of : p.w_tiles - 1);   // absent rows are not stored
                 for (int s = 0; s < w_stages; ++s) {
@@ -280,54 +281,38 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         lin_zero_outside<true>(p.offsets, p.groups, p.T, p.N, p.Y, p.ldy, p.y_vec != 0, (int64_t)blockIdx.x * EPI + threadIdx.x - (MW_THREADS - EPI),
                                (int64_t)gridDim.x * EPI);
         const int quad = warp & 3, half = (warp - MW_FIRST_EPILOGUE) >> 2;
-        constexpr int ROWS = NT / 2;                             // rows of Y of a thread
-        constexpr int CH = 16;                                   // at a time
+        constexpr int ROWS = S::ROWS;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16) + half * ROWS;
         const uint32_t leader_acc_empty = map_to_cta(acc_empty, 0);
+        uint16_t *block = reinterpret_cast<uint16_t *>(aligned + S::W_AT + WS * S::W_BYTES + (warp - MW_FIRST_EPILOGUE) * (ROWS * 64));
         uint32_t tile = 0;
-        for (int64_t idx = pair; ok && mx4_item<1, NT>(table, p.groups, p.col_tiles, 2 * MW_ROWS, idx, it); idx += pairs, ++tile) {
-            const int n = it.col + (int)rank * MW_ROWS + quad * 32 + lane;
+        for (int64_t idx = pair; ok && mx4_item(table, p.groups, 1, NT, p.col_tiles, 2 * MW_ROWS, idx, it); idx += pairs, ++tile) {
+            const int n0 = it.col + (int)rank * MW_ROWS + quad * 32, left = p.N - n0;
             const int64_t t0 = (int64_t)it.row + half * ROWS;
-            const int left = it.row_hi - t0 < ROWS ? (int)(it.row_hi - t0) : ROWS;
-            const int rows = n < p.N ? left : 0;                 // this thread's rows of Y; <= 0: none
-            const float b = p.bias && n < p.N ? __uint_as_float((uint32_t)DASS_LD(p.bias + (int64_t)it.g * p.N + n) << 16) : 0.f;
-            const float bu = GLU && p.bias_up && n < p.N ? __uint_as_float((uint32_t)DASS_LD(p.bias_up + (int64_t)it.g * p.N + n) << 16) : 0.f;
-            uint32_t y[ROWS / 2];                                // pairs of rows: the residual, then the result
-#pragma unroll
-            for (int i = 0; i < ROWS / 2; ++i) y[i] = 0u;
-            if (p.residual) {
-                const uint16_t *res = p.residual + t0 * p.ldr + n;
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-                    if (i < rows) y[i / 2] |= (uint32_t)DASS_LD(res + i * p.ldr) << (16 * (i & 1));
-            }
+            const int rows = left <= 0 ? 0 : it.row_hi - t0 < ROWS ? (int)(it.row_hi - t0) : ROWS;   // <= 0: none
+            const float b = p.bias && lane < left ? __uint_as_float((uint32_t)DASS_LD(p.bias + (int64_t)it.g * p.N + n0 + lane) << 16) : 0.f;
+            const float bu = GLU && p.bias_up && lane < left ? __uint_as_float((uint32_t)DASS_LD(p.bias_up + (int64_t)it.g * p.N + n0 + lane) << 16) : 0.f;
+            if (p.residual) mx4_block_in(block, p.residual + t0 * p.ldr + n0, p.ldr, p.r_vec, 0, rows, left);
             if (!warp_wait(acc_full, tile & 1u, abort_flag)) { ok = false; break; }
             tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < ROWS; c += CH) {
-                uint32_t a[CH], u[CH];
+#pragma unroll 1
+            for (int c = 0; c < rows; c += 16) {
+                uint32_t a[16], u[16];
+                float y[16];
                 tmem_ld_16(lane_addr + c, a);
                 if constexpr (GLU) tmem_ld_16(lane_addr + NT + c, u);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < CH; i += 2) {
-                    float v[2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        v[h] = lt_act<ACT>(__uint_as_float(a[i + h]) + b);
-                        if constexpr (GLU) v[h] *= __uint_as_float(u[i + h]) + bu;
-                    }
-                    uint32_t &w = y[(c + i) / 2];
-                    w = pack_bf16x2(v[0] + __uint_as_float(w << 16), v[1] + __uint_as_float(w & 0xffff0000u));
+                for (int i = 0; i < 16; ++i) {
+                    y[i] = lt_act<ACT>(__uint_as_float(a[i]) + b);
+                    if constexpr (GLU) y[i] *= __uint_as_float(u[i]) + bu;
                 }
+                mx4_block_set(block, c, y, p.residual != nullptr);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_tmem(leader_acc_empty);   // release the accumulator to the leader's MMA warp
-            uint16_t *out = p.Y + t0 * p.ldy + n;                // a warp stores runs of 32 columns
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i)
-                if (i < rows) DASS_ST(out + i * p.ldy, (uint16_t)(y[i / 2] >> (16 * (i & 1))));
+            mx4_block_out(block, p.Y + t0 * p.ldy + n0, p.ldy, p.y_vec, 0, rows, left);
         }
     }
     if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }
@@ -398,6 +383,7 @@ dass_status mx4_wide_launch(const Mx4Args &q, int nt)
     p.slabs = (int)((a.K + MW_BK - 1) / MW_BK);
     p.w_tiles = (int)w_tiles;
     p.y_vec = rows_vec_ok(a.Y, a.ldy, true);
+    p.r_vec = a.residual && rows_vec_ok(a.residual, a.ldr, true);
     p.timeouts = linear_timeouts();
     if (!p.timeouts) return DASS_ERR_CUDA;
     const int64_t items = ((a.T + nt - 1) / nt + (a.offsets ? a.groups : 0)) * p.col_tiles;   // at most

@@ -102,7 +102,7 @@ def test_every_code_and_scale():
     want = ref.values(codes, scales)
     for dtype in (BF16, F32):
         top = float(torch.finfo(dtype).max)
-        _same_values(eref.f64(b.mx4_dequantize(Q, dtype)), np.where(np.abs(want) > top, np.sign(want) * np.inf, want))
+        _same_values(eref.f64(b.mx4_dequantize(Q, dtype)), np.where(np.abs(want) > top, np.copysign(np.inf, want), want))
 
 
 def test_no_rows():
@@ -177,6 +177,98 @@ options = pytest.mark.parametrize("options", OPTIONS, ids=lambda o: "-".join([o[
                                    (33, 96, 257), (64, 200, 512), (65, 128, 127), (100, 1024, 200), (129, 72, 300), (300, 392, 520), (513, 64, 129)])
 def test_dense(T, K, N, both4, options):
     _dense(T, K, N, both4, **options)
+
+
+def _on_device(X, W, V, bias, bias_up, R, act, rows16):
+    """eref.linear on the device, for weights of a realistic size: (value, bound).  Rows that were split into 4-bit ones carry
+    2^-24 of the largest value of their block of 32 at every k."""
+    v = lambda q: b.mx4_dequantize(q, F32).double()                    # noqa: E731
+    x = v(X) if isinstance(X, b.MX4) else X.double()
+    K, eps = x.shape[1], eref.EPS24
+    lost = torch.zeros_like(x)
+    if rows16:
+        pad = torch.nn.functional.pad(x.abs(), (0, -K % 32)).view(len(x), -1, 32)
+        lost = (2.0 ** -24 * pad.amax(2, keepdim=True)).expand_as(pad).reshape(len(x), -1)[:, :K]
+
+    def product(q, bb):
+        w = v(q)
+        add = 0.0 if bb is None else bb.double()
+        p = x @ w.t() + add
+        return p, (K + 1) * 2 * eps * (x.abs() @ w.abs().t() + abs(add)) + lost @ w.abs().t() + (0 if not rows16 else 12 * eps * (x.abs() @ w.abs().t()))
+
+    p, ep = product(W, bias)
+    y = {"none": lambda t: t, "silu": lambda t: t * torch.sigmoid(t)}[act](p)
+    e = ep if act == "none" else 1.13 * ep + 2.0 ** -19 * p.abs()
+    if V is not None:
+        u, eu = product(V, bias_up)
+        e = e * (u.abs() + eu) + y.abs() * eu + 2 * eps * (y * u).abs()
+        y = y * u
+    if R is not None:
+        y = y + R.double()
+        e = e + 2 * eps * y.abs()
+    return y, e + eref.HALF_ULP[BF16] * (y.abs() + e) + 1e-37
+
+
+def _normal_mx4(N, K, seed):
+    return b.mx4_quantize(_randn((N, K), seed, 0.02))
+
+
+@forms
+@pytest.mark.parametrize("T,K,N,glu", [(1, 4096, 14336, True), (5, 4096, 14336, True), (12, 4096, 14300, True), (3, 8192, 9001, False), (9, 8200, 8192, False),
+                                       (40, 4096, 14336, True), (130, 4096, 14336, True), (300, 4096, 4096, False), (900, 1032, 4001, True)])
+def test_weights_that_are_the_time(T, K, N, glu, both4):
+    X = _pitched((T, K), 1)
+    X[:, 7] *= 300                                                     # a channel that its neighbours' block has to live with
+    rows16 = not both4 and b.linear_mx4_workspace_bytes(T, K, N, has_up=glu) > 0
+    X = b.mx4_quantize(X) if both4 else X
+    W, V = _normal_mx4(N, K, 2), _normal_mx4(N, K, 3) if glu else None
+    bias, bias_up, R = _randn((N,), 4), _randn((N,), 5) if glu else None, _randn((T, N + 3), 6)[:, 1:1 + N]
+    act = "silu" if glu else "none"
+    Y = b.linear_mx4(X, W, bias=bias, act=ACTS[act], W_up=V, bias_up=bias_up, residual=R)
+    again = b.linear_mx4(X, W, bias=bias, act=ACTS[act], W_up=V, bias_up=bias_up, residual=R)
+    b.linear_status()
+    assert torch.equal(Y, again)
+    want, bound = _on_device(X, W, V, bias, bias_up, R, act, rows16)
+    err = (Y.double() - want).abs()
+    assert bool((err <= bound).all()), float((err / bound).max())
+
+
+@forms
+@pytest.mark.parametrize("counts", [[4, 0, 1, 9, 3, 12, 2, 1], [0, 25, 0, 0, 31, 0, 0, 3], [64, 1, 0, 90, 130, 12, 300, 8]], ids=lambda c: str(sum(c)))
+@pytest.mark.parametrize("K,N,glu", [(2048, 7168, True), (7168, 2050, False)])
+def test_experts_of_a_size(counts, K, N, glu, both4):
+    G, n = len(counts), sum(counts) + 3
+    edges = np.concatenate([[0], np.cumsum(counts)])
+    offsets = torch.tensor(edges, dtype=torch.int32, device=DEV)
+    X = _pitched((n, K), 1)
+    X[-3:] = float("nan")
+    rows16 = not both4 and b.linear_mx4_workspace_bytes(n, K, N, G, True, glu) > 0
+    X = b.mx4_quantize(X) if both4 else X
+    stack = lambda seed: [_normal_mx4(N, K, seed + g) for g in range(G)]                                            # noqa: E731
+    join = lambda q: b.MX4(torch.stack([m.codes for m in q]), torch.stack([m.scales for m in q]), K)                # noqa: E731
+    W, V = stack(10), stack(30) if glu else None
+    bias, R = _randn((G, N), 4), _randn((n, N), 6)
+    act = "silu" if glu else "none"
+    Y = b.linear_mx4(X, join(W), bias=bias, act=ACTS[act], W_up=join(V) if glu else None, residual=R, offsets=offsets)
+    b.linear_status()
+    assert bool((Y[-3:] == 0).all())
+    whole = b.mx4_dequantize(X, F32) if both4 else None
+    for g in range(G):
+        lo, hi = edges[g], edges[g + 1]
+        if hi > lo:
+            rows = b.mx4_quantize(whole[lo:hi]) if both4 else X[lo:hi]  # values that are in 4 bits stay what they are
+            want, bound = _on_device(rows, W[g], V[g] if glu else None, bias[g], None, R[lo:hi], act, rows16)
+            err = (Y[lo:hi].double() - want).abs()
+            assert bool((err <= bound).all()), (g, float((err / bound).max()))
+
+
+def test_nan_and_infinity_in_rows_that_are_split():
+    X = _randn((3, 4096), 1)
+    W = _normal_mx4(14336, 4096, 2)
+    assert b.linear_mx4_workspace_bytes(3, 4096, 14336, has_up=True) > 0
+    X[1, 100], X[2, 4095] = float("nan"), float("inf")
+    Y = b.linear_mx4(X, W, W_up=W)
+    assert bool(torch.isfinite(Y[0]).all()) and not bool(torch.isfinite(Y[1:]).any())
 
 
 @forms
@@ -331,5 +423,12 @@ def test_every_access_stays_inside():
             for edges in ([0, T // 2, T // 2, T], [-5, 2, 1, T + 90], [1, 1, 1, 1]):
                 for x in (X, b.mx4_quantize(X)):
                     b.linear_mx4(x, S, bias=_randn((3, N), 6), offsets=torch.tensor(edges, dtype=torch.int32, device=DEV))
+        for T, K, N in ((2, 4096, 14336), (11, 4100, 14001)):          # rows that are split into 4-bit ones
+            assert b.linear_mx4_workspace_bytes(T, K, N, has_up=True) > 0
+            W, X = _normal_mx4(N, K, 1), _pitched((T, K), 3)
+            for x in (X, b.mx4_quantize(X)):
+                b.linear_mx4(x, W, W_up=W, residual=_randn((T, N), 5))
+            S, edges = b.MX4(W.codes.expand(2, -1, -1).contiguous(), W.scales.expand(2, -1, -1, -1).contiguous(), K), torch.tensor([-5, 1, T + 9], dtype=torch.int32, device=DEV)
+            b.linear_mx4(X, S, W_up=S, offsets=edges)
         rep = b.bounds_report()
     assert rep["violations"] == 0, rep

@@ -44,8 +44,8 @@ def test_quantize(lib):
 
 def test_linear(lib):
     def f(X=P, ldx=64, xc=None, xs=None, T=4, K=64, wc=P, ws=P, uc=None, us=None, N=8, bias=None, bu=None, act=3, R=None, ldr=8, Y=P, ldy=8,
-          off=None, groups=1):
-        return lib.dass_linear_mx4(X, ldx, xc, xs, T, K, wc, ws, uc, us, N, bias, bu, act, R, ldr, Y, ldy, off, groups, None)
+          off=None, groups=1, work=None):
+        return lib.dass_linear_mx4(X, ldx, xc, xs, T, K, wc, ws, uc, us, N, bias, bu, act, R, ldr, Y, ldy, off, groups, work, 0, None)
 
     assert f(act=4) == DTYPE
     assert f(X=None) == NULL and f(wc=None) == NULL and f(ws=None) == NULL and f(uc=P) == NULL and f(us=P) == NULL and f(Y=None) == NULL
@@ -58,8 +58,26 @@ def test_linear(lib):
     assert f(uc=P + 8, us=P) == ALIGN and f(uc=P, us=P + 8) == ALIGN and f(ldx=65) == ALIGN
     assert f(X=None, xc=P + 8, xs=P) == ALIGN and f(X=None, xc=P, xs=P + 8) == ALIGN
     assert f(bias=P + 1) == ALIGN and f(R=P + 1) == ALIGN and f(Y=P + 1) == ALIGN and f(off=P + 2) == ALIGN
+    assert f(work=P + 8) == ALIGN
     assert f(T=1 << 29) == UNSUPPORTED and f(N=1 << 31, ldy=1 << 31) == UNSUPPORTED and f(off=P, groups=1025) == UNSUPPORTED
     assert f(T=0) == OK and f(T=0, X=None, Y=None) == OK
+
+
+def test_workspace_of_the_product(lib):
+    q, out = lib.dass_linear_mx4_workspace_bytes, ctypes.c_size_t(9)
+    f = lambda T=5, K=4096, N=14336, G=1, off=0, up=1, x4=0: q(T, K, N, G, off, up, x4, ctypes.byref(out))          # noqa: E731
+    assert q(1, 1, 1, 1, 0, 0, 0, None) == NULL
+    assert f(T=-1) == SHAPE and f(K=0) == SHAPE and f(N=0) == SHAPE and f(G=0) == SHAPE and f(G=2) == SHAPE
+    assert f(T=1 << 29) == UNSUPPORTED and f(off=1, G=1025) == UNSUPPORTED
+    assert f(T=0) == OK and out.value == 0
+    assert f(x4=1) == OK and out.value == 0                            # only bf16 rows are split into others
+    assert f(K=64, N=64) == OK and out.value == 0                      # and only where the weights are the time
+    assert f() == OK and out.value > 0
+    need = out.value
+    assert lib.dass_linear_mx4(P, 4096, None, None, 5, 4096, P, P, P, P, 14336, None, None, 3, None, 0, P, 14336, None, 1, P, need - 1, None) == WORKSPACE
+    assert lib.dass_linear_mx4(P, 4096, None, None, 5, 4096, P, P, P, P, 14336, None, None, 3, None, 0, P, 14336, None, 1, None, need, None) == WORKSPACE
+    assert f(G=8, off=1) == OK and out.value > need
+    assert b.linear_mx4_workspace_bytes(5, 4096, 14336, has_up=True) == need
 
 
 def test_balance(lib):
