@@ -1,5 +1,6 @@
 """Prunes the experts of a mixture-of-experts layer 2:4 by the norms over each expert's own tokens, then tunes the router
-around the pruned experts towards the dense layer's output.  Synthetic weights and tokens.
+around the pruned experts towards the dense layer's output, and puts what is left of the experts into 4 bits a weight.
+Synthetic weights and tokens.
 
     python examples/prune_expert_layer.py [tokens] [experts] [d] [d_int]
 """
@@ -51,6 +52,12 @@ def main(T: int = 4096, E: int = 8, d: int = 1024, I: int = 2816, k: int = 2, st
     pruned.check()
     print(f"{E} experts of {d} x {I}, top-{k}; tokens per expert {min(tokens)} .. {max(tokens)} of {T * k}")
     print(f"2:4 pruned, relative squared error of the layer's output: {before:.4f}; after {steps} steps on the router: {loss:.4f}")
+    small = pruned.quantize()
+    error4 = small.forward(X).float() - target.float()
+    small.check()
+    balance, counts, _ = pruned.balance(pruned.route(X))
+    print(f"in 4 bits a weight: {float(error4.square().mean() / target.float().square().mean()):.4f}; "
+          f"balance loss of the router left alone: {float(balance):.3f}, choices per expert {int(counts[:-1].min())} .. {int(counts[:-1].max())}")
     return before - loss
 
 

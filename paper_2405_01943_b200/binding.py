@@ -9,6 +9,7 @@ fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Callable, NamedTuple, Optional, Tuple, Union
 
@@ -838,6 +839,9 @@ def route_balance_workspace_bytes(T: int, E: int) -> int:
     return int(out.value)
 
 
+_balance_bytes = functools.lru_cache(maxsize=1024)(route_balance_workspace_bytes)      # a query costs as much as a check
+
+
 def route_balance(logits: torch.Tensor, expert: torch.Tensor, loss: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
                   share: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                   stream: Optional[torch.cuda.Stream] = None):
@@ -862,7 +866,7 @@ def route_balance(logits: torch.Tensor, expert: torch.Tensor, loss: Optional[tor
     else:
         _same(share, "share", (E,), torch.float32, dev)
     if workspace is None:
-        need = route_balance_workspace_bytes(T, E)
+        need = _balance_bytes(T, E)
         workspace = new(need, dtype=torch.uint8) if need else None
     else:
         _workspace(workspace, dev)
@@ -916,58 +920,64 @@ def _mx4_shapes(lead: Tuple[int, ...], cols: int) -> Tuple[Tuple[int, ...], Tupl
 
 
 def _mx4(q: MX4, name: str, device: torch.device) -> Tuple[int, int]:
-    """Checks a 4-bit matrix and returns its addresses."""
+    """Checks a 4-bit matrix or a stack of them and returns its addresses."""
     codes, scales, cols = q
-    lead = codes.shape[:-1]
-    if len(lead) not in (1, 2) or cols < 1:
-        raise ValueError(f"{name} must be an MX4 of [rows x cols] or [G x rows x cols]")
-    want = _mx4_shapes(lead, cols)
-    return _same(codes, f"{name}.codes", want[0], torch.uint8, device), _same(scales, f"{name}.scales", want[1], torch.uint8, device)
+    shape, tiles = codes.shape, scales.shape
+    if (len(shape) not in (2, 3) or cols < 1 or shape[-1] != (cols + 31) // 32 * 16 or len(tiles) != len(shape) + 1 or
+            tiles[-3] != (shape[-2] + 127) // 128 or tiles[-2] != (cols + 127) // 128 or tiles[-1] != 512 or (len(shape) == 3 and tiles[0] != shape[0]) or
+            codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.device != device or scales.device != device or
+            not codes.is_contiguous() or not scales.is_contiguous()):
+        raise ValueError(f"{name} must be an MX4 of [rows x cols] or [G x rows x cols] on {device}: contiguous uint8 codes and scales of the shapes it states")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def mx4_quantize(X: torch.Tensor, out: Optional[MX4] = None, stream: Optional[torch.cuda.Stream] = None) -> MX4:
     """X [rows x cols] or [G x rows x cols] (bfloat16 or float32, unit stride along columns) in microscaled 4-bit values."""
-    if X.dim() not in (2, 3) or not X.is_cuda:
-        raise ValueError("X must be a 2-D or 3-D CUDA tensor")
-    _here(X, stream)
     shape, strides = X.shape, X.stride()
-    G, rows, cols = shape if len(shape) == 3 else (1, *shape)
+    dims = len(shape)
+    if dims not in (2, 3) or not X.is_cuda:
+        raise ValueError("X must be a 2-D or 3-D CUDA tensor")
+    rows, cols = shape[-2:]
+    G, group_stride = (shape[0], strides[0]) if dims == 3 else (1, 0)
     if strides[-1] != 1 and cols > 1:
         raise ValueError("X must have unit stride along its columns")
     dt = _code(X)
     if cols < 1 or G < 1:
         raise ValueError("X must have columns (and, as a stack, matrices)")
     ld = strides[-2] if rows > 1 or strides[-2] > cols else cols
+    handle = _stream_of(X, stream)
     if out is None:
         want, new = _mx4_shapes(shape[:-1], cols), _new(X, stream)
         out = MX4(new(want[0], dtype=torch.uint8), new(want[1], dtype=torch.uint8), cols)
+        codes, scales = out.codes.data_ptr(), out.scales.data_ptr()
     elif out.shape != shape:
         raise ValueError("out must be an MX4 of X's shape")
-    codes, scales = _mx4(out, "out", X.device)
+    else:
+        codes, scales = _mx4(out, "out", X.device)
     if rows:
-        _check(load().dass_mx4_quantize(X.data_ptr(), G, rows, cols, ld, strides[0] if len(shape) == 3 else 0, dt, codes, scales,
-                                        _stream_of(X, stream)), "dass_mx4_quantize")
+        _check(load().dass_mx4_quantize(X.data_ptr(), G, rows, cols, ld, group_stride, dt, codes, scales, handle), "dass_mx4_quantize")
     return out
 
 
 def mx4_dequantize(Q: MX4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The values an MX4 stands for, exactly."""
-    if not Q.codes.is_cuda:
+    first, cols = Q.codes, Q.cols
+    if not first.is_cuda:
         raise ValueError("Q must be on a CUDA device")
-    _here(Q.codes, stream)
-    codes, scales = _mx4(Q, "Q", Q.codes.device)
-    shape = Q.shape
-    G, rows, cols = shape if len(shape) == 3 else (1, *shape)
+    handle = _stream_of(first, stream)
+    codes, scales = _mx4(Q, "Q", first.device)
+    lead = first.shape[:-1]
+    G, rows = (lead[0], lead[1]) if len(lead) == 2 else (1, lead[0])
     if out is None:
-        out = _new(Q.codes, stream)(shape, dtype=dtype)
-    elif out.shape != shape or out.dtype != dtype or out.device != Q.codes.device or (out.stride(-1) != 1 and cols > 1):
+        out = _new(first, stream)((*lead, cols), dtype=dtype)
+    elif out.shape != (*lead, cols) or out.dtype != dtype or out.device != first.device or (out.stride(-1) != 1 and cols > 1):
         raise ValueError("out must be a tensor of Q's shape and device and of the dtype asked for, with unit stride along its columns")
     strides, dt = out.stride(), _code(out)
     ld = strides[-2] if rows > 1 or strides[-2] > cols else cols
     if rows:
-        _check(load().dass_mx4_dequantize(codes, scales, G, rows, cols, out.data_ptr(), ld, strides[0] if len(shape) == 3 else 0, dt,
-                                          _stream_of(Q.codes, stream)), "dass_mx4_dequantize")
+        _check(load().dass_mx4_dequantize(codes, scales, G, rows, cols, out.data_ptr(), ld, strides[0] if len(lead) == 2 else 0, dt, handle),
+               "dass_mx4_dequantize")
     return out
 
 
@@ -977,6 +987,10 @@ def linear_mx4_workspace_bytes(T: int, K: int, N: int, groups: int = 1, has_offs
     _check(load().dass_linear_mx4_workspace_bytes(int(T), int(K), int(N), int(groups), int(has_offsets), int(has_up), int(x_in_4_bits),
                                                   ctypes.byref(out)), "dass_linear_mx4_workspace_bytes")
     return int(out.value)
+
+
+# The choice of kernel behind it is the same for equal sizes and goes by the device's SMs.
+_linear_mx4_bytes = functools.lru_cache(maxsize=4096)(lambda device, *sizes: linear_mx4_workspace_bytes(*sizes))
 
 
 def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, W_up: Optional[MX4] = None,
@@ -989,10 +1003,10 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
     [G x N x K], as for linear().  ``Y`` may be the residual itself."""
     quantized = isinstance(X, MX4)
     if quantized:
-        first = X.codes
-        if first.dim() != 2 or not first.is_cuda:
+        first, ldx, x = X.codes, 0, None
+        if len(first.shape) != 2 or not first.is_cuda:
             raise ValueError("X must be an MX4 of [T x K] on a CUDA device")
-        (T, K), ldx, x = X.shape, 0, None
+        T, K = first.shape[0], X.cols
         xc, xs = _mx4(X, "X", first.device)
     else:
         first = X
@@ -1001,13 +1015,13 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
             raise TypeError(f"unsupported dtype {X.dtype}: linear_mx4 takes bfloat16 rows or an MX4")
         x, xc, xs = X.data_ptr(), None, None
     device, dtype = first.device, torch.bfloat16
-    shape = W.shape
-    if len(shape) != (2 if offsets is None else 3) or shape[-1] != K:
+    shape = W.codes.shape
+    if len(shape) != (2 if offsets is None else 3) or W.cols != K:
         raise ValueError(f"W must be an MX4 of {'[N x K]' if offsets is None else '[G x N x K]'}")
     wc, ws = _mx4(W, "W", device)
     uc = us = None
     if W_up is not None:
-        if W_up.shape != shape:
+        if W_up.codes.shape != shape or W_up.cols != K:
             raise ValueError("W_up must have W's shape")
         uc, us = _mx4(W_up, "W_up", device)
     N = shape[-2]
@@ -1033,12 +1047,12 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
     else:
         ldy = like(Y, "Y")
     if T:
+        handle = _stream_of(first, stream)
         if workspace is None:
-            need = linear_mx4_workspace_bytes(T, K, N, groups, offsets is not None, W_up is not None, quantized)
+            need = _linear_mx4_bytes(first.get_device(), T, K, N, groups, offsets is not None, W_up is not None, quantized)
             workspace = _new(first, stream)(need, dtype=torch.uint8) if need else None
         else:
             _workspace(workspace, device)
         _check(load().dass_linear_mx4(x, ldx, xc, xs, T, K, wc, ws, uc, us, N, b, bu, act, _ptr(residual), ldr, Y.data_ptr(), ldy, edges,
-                                      groups, _ptr(workspace), workspace.numel() if workspace is not None else 0,
-                                      _stream_of(first, stream)), "dass_linear_mx4")
+                                      groups, _ptr(workspace), workspace.numel() if workspace is not None else 0, handle), "dass_linear_mx4")
     return Y

@@ -6,13 +6,14 @@ tokens the router sends it.
     layer.calibrate(X); norm = layer.finalize()                 # per expert: the neuron norms over its own tokens
     pruned = layer.prune(alpha=0.5)                             # an ExpertLayer with N:M-pruned experts, same router
     Yp, saved = pruned.forward(X, keep=True)
-    dlogits = pruned.router_gradient(dY, saved)                 # what tuning the router around the pruned experts needs
+    dlogits = pruned.router_gradient(dY, saved, balance=0.01)   # what tuning the router around the pruned experts needs
+    small = pruned.quantize()                                   # the same experts in 4 bits a weight
 
 All work runs in the CUDA library; the sequence of its calls is what this file adds.
 """
 from __future__ import annotations
 
-from typing import NamedTuple, Optional
+from typing import NamedTuple, Optional, Union
 
 import torch
 
@@ -36,16 +37,23 @@ class Saved(NamedTuple):
 
 
 class ExpertLayer:
-    """Weights of E experts stacked in one tensor per projection, and their router."""
+    """Weights of E experts stacked in one tensor (or one MX4) per projection, and their router.
 
-    def __init__(self, Wr: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, k: int, act: str = "silu",
-                 renormalise: bool = True, router_bias: Optional[torch.Tensor] = None):
+    With ``rows_in_4_bits`` the rows that meet 4-bit weights are quantised too."""
+
+    def __init__(self, Wr: torch.Tensor, Wg: Union[torch.Tensor, b.MX4], Wu: Union[torch.Tensor, b.MX4], Wd: Union[torch.Tensor, b.MX4], k: int,
+                 act: str = "silu", renormalise: bool = True, router_bias: Optional[torch.Tensor] = None, rows_in_4_bits: bool = False):
         E, I, d = Wg.shape
         if Wu.shape != (E, I, d) or Wd.shape != (E, d, I) or Wr.shape != (E, d):
             raise ValueError("Wr [E x d], Wg and Wu [E x I x d] and Wd [E x d x I] must agree in E, I and d")
         self.E, self.I, self.d, self.k = E, I, d, int(k)
         self.Wr, self.Wg, self.Wu, self.Wd, self.router_bias = Wr, Wg, Wu, Wd, router_bias
         self.act, self.renormalise = b.ACT_BY_NAME[act], bool(renormalise)
+        self.quantized, self.rows_in_4_bits = isinstance(Wg, b.MX4), bool(rows_in_4_bits)
+        if not self.quantized == isinstance(Wu, b.MX4) == isinstance(Wd, b.MX4):
+            raise ValueError("all three projections must be in 4 bits, or none")
+        if self.rows_in_4_bits and not self.quantized:
+            raise ValueError("rows in 4 bits go with weights in 4 bits")
         self.sumsq = torch.zeros((E, I), dtype=torch.float64, device=Wg.device)
         self.norm = torch.zeros((E, I), dtype=torch.float32, device=Wg.device)
         self._finalized = False
@@ -71,18 +79,46 @@ class ExpertLayer:
         an expert's output is 2.3e-3 off the exact one, of which the last rounding alone is 1.7e-3."""
         r = routed if routed is not None else self.route(X)
         Xs = b.expert_gather(X, r.slot, r.offsets)
-        H = b.linear(Xs, self.Wg, act=self.act, W_up=self.Wu, offsets=r.offsets)
-        Ys = b.linear(H, self.Wd, offsets=r.offsets)
+        H = self._product(Xs, self.Wg, r.offsets, act=self.act, W_up=self.Wu)
+        Ys = self._product(H, self.Wd, r.offsets)
         Y = b.expert_combine(Ys, r.slot, r.weight, residual=residual)
         return (Y, Saved(r, Ys)) if keep else Y
 
-    # ------------------------------------------------------------------ the router's gradient
-    def router_gradient(self, dY: torch.Tensor, saved: Saved) -> torch.Tensor:
-        """Gradient of the router's logits [T x E] from that of the layer's output, the experts held fixed.  (Through
-        the router's product it is dWr = dlogits^T X, and dlogits Wr for the layer's input.)"""
+    def _product(self, X: torch.Tensor, W: Union[torch.Tensor, b.MX4], offsets: torch.Tensor, **options) -> torch.Tensor:
+        if not self.quantized:
+            return b.linear(X, W, offsets=offsets, **options)
+        return b.linear_mx4(b.mx4_quantize(X) if self.rows_in_4_bits else X, W, offsets=offsets, **options)
+
+    # ------------------------------------------------------------------ the router's balance and gradient
+    def balance(self, routed: Routed):
+        """(loss, counts, share): the balance loss of a batch's choices (1 for even loads, E for one expert alone), the choices
+        per expert and, last, the tokens that have any, and the mean probability of each expert."""
+        return b.route_balance(routed.logits, routed.expert)
+
+    def router_gradient(self, dY: torch.Tensor, saved: Saved, balance: float = 0.0, counts: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Gradient of the router's logits [T x E] from that of the layer's output, the experts held fixed, plus ``balance``
+        times that of the balance loss.  ``counts`` are the batch's own unless given (summed over several batches or ranks).
+        (Through the router's product it is dWr = dlogits^T X, and dlogits Wr for the layer's input.)"""
         r = saved.routed
         _, dweight = b.expert_combine_backward(dY, saved.Ys, r.slot, r.weight, want_rows=False)
-        return b.route_topk_backward(r.logits, r.expert, dweight, renormalise=self.renormalise)
+        dlogits = b.route_topk_backward(r.logits, r.expert, dweight, renormalise=self.renormalise)
+        if balance:
+            if counts is None:
+                _, counts, _ = self.balance(r)
+            factor = torch.full((), float(balance), dtype=torch.float32, device=dlogits.device)
+            b.route_balance_backward(r.logits, r.expert, counts, dloss=factor, add=dlogits, dlogits=dlogits)
+        return dlogits
+
+    # ------------------------------------------------------------------ 4-bit weights
+    def quantize(self, rows_in_4_bits: bool = False) -> "ExpertLayer":
+        """The layer with its experts in microscaled 4-bit values (a quarter of the bytes; what pruning set to zero stays zero).
+        With ``rows_in_4_bits`` tokens and intermediate rows are quantised as well, which the 4-bit tensor pipe needs."""
+        if self.quantized:
+            raise RuntimeError("the experts are in 4 bits already")
+        out = ExpertLayer(self.Wr, *(b.mx4_quantize(W) for W in (self.Wg, self.Wu, self.Wd)), self.k, renormalise=self.renormalise,
+                          router_bias=self.router_bias, rows_in_4_bits=rows_in_4_bits)
+        out.act = self.act
+        return out
 
     # ------------------------------------------------------------------ calibration and pruning
     def reset(self) -> None:
@@ -92,6 +128,8 @@ class ExpertLayer:
     def calibrate(self, X: torch.Tensor, routed: Optional[Routed] = None) -> list:
         """Adds a batch of tokens to every expert's neuron sums: the tokens routed to an expert are its calibration set.
         Returns the tokens per expert.  (Waits for the device once: the calibration calls take their sizes on the host.)"""
+        if self.quantized:
+            raise RuntimeError("calibrate the layer before its experts are quantised")
         r = routed if routed is not None else self.route(X)
         Xs = b.expert_gather(X, r.slot, r.offsets)
         edges = r.offsets.tolist()
@@ -114,6 +152,8 @@ class ExpertLayer:
     def prune(self, alpha: float = 0.5, n_keep: int = 2, m: int = 4) -> "ExpertLayer":
         """A layer with every expert's projections pruned N:M by the norms of the last finalize(): Eq. 4 with ``alpha`` on
         gate and up, Eq. 5 on down.  An expert that had no tokens then has no norms: it is pruned by magnitude alone."""
+        if self.quantized:
+            raise RuntimeError("prune the layer before its experts are quantised")
         if not self._finalized:
             raise RuntimeError("prune() needs the norms of a finalize()")
         out = ExpertLayer(self.Wr, torch.empty_like(self.Wg), torch.empty_like(self.Wu), torch.empty_like(self.Wd), self.k,

@@ -142,3 +142,16 @@ class LayerPruner:
         if self._forward_ws is None or self._forward_ws.numel() != nbytes:
             self._forward_ws = b.mlp_forward_workspace(nbytes, self.device)
         return b.mlp_forward(X, Wg, Wu, Wd, self.act, Z=Z, workspace=self._forward_ws)
+
+    # ------------------------------------------------------------------ the pruned layer in 4 bits
+    def quantize_pruned(self) -> Dict[str, b.MX4]:
+        """The pruned copies the last prune() / score_nm() / select_unstructured() wrote, in microscaled 4-bit values: zeros stay
+        zeros, what is left takes 4.25 bits a weight."""
+        return {name: b.mx4_quantize(self.out[name]["pruned"]) for name in _PROJECTIONS}
+
+    def forward_quantized(self, X: torch.Tensor, weights: Dict[str, b.MX4], rows_in_4_bits: bool = False) -> torch.Tensor:
+        """The layer's output (Eq. 2 then Eq. 3) for weights in 4 bits, the intermediate rounded to bfloat16 as forward_with
+        rounds it; with ``rows_in_4_bits`` the rows of both products are quantised too."""
+        rows = b.mx4_quantize if rows_in_4_bits else lambda x: x
+        H = b.linear_mx4(rows(X), weights["gate"], act=self.act, W_up=weights["up"])
+        return b.linear_mx4(rows(H), weights["down"])
