@@ -78,6 +78,15 @@ __device__ __forceinline__ void mq_floats(const MqRaw<BF16, VECTOR> &r, float *t
     }
 }
 
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// The scale of a block from its largest value's exponent field: 255 where it holds a NaN or an infinity.
+__device__ __forceinline__ uint32_t mq_scale(uint32_t e) { return e == 255u ? 255u : e > 2u ? e - 2u : 0u; }
+
 template <bool BF16, bool VECTOR>
 __global__ void __launch_bounds__(MQ_THREADS)
 mx4_quantize_kernel(const void *__restrict__ X, int64_t rows, int64_t K, int64_t ldx, int64_t group_stride,
@@ -99,20 +108,37 @@ mx4_quantize_kernel(const void *__restrict__ X, int64_t rows, int64_t K, int64_t
                 mq_load<BF16, VECTOR>(raw[i], X, g * group_stride + (r0 + i) * ldx, c0, lane, r0 + i < rows ? K : 0);
 #pragma unroll
             for (int i = 0; i < MQ_ROWS; ++i) {
-                float v[8];
-                mq_floats<BF16, VECTOR>(raw[i], turn[VECTOR ? 0 : warp], lane, v);
-                uint32_t most = 0u;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
-                most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
-                most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
-                const uint32_t e = most >> 23;
-                const uint32_t s = e == 255u ? 255u : e > 2u ? e - 2u : 0u;
-                const float up = __uint_as_float((254u - s) << 23);
+                uint32_t s;
                 float y[8];
+                if constexpr (BF16 && VECTOR) {
+                    // two values to a word: maximum and product by a power of two of both halves at once
+                    const uint32_t w[4] = {raw[i].piece[0].w.x, raw[i].piece[0].w.y, raw[i].piece[0].w.z, raw[i].piece[0].w.w};
+                    uint32_t most = max_u16x2(max_u16x2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_u16x2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+                    most = max_u16x2(most, __shfl_xor_sync(FULL_MASK, most, 1));
+                    most = max_u16x2(most, __shfl_xor_sync(FULL_MASK, most, 2));
+                    const uint32_t e = max(most >> 23, (most >> 7) & 255u);
+                    s = mq_scale(e);
+                    const uint32_t up = e == 255u ? 0u : (254u - s) * 0x00800080u;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = v[j] * up;
-                const uint32_t packed = e == 255u ? 0u : mx4_encode8(y);
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t p = mul_bf16x2(w[j], up);
+                        y[2 * j] = __uint_as_float(p << 16);
+                        y[2 * j + 1] = __uint_as_float(p & 0xffff0000u);
+                    }
+                } else {
+                    float v[8];
+                    mq_floats<BF16, VECTOR>(raw[i], turn[VECTOR ? 0 : warp], lane, v);
+                    uint32_t most = 0u;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
+                    most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
+                    most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
+                    s = mq_scale(most >> 23);
+                    const float up = __uint_as_float((254u - s) << 23);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = v[j] * up;
+                }
+                const uint32_t packed = s == 255u ? 0u : mx4_encode8(y);
                 if (r0 + i < rows && c < pitch * 2) DASS_ST_CS(reinterpret_cast<uint32_t *>(gcodes + i * pitch), packed);
                 uint32_t word = s << (8 * ((lane >> 2) & 3));
                 word |= __shfl_xor_sync(FULL_MASK, word, 4);
@@ -149,12 +175,17 @@ mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restri
             for (int i = 0; i < MQ_ROWS; ++i) {
                 if (r0 + i >= rows) break;
                 const int64_t at = g * group_stride + (r0 + i) * ldy;
+                // every value is a bf16 number, or past the range of f32 as well
+                uint32_t w[4];
+                mx4_decode8(x[i], mx4_factor(s[i]), mx4_two(s[i]), w);
+                const uint32_t pairs[4] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632)};
                 float v[8];
-                mx4_decode8_f32(x[i], mx4_scale(s[i]), v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(pairs[j] << 16); v[2 * j + 1] = __uint_as_float(pairs[j] & 0xffff0000u); }
                 if constexpr (VECTOR) {
                     if (c + 8 <= K) {
                         if constexpr (BF16) {
-                            row_store<true, 8>(Y, at + c, v);
+                            DASS_ST_CS(reinterpret_cast<uint4 *>(static_cast<uint16_t *>(Y) + at + c), make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]));
                         } else {
                             const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
                             row_store<false, 4>(Y, at + c, a);

@@ -8,8 +8,7 @@
 // maximum and sum crosses lanes.  At the end the groups of a block add up, a block writes one row of partial sums, and a
 // second kernel adds the rows in a fixed order.  Small calls are one block and one launch.  Choices are counted in shared
 // memory; integer sums do not depend on their order.
-#include "rows_common.cuh"
-#include "tc_common.cuh"
+#include "linear_tc.cuh"
 
 namespace dass {
 
@@ -17,11 +16,12 @@ constexpr int RB_THREADS = 512;            // of the loss
 constexpr int RB_BACK_THREADS = 256;       // of the gradient
 constexpr int RB_MAX_E = 1024;
 constexpr int RB_MAX_K = 32;
-constexpr int RB_BLOCKS = 296;             // partial rows at most: two blocks to each of 148 SMs
+constexpr int RB_BLOCKS = 296;             // at most: two to each of 148 SMs
+constexpr int RB_CLUSTER = 8;             // blocks whose sums make one row
 constexpr int RB_ONE_BLOCK = 1 << 14;      // logits that one block takes alone
 
-// -inf and NaN are masked; +inf counts as the largest finite value.
-__device__ __forceinline__ float rb_logit(float x) { return x > -INFINITY ? fminf(x, 3.402823466e38f) : -INFINITY; }
+// -inf and NaN are masked (fmaxf drops a NaN); +inf counts as the largest finite value.
+__device__ __forceinline__ float rb_logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.402823466e38f); }
 
 template <int L> __device__ __forceinline__ float rb_max(float v)
 {
@@ -39,17 +39,18 @@ template <int L> __device__ __forceinline__ float rb_sum(float v)
 // The column of a lane's element i * W + c.
 template <int L, int W> __device__ __forceinline__ int rb_col(int gl, int i) { return (i * L + gl) * W; }
 
+// FULL: the row has exactly the group's V L columns.  Else columns past E are absent.
 // A row as it lies in memory, all of its loads in flight before the first is used; absent columns hold bits that
 // rb_floats does not look at.
 template <bool BF16, int W, int V> struct RbRow { RowRaw<BF16, W> piece[V / W]; RowRaw<BF16, 1> tail[W > 1 ? W : 1]; };
 
-template <bool BF16, int W, int V, int L>
+template <bool BF16, int W, int V, int L, bool FULL>
 __device__ __forceinline__ void rb_load(RbRow<BF16, W, V> &r, const void *logits, int64_t row, int gl, int E)
 {
 #pragma unroll
     for (int i = 0; i < V / W; ++i) {
         const int e = rb_col<L, W>(gl, i);
-        if (e + W <= E) raw_load<BF16, W>(r.piece[i], logits, row + e);
+        if (FULL || e + W <= E) raw_load<BF16, W>(r.piece[i], logits, row + e);
         else if (W > 1 && e < E) {                                     // the one ragged piece of the row
 #pragma unroll
             for (int c = 0; c < W; ++c)
@@ -58,7 +59,7 @@ __device__ __forceinline__ void rb_load(RbRow<BF16, W, V> &r, const void *logits
     }
 }
 // The row's masked logits; absent columns are -inf.
-template <bool BF16, int W, int V, int L>
+template <bool BF16, int W, int V, int L, bool FULL>
 __device__ __forceinline__ void rb_floats(const RbRow<BF16, W, V> &r, int gl, int E, float (&x)[V])
 {
 #pragma unroll
@@ -66,7 +67,7 @@ __device__ __forceinline__ void rb_floats(const RbRow<BF16, W, V> &r, int gl, in
         const int e = rb_col<L, W>(gl, i);
         float v[W];
         raw_floats<BF16, W>(r.piece[i], v);
-        if (W > 1 && e < E && e + W > E) {
+        if (!FULL && W > 1 && e < E && e + W > E) {
 #pragma unroll
             for (int c = 0; c < W; ++c) {
                 float one[1];
@@ -75,7 +76,7 @@ __device__ __forceinline__ void rb_floats(const RbRow<BF16, W, V> &r, int gl, in
             }
         }
 #pragma unroll
-        for (int c = 0; c < W; ++c) x[i * W + c] = e + c < E ? rb_logit(v[c]) : -INFINITY;
+        for (int c = 0; c < W; ++c) x[i * W + c] = FULL || e + c < E ? rb_logit(v[c]) : -INFINITY;
     }
 }
 
@@ -87,10 +88,11 @@ __device__ __forceinline__ float rb_softmax(float (&x)[V])
 #pragma unroll
     for (int i = 1; i < V; ++i) top = fmaxf(top, x[i]);
     top = rb_max<L>(top);
+    top = top > -INFINITY ? top : 0.f;                               // nothing unmasked: every exponential is 0
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        x[i] = x[i] > -INFINITY ? expf(x[i] - top) : 0.f;
+        x[i] = expf(x[i] - top);
         sum += x[i];
     }
     sum = rb_sum<L>(sum);
@@ -103,26 +105,29 @@ template <int L>
 __device__ __forceinline__ void rb_load_ids(int (&id)[RB_IDS<L>], const int32_t *expert, int64_t t, int k, int gl, bool live)
 {
 #pragma unroll
-    for (int i = 0; i < RB_IDS<L>; ++i) id[i] = live && gl + i * L < k ? DASS_LD(expert + t * k + gl + i * L) : -1;
+    for (int i = 0; i < RB_IDS<L>; ++i) {
+        id[i] = -1;
+        if (i * L < k && live && gl + i * L < k) id[i] = DASS_LD(expert + t * k + gl + i * L);
+    }
 }
 // Whether the token has a choice inside [0, E), for all lanes of its group; COUNT: the choices are counted too.
 template <int L, bool COUNT>
 __device__ __forceinline__ bool rb_chosen(const int (&id)[RB_IDS<L>], const int32_t *expert, int64_t t, int k, int E, int gl, bool live, int *count)
 {
-    int any = 0;
+    bool any = false;
     auto look = [&](int e) {
         if (e >= 0 && e < E) {
-            any = 1;
+            any = true;
             if (COUNT) atomicAdd(count + e, 1);
         }
     };
 #pragma unroll
-    for (int i = 0; i < RB_IDS<L>; ++i) look(id[i]);
+    for (int i = 0; i < RB_IDS<L>; ++i)
+        if (i * L < k) look(id[i]);
     if (live)
         for (int j = gl + RB_IDS<L> * L; j < k; j += L) look(DASS_LD(expert + t * k + j));
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) any |= __shfl_xor_sync(FULL_MASK, any, o);
-    return any != 0;
+    const unsigned group = (L == 32 ? FULL_MASK : ((1u << (L & 31)) - 1u)) << (threadIdx.x & 31 & ~(L - 1));
+    return (__ballot_sync(FULL_MASK, any) & group) != 0u;
 }
 
 // loss, share and the last count from sums and counts; called by a whole block with both complete in shared memory.
@@ -149,11 +154,11 @@ __device__ __forceinline__ void rb_finish(const float *sum, const int *count, in
     }
 }
 
-// One row of partial sums and counts per block (partial null: the only block, which finishes).
-template <bool BF16, int W, int V, int L>
-__global__ void __launch_bounds__(RB_THREADS)
+// One row of partial sums and counts per cluster of blocks (partial null: the only block, which finishes).
+template <bool BF16, int W, int V, int L, bool FULL>
+__global__ void __launch_bounds__(RB_THREADS, V <= 16 ? 2 : 1)
 route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, const int32_t *__restrict__ expert,
-                     float *__restrict__ partial, int32_t *__restrict__ partial_counts, float *loss, int32_t *counts, float *share)
+                     float *__restrict__ partial, int32_t *__restrict__ partial_counts, float *loss, int32_t *counts, float *share, int cluster)
 {
     constexpr int TOKENS = RB_THREADS / L, WARPS = RB_THREADS / 32;
     extern __shared__ float rb_smem[];
@@ -166,32 +171,23 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
     int seen = 0;
-    const int64_t rounds = (T + TOKENS - 1) / TOKENS;               // every lane takes part in every round of its warp
-    RbRow<BF16, W, V> next;
-    int next_id[RB_IDS<L>];
-    auto fetch = [&](int64_t r) {                                   // the next round's loads run under this one's arithmetic
-        const int64_t t = r * TOKENS + threadIdx.x / L;
-        const bool live = r < rounds && t < T;
-        rb_load<BF16, W, V, L>(next, logits, (live ? t : 0) * ld, gl, live ? E : 0);
-        rb_load_ids<L>(next_id, expert, t, k, gl, live);
-    };
-    fetch(blockIdx.x);
-    for (int64_t r = blockIdx.x; r < rounds; r += gridDim.x) {
-        const int64_t t = r * TOKENS + threadIdx.x / L;
+    const int rounds = (int)((T + TOKENS - 1) / TOKENS);            // every lane takes part in every round of its warp
+    for (int r = blockIdx.x; r < rounds; r += gridDim.x) {
+        const int64_t t = (int64_t)r * TOKENS + threadIdx.x / L;
         const bool live = t < T;
-        float x[V];
+        RbRow<BF16, W, V> row;
         int id[RB_IDS<L>];
-        rb_floats<BF16, W, V, L>(next, gl, live ? E : 0, x);
-#pragma unroll
-        for (int i = 0; i < RB_IDS<L>; ++i) id[i] = next_id[i];
-        fetch(r + gridDim.x);
+        float x[V];
+        rb_load<BF16, W, V, L, FULL>(row, logits, (live ? t : 0) * ld, gl, E);
+        rb_load_ids<L>(id, expert, t, k, gl, live);
+        rb_floats<BF16, W, V, L, FULL>(row, gl, E, x);
         const bool in = rb_chosen<L, true>(id, expert, t, k, E, gl, live, count);
-        const float inv = rb_softmax<V, L>(x) * (in ? 1.f : 0.f);
+        const float inv = rb_softmax<V, L>(x) * (in ? 1.f : 0.f);   // a row past the last has no choice
         seen += in && gl == 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], inv, acc[i]);
     }
-    // over the groups of a warp, then over the warps, in order
+    // over the groups of a warp, then over the warps, then over the cluster's blocks, in order
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
@@ -210,15 +206,31 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
         float s = sums[e];
 #pragma unroll
         for (int w = 1; w < WARPS; ++w) s += sums[w * E + e];
-        if (partial) DASS_ST(partial + (int64_t)blockIdx.x * E + e, s);
-        else sums[e] = s;
+        sums[e] = s;
     }
-    if (partial) {
-        for (int e = threadIdx.x; e <= E; e += RB_THREADS) DASS_ST(partial_counts + (int64_t)blockIdx.x * (E + 1) + e, (int32_t)count[e]);
+    if (!partial) {
+        __syncthreads();
+        rb_finish(sums, count, E, k, loss, counts, share);
         return;
     }
-    __syncthreads();
-    rb_finish(sums, count, E, k, loss, counts, share);
+    __syncwarp();                                                    // the cluster barrier wants whole warps
+    if (cluster > 1) cluster_sync_all(); else __syncthreads();
+    const int rank = (int)(blockIdx.x % cluster);
+    const int64_t out = blockIdx.x / cluster;
+    const uint32_t sums_addr = smem_u32(sums), count_addr = smem_u32(count);
+    for (int e = threadIdx.x + rank * RB_THREADS; e < 2 * E + 1; e += cluster * RB_THREADS) {
+        if (e < E) {
+            float s = 0.f;
+            for (int r = 0; r < cluster; ++r) s += cluster > 1 ? ld_cluster(map_to_cta(sums_addr + 4 * e, r)) : sums[e];
+            DASS_ST(partial + out * E + e, s);
+        } else {
+            int c = 0;
+            for (int r = 0; r < cluster; ++r) c += cluster > 1 ? __float_as_int(ld_cluster(map_to_cta(count_addr + 4 * (e - E), r))) : count[e - E];
+            DASS_ST(partial_counts + out * (E + 1) + e - E, (int32_t)c);
+        }
+    }
+    __syncwarp();
+    if (cluster > 1) cluster_sync_all();                             // the others may still read this block's sums
 }
 
 // The rows of partial sums added up: warps take rows in turn, lanes columns.
@@ -256,8 +268,8 @@ route_balance_finish_kernel(const float *__restrict__ partial, const int32_t *__
 }
 
 // dlogits = add + dloss * E/n p (f - sum f p); 0 + add for tokens without a choice.
-template <bool BF16, int W, int V, int L>
-__global__ void __launch_bounds__(RB_BACK_THREADS)
+template <bool BF16, int W, int V, int L, bool FULL>
+__global__ void __launch_bounds__(RB_BACK_THREADS, V <= 16 ? 4 : 2)
 route_balance_backward_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, const int32_t *__restrict__ expert,
                               const int32_t *__restrict__ counts, const float *__restrict__ dloss, const void *add, int64_t lda,
                               void *dlogits, int64_t ldd)
@@ -273,16 +285,16 @@ route_balance_backward_kernel(const void *__restrict__ logits, int64_t T, int E,
         const int e = rb_col<L, W>(gl, i / W) + i % W;
         f[i] = e < E ? (float)DASS_LD(counts + e) * inverse / (float)k : 0.f;
     }
-    const int64_t rounds = (T + TOKENS - 1) / TOKENS;
-    for (int64_t r = blockIdx.x; r < rounds; r += gridDim.x) {
-        const int64_t t = r * TOKENS + threadIdx.x / L;
+    const int rounds = (int)((T + TOKENS - 1) / TOKENS);
+    for (int r = blockIdx.x; r < rounds; r += gridDim.x) {
+        const int64_t t = (int64_t)r * TOKENS + threadIdx.x / L;
         const bool live = t < T;
         RbRow<BF16, W, V> row;
         int id[RB_IDS<L>];
         float x[V];
-        rb_load<BF16, W, V, L>(row, logits, (live ? t : 0) * ld, gl, live ? E : 0);
+        rb_load<BF16, W, V, L, FULL>(row, logits, (live ? t : 0) * ld, gl, E);
         rb_load_ids<L>(id, expert, t, k, gl, live);
-        rb_floats<BF16, W, V, L>(row, gl, live ? E : 0, x);
+        rb_floats<BF16, W, V, L, FULL>(row, gl, E, x);
         const bool in = rb_chosen<L, false>(id, expert, t, k, E, gl, live, nullptr);
         const float inv = rb_softmax<V, L>(x);
         float dot = 0.f;
@@ -297,7 +309,7 @@ route_balance_backward_kernel(const void *__restrict__ logits, int64_t T, int E,
             float y[W];
 #pragma unroll
             for (int c = 0; c < W; ++c) y[c] = in ? g * x[i * W + c] * (f[i * W + c] - dot) : 0.f;
-            if (e + W <= E) {
+            if (FULL || e + W <= E) {
                 if (add) {
                     float a[W];
                     row_load<BF16, W>(add, t * lda + e, a);
@@ -323,39 +335,57 @@ struct BalanceArgs {
     const void *logits; int64_t T; int E; int64_t ld; int k; const int32_t *expert;
     float *partial; int32_t *partial_counts; float *loss; int32_t *counts; float *share;              // forward
     const int32_t *load; const float *dloss; const void *add; int64_t lda; void *dlogits; int64_t ldd;   // backward (dlogits not null)
-    bool vector; int blocks; cudaStream_t st;
+    bool vector; int blocks, cluster; cudaStream_t st;
 };
 
 int device_sm_count();   // dass_abi.cu
 
-// Blocks that share T tokens: enough to fill the SMs, one for what one block does sooner than a second launch.
+// Blocks that share T tokens: enough to fill the SMs, one for what one block does sooner than a second launch; and how many
+// of them add up in a cluster, which leaves the second kernel fewer rows.
 static int rb_blocks(int64_t T, int64_t E)
 {
     if (T * E <= RB_ONE_BLOCK) return 1;
     const int64_t lanes = E <= 8 ? 1 : E <= 16 ? 2 : E <= 32 ? 4 : E <= 128 ? 8 : E <= 256 ? 16 : 32;
     const int64_t rounds = (T * lanes + RB_THREADS - 1) / RB_THREADS;
-    return (int)(rounds < RB_BLOCKS ? rounds : RB_BLOCKS);
+    const int64_t blocks = rounds < RB_BLOCKS ? rounds : RB_BLOCKS;
+    return (int)(blocks < RB_CLUSTER ? blocks : blocks / RB_CLUSTER * RB_CLUSTER);
 }
+static int rb_cluster(int blocks) { return blocks >= RB_CLUSTER ? RB_CLUSTER : 1; }
 
-template <bool BF16, int W, int V, int L>
-static cudaError_t rb_launch(const BalanceArgs &a)
+template <bool BF16, int W, int V, int L, bool FULL>
+static cudaError_t rb_go(const BalanceArgs &a)
 {
     if (a.dlogits) {
         constexpr int TOKENS = RB_BACK_THREADS / L;
         const int64_t rounds = (a.T + TOKENS - 1) / TOKENS, most = 8 * (int64_t)device_sm_count();
-        route_balance_backward_kernel<BF16, W, V, L><<<(unsigned)(rounds < most ? rounds : most), RB_BACK_THREADS, 0, a.st>>>(
+        route_balance_backward_kernel<BF16, W, V, L, FULL><<<(unsigned)(rounds < most ? rounds : most), RB_BACK_THREADS, 0, a.st>>>(
             a.logits, a.T, a.E, a.ld, a.k, a.expert, a.load, a.dloss, a.add, a.lda, a.dlogits, a.ldd);
         return cudaGetLastError();
     }
     const size_t smem = ((size_t)(RB_THREADS / 32) * a.E + a.E + 1) * 4;       // at most 68 KB
     if (smem > 48 * 1024) {                                                      // E above 722
         static DeviceMask configured{0ull};                                      // per device
-        const cudaError_t e = ensure_dynamic_smem(route_balance_kernel<BF16, W, V, L>, 68 * 1024 + 8, configured);
+        const cudaError_t e = ensure_dynamic_smem(route_balance_kernel<BF16, W, V, L, FULL>, 68 * 1024 + 8, configured);
         if (e != cudaSuccess) return e;
     }
-    route_balance_kernel<BF16, W, V, L><<<a.blocks, RB_THREADS, smem, a.st>>>(a.logits, a.T, a.E, a.ld, a.k, a.expert, a.partial,
-                                                                             a.partial_counts, a.loss, a.counts, a.share);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.blocks);
+    cfg.blockDim = dim3(RB_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = a.st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, route_balance_kernel<BF16, W, V, L, FULL>, a.logits, a.T, a.E, a.ld, a.k, a.expert, a.partial, a.partial_counts,
+                              a.loss, a.counts, a.share, a.cluster);
+}
+template <bool BF16, int W, int V, int L>
+static cudaError_t rb_launch(const BalanceArgs &a)
+{
+    return a.E == V * L ? rb_go<BF16, W, V, L, true>(a) : rb_go<BF16, W, V, L, false>(a);
 }
 template <bool BF16, bool VECTOR>
 static cudaError_t rb_pick(const BalanceArgs &a)
@@ -385,8 +415,8 @@ static dass_status rb_check(int64_t T, int64_t E, int64_t ld, int dt, int64_t k)
 }
 static size_t rb_workspace(int64_t T, int64_t E)
 {
-    const int64_t blocks = rb_blocks(T, E);
-    return blocks > 1 ? (size_t)blocks * (2 * E + 1) * 4 : 0;
+    const int blocks = rb_blocks(T, E);
+    return blocks > 1 ? (size_t)(blocks / rb_cluster(blocks)) * (2 * E + 1) * 4 : 0;
 }
 
 }  // namespace dass
@@ -420,11 +450,13 @@ dass_status dass_route_balance(const void *logits, int64_t T, int64_t E, int64_t
     a.logits = logits; a.T = T; a.E = (int)E; a.ld = ld; a.k = (int)k; a.expert = expert;
     a.loss = loss; a.counts = counts; a.share = share;
     a.blocks = rb_blocks(T, E);
+    a.cluster = rb_cluster(a.blocks);
+    const int partial_rows = a.blocks / a.cluster;
     a.vector = rows_vec_ok(logits, ld, bf16);
     a.st = static_cast<cudaStream_t>(cuda_stream);
     if (a.blocks > 1) {
         a.partial = static_cast<float *>(workspace);
-        a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (int64_t)a.blocks * E);
+        a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (int64_t)partial_rows * E);
     }
     DASS_BOUNDS_SCOPE(bs);
     if (T > 0) {
@@ -439,7 +471,7 @@ dass_status dass_route_balance(const void *logits, int64_t T, int64_t E, int64_t
     if (rb_dispatch(a, bf16) != cudaSuccess) return DASS_ERR_CUDA;
     if (a.blocks > 1) {
         const int deep = 1024 / (int)E;                              // E <= 1024
-        route_balance_finish_kernel<<<1, 1024, (size_t)deep * (2 * E + 1) * 4, a.st>>>(a.partial, a.partial_counts, a.blocks, (int)E, (int)k,
+        route_balance_finish_kernel<<<1, 1024, (size_t)deep * (2 * E + 1) * 4, a.st>>>(a.partial, a.partial_counts, partial_rows, (int)E, (int)k,
                                                                                       loss, counts, share);
         if (cudaGetLastError() != cudaSuccess) return DASS_ERR_CUDA;
     }
