@@ -62,6 +62,7 @@ struct SplitArgs {
 __global__ void __launch_bounds__(128)
 mx4_split_kernel(const SplitArgs a)
 {
+    grid_dependents_launch();
     const int lane = threadIdx.x & 31;
     const LinTile tile = lin_find_tile(a.offsets, a.groups, a.T, a.rows, blockIdx.y);
     if (tile.g < 0 || tile.lo + blockIdx.z >= tile.hi) return;
@@ -175,32 +176,45 @@ mx4_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     const int64_t items = (int64_t)table[p.groups] * p.col_tiles;
-    Mx4Item it;
+    Mx4Item it{};
     bool ok = true;
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
         uint32_t stage = 0, phase = 0;
         const uint64_t pol_w = l2_policy_evict_first(), pol_x = l2_policy_evict_last();
+        auto load_w = [&](uint32_t at, uint32_t full, int kb) {
+            const int w_tile = it.g * p.w_tiles + it.col / MX4_TILE_ROWS;
+            mbar_arrive_expect_tx(full, S::STAGE);
+            tma_load_3d_hint(at, &map_w, full, kb * (MS_BK / 2), it.col, it.g, pol_w);
+            tma_load_3d_hint(at + MS_W_BYTES, &map_ws, full, 0, kb * 2, w_tile, pol_w);
+            if constexpr (GLU) {
+                tma_load_3d_hint(at + MS_W_BYTES + MS_SCALES, &map_up, full, kb * (MS_BK / 2), it.col, it.g, pol_w);
+                tma_load_3d_hint(at + 2 * MS_W_BYTES + MS_SCALES, &map_us, full, 0, kb * 2, w_tile, pol_w);
+            }
+        };
+        // The ring's first weights are on their way before the split rows are there.
+        int early = 0;
+        if (SPLIT && mx4_item(table, p.groups, p.align, p.rows, p.col_tiles, MS_COLS, blockIdx.x, it)) {
+            early = p.k_stages < STAGES ? p.k_stages : STAGES;
+            if (elect_one())
+                for (int kb = 0; kb < early; ++kb) load_w(base + kb * S::STAGE, bar_full + 8 * kb, kb);
+            __syncwarp();
+        }
+        if (SPLIT) grid_dependency_wait();
         for (int64_t idx = blockIdx.x; ok && mx4_item(table, p.groups, p.align, p.rows, p.col_tiles, MS_COLS, idx, it); idx += gridDim.x) {
             const int x_tile = SPLIT ? it.tile : it.row / MX4_TILE_ROWS;
-            const int w_tile = it.g * p.w_tiles + it.col / MX4_TILE_ROWS;
             for (int kb = 0; kb < p.k_stages; ++kb) {
                 if (!warp_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
                 const uint32_t sbase = base + stage * S::STAGE, full = bar_full + 8 * stage;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(full, S::STAGE);
-                    tma_load_3d_hint(sbase, &map_w, full, kb * (MS_BK / 2), it.col, it.g, pol_w);
-                    tma_load_3d_hint(sbase + MS_W_BYTES, &map_ws, full, 0, kb * 2, w_tile, pol_w);
-                    if constexpr (GLU) {
-                        tma_load_3d_hint(sbase + MS_W_BYTES + MS_SCALES, &map_up, full, kb * (MS_BK / 2), it.col, it.g, pol_w);
-                        tma_load_3d_hint(sbase + 2 * MS_W_BYTES + MS_SCALES, &map_us, full, 0, kb * 2, w_tile, pol_w);
-                    }
+                    if (early == 0) load_w(sbase, full, kb);
                     if constexpr (SPLIT) tma_load_3d_hint(sbase + S::X_AT, &map_x, full, kb * (MS_BK / 2), 0, it.tile, pol_x);
                     else tma_load_3d_hint(sbase + S::X_AT, &map_x, full, kb * (MS_BK / 2), it.row, 0, pol_x);
                     tma_load_3d_hint(sbase + S::X_AT + NT * (MS_BK / 2), &map_xs, full, 0, kb * 2, x_tile, pol_x);
                 }
                 __syncwarp();
+                if (early > 0) --early;
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
         }
@@ -333,6 +347,7 @@ static cudaError_t ms_launch(const MsMaps &m, const MsParams &p, int act, int gr
     static DeviceMask configured{0ull};               // per device
     const cudaError_t ce = ensure_dynamic_smem(mx4_mid_kernel<NT, GLU, SPLIT>, (int)MsShape<NT, GLU>::BYTES, configured);
     if (ce != cudaSuccess) return ce;
+    if (SPLIT) return launch_dependent(mx4_mid_kernel<NT, GLU, SPLIT>, dim3(grid), dim3(MS_THREADS), MsShape<NT, GLU>::BYTES, st, m.x, m.w, m.up, m.xs, m.ws, m.us, p, act);
     mx4_mid_kernel<NT, GLU, SPLIT><<<grid, MS_THREADS, MsShape<NT, GLU>::BYTES, st>>>(m.x, m.w, m.up, m.xs, m.ws, m.us, p, act);
     return cudaGetLastError();
 }

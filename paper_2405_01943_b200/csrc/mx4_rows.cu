@@ -87,65 +87,150 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
 // The scale of a block from its largest value's exponent field: 255 where it holds a NaN or an infinity.
 __device__ __forceinline__ uint32_t mq_scale(uint32_t e) { return e == 255u ? 255u : e > 2u ? e - 2u : 0u; }
 
+// MQ_ROWS rows of 8 values a lane.  INSIDE: all rows and columns exist and are read 16 bytes at a time.
+template <bool BF16, bool VECTOR, bool INSIDE>
+__device__ __forceinline__ void mq_encode(const char *src, int64_t row_bytes, int64_t c0, int64_t rows, int64_t K, int lane, float *turn,
+                                          uint8_t *codes, int64_t pitch, uint8_t *scales, int64_t scale_cols)
+{
+    constexpr int ES = BF16 ? 2 : 4;
+    const int64_t c = c0 + lane * 8;
+    MqRaw<BF16, VECTOR> raw[MQ_ROWS];
+#pragma unroll
+    for (int i = 0; i < MQ_ROWS; ++i) {
+        const char *row = src + i * row_bytes;
+        if constexpr (INSIDE) {
+            constexpr int W = ROW_VEC<BF16>;
+#pragma unroll
+            for (int j = 0; j < 8 / W; ++j) raw[i].piece[j].w = DASS_LD_CS(reinterpret_cast<const uint4 *>(row + (lane * 8 + j * W) * ES));
+        } else {
+            mq_load<BF16, VECTOR>(raw[i], row - c0 * ES, 0, c0, lane, i < rows ? K : 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MQ_ROWS; ++i) {
+        uint32_t s;
+        float y[8];
+        if constexpr (BF16 && VECTOR) {
+            // two values to a word: maximum and product by a power of two of both halves at once
+            const uint32_t w[4] = {raw[i].piece[0].w.x, raw[i].piece[0].w.y, raw[i].piece[0].w.z, raw[i].piece[0].w.w};
+            uint32_t most = max_u16x2(max_u16x2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_u16x2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+            most = max_u16x2(most, __shfl_xor_sync(FULL_MASK, most, 1));
+            most = max_u16x2(most, __shfl_xor_sync(FULL_MASK, most, 2));
+            s = mq_scale(max(most >> 23, (most >> 7) & 255u));
+            const uint32_t up = s == 255u ? 0u : (254u - s) * 0x00800080u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t p = mul_bf16x2(w[j], up);
+                y[2 * j] = __uint_as_float(p << 16);
+                y[2 * j + 1] = __uint_as_float(p & 0xffff0000u);
+            }
+        } else {
+            float v[8];
+            mq_floats<BF16, VECTOR>(raw[i], turn, lane, v);
+            uint32_t most = 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
+            most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
+            most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
+            s = mq_scale(most >> 23);
+            const float up = __uint_as_float((254u - s) << 23);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = v[j] * up;
+        }
+        const uint32_t packed = s == 255u ? 0u : mx4_encode8(y);
+        if (INSIDE || (i < rows && c < pitch * 2)) DASS_ST_CS(reinterpret_cast<uint32_t *>(codes + i * pitch), packed);
+        uint32_t word = s << (8 * ((lane >> 2) & 3));
+        word |= __shfl_xor_sync(FULL_MASK, word, 4);
+        word |= __shfl_xor_sync(FULL_MASK, word, 8);
+        if ((lane & 15) == 0 && (INSIDE || c < scale_cols)) DASS_ST(reinterpret_cast<uint32_t *>(scales + i * 16), word);   // the four rows' slots are neighbours
+    }
+}
+
 template <bool BF16, bool VECTOR>
 __global__ void __launch_bounds__(MQ_THREADS)
 mx4_quantize_kernel(const void *__restrict__ X, int64_t rows, int64_t K, int64_t ldx, int64_t group_stride,
                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, const MqGrid q)
 {
-    __shared__ float turn[VECTOR ? 1 : MQ_WARPS][VECTOR ? 4 : MQ_COLS];
+    constexpr int ES = BF16 ? 2 : 4;
+    __shared__ __align__(16) float turn[VECTOR ? 1 : MQ_WARPS][VECTOR ? 4 : MQ_COLS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float *const mine = turn[VECTOR ? 0 : warp];
     const int64_t c0 = ((int64_t)blockIdx.x * q.across + (warp & (q.across - 1))) * MQ_COLS, c = c0 + lane * 8;
     const int64_t pitch = mx4_pitch(K), k_tiles = mx4_k_tiles(K);
-    const int64_t first = (int64_t)blockIdx.y * (MQ_WARPS / q.across) + warp / q.across;
-    for (int64_t g = blockIdx.z; g < q.groups; g += gridDim.z)
-        for (int64_t rg = first; rg < q.row_groups; rg += (int64_t)gridDim.y * (MQ_WARPS / q.across)) {
-            const int64_t r0 = rg * MQ_ROWS;
-            uint8_t *const gcodes = codes + (g * rows + r0) * pitch + c / 2;
-            uint8_t *const gscales = scales + g * mx4_row_tiles(rows) * k_tiles * MX4_TILE_BYTES + mx4_scale_word(r0, c / MX4_TILE_K, k_tiles);
-            MqRaw<BF16, VECTOR> raw[MQ_ROWS];
+    const int64_t first = (int64_t)blockIdx.y * (MQ_WARPS / q.across) + warp / q.across, step = (int64_t)gridDim.y * (MQ_WARPS / q.across);
+    for (int64_t g = blockIdx.z; g < q.groups; g += gridDim.z) {
+        const char *src = static_cast<const char *>(X) + (g * group_stride + first * MQ_ROWS * ldx + c0) * ES;
+        uint8_t *dst = codes + (g * rows + first * MQ_ROWS) * pitch + c / 2;
+        uint8_t *const gscales = scales + (g * mx4_row_tiles(rows) * k_tiles + c / MX4_TILE_K) * MX4_TILE_BYTES;
+        for (int64_t rg = first; rg < q.row_groups; rg += step, src += step * MQ_ROWS * ldx * ES, dst += step * MQ_ROWS * pitch) {
+            uint8_t *const word = gscales + mx4_scale_word(rg * MQ_ROWS, 0, k_tiles);
+            if (VECTOR && c0 + MQ_COLS <= K && rg * MQ_ROWS + MQ_ROWS <= rows)
+                mq_encode<BF16, VECTOR, VECTOR>(src, ldx * ES, c0, MQ_ROWS, K, lane, mine, dst, pitch, word, k_tiles * MX4_TILE_K);
+            else
+                mq_encode<BF16, VECTOR, false>(src, ldx * ES, c0, rows - rg * MQ_ROWS, K, lane, mine, dst, pitch, word, k_tiles * MX4_TILE_K);
+        }
+    }
+}
+
+// The four rows again, decoded.  INSIDE as above, for Y.
+template <bool BF16, bool VECTOR, bool INSIDE>
+__device__ __forceinline__ void mq_decode(const uint8_t *codes, int64_t pitch, const uint8_t *scales, int64_t c0, int64_t rows, int64_t K, int lane,
+                                          float *turn, char *dst, int64_t row_bytes)
+{
+    constexpr int ES = BF16 ? 2 : 4;
+    const int64_t c = c0 + lane * 8;
+    uint32_t x[MQ_ROWS], s[MQ_ROWS];
 #pragma unroll
-            for (int i = 0; i < MQ_ROWS; ++i)
-                mq_load<BF16, VECTOR>(raw[i], X, g * group_stride + (r0 + i) * ldx, c0, lane, r0 + i < rows ? K : 0);
+    for (int i = 0; i < MQ_ROWS; ++i) {
+        const bool in = INSIDE || (i < rows && c < K);
+        x[i] = in ? DASS_LD_CS(reinterpret_cast<const uint32_t *>(codes + i * pitch)) : 0u;
+        s[i] = in ? DASS_LD(scales + i * 16) : 0u;
+    }
 #pragma unroll
-            for (int i = 0; i < MQ_ROWS; ++i) {
-                uint32_t s;
-                float y[8];
-                if constexpr (BF16 && VECTOR) {
-                    // two values to a word: maximum and product by a power of two of both halves at once
-                    const uint32_t w[4] = {raw[i].piece[0].w.x, raw[i].piece[0].w.y, raw[i].piece[0].w.z, raw[i].piece[0].w.w};
-                    uint32_t most = max_u16x2(max_u16x2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_u16x2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
-                    most = max_u16x2(most, __shfl_xor_sync(FULL_MASK, most, 1));
-                    most = max_u16x2(most, __shfl_xor_sync(FULL_MASK, most, 2));
-                    const uint32_t e = max(most >> 23, (most >> 7) & 255u);
-                    s = mq_scale(e);
-                    const uint32_t up = e == 255u ? 0u : (254u - s) * 0x00800080u;
+    for (int i = 0; i < MQ_ROWS; ++i) {
+        if (!INSIDE && i >= rows) break;
+        char *const row = dst + i * row_bytes;                         // column c0
+        // every value is a bf16 number, or past the range of f32 as well
+        uint32_t w[4];
+        mx4_decode8(x[i], mx4_factor(s[i]), mx4_two(s[i]), w);
+        const uint32_t pairs[4] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632)};
+        uint4 *const at = reinterpret_cast<uint4 *>(row + lane * 8 * ES);
+        if constexpr (VECTOR && BF16) {
+            if (INSIDE || c + 8 <= K) {
+                DASS_ST_CS(at, make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]));
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t p = mul_bf16x2(w[j], up);
-                        y[2 * j] = __uint_as_float(p << 16);
-                        y[2 * j + 1] = __uint_as_float(p & 0xffff0000u);
-                    }
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < K) DASS_ST(reinterpret_cast<uint16_t *>(at) + j, (uint16_t)(pairs[j / 2] >> (16 * (j & 1))));
+            }
+        } else {
+            uint32_t v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { v[2 * j] = pairs[j] << 16; v[2 * j + 1] = pairs[j] & 0xffff0000u; }
+            if constexpr (VECTOR) {
+                if (INSIDE || c + 8 <= K) {
+                    DASS_ST(at, make_uint4(v[0], v[1], v[2], v[3]));     // half a sector each: they meet in the cache
+                    DASS_ST(at + 1, make_uint4(v[4], v[5], v[6], v[7]));
                 } else {
-                    float v[8];
-                    mq_floats<BF16, VECTOR>(raw[i], turn[VECTOR ? 0 : warp], lane, v);
-                    uint32_t most = 0u;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
-                    most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
-                    most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
-                    s = mq_scale(most >> 23);
-                    const float up = __uint_as_float((254u - s) << 23);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = v[j] * up;
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < K) DASS_ST(reinterpret_cast<uint32_t *>(at) + j, v[j]);
                 }
-                const uint32_t packed = s == 255u ? 0u : mx4_encode8(y);
-                if (r0 + i < rows && c < pitch * 2) DASS_ST_CS(reinterpret_cast<uint32_t *>(gcodes + i * pitch), packed);
-                uint32_t word = s << (8 * ((lane >> 2) & 3));
-                word |= __shfl_xor_sync(FULL_MASK, word, 4);
-                word |= __shfl_xor_sync(FULL_MASK, word, 8);
-                if ((lane & 15) == 0 && c < k_tiles * MX4_TILE_K) DASS_ST(reinterpret_cast<uint32_t *>(gscales + i * 16), word);   // the four rows' slots are neighbours
+            } else {
+                *reinterpret_cast<uint4 *>(turn + lane * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<uint4 *>(turn + lane * 8 + 4) = make_uint4(v[4], v[5], v[6], v[7]);
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t one = __float_as_uint(turn[j * 32 + lane]);
+                    if (c0 + j * 32 + lane >= K) continue;
+                    if constexpr (BF16) DASS_ST(reinterpret_cast<uint16_t *>(row) + j * 32 + lane, (uint16_t)(one >> 16));
+                    else DASS_ST(reinterpret_cast<uint32_t *>(row) + j * 32 + lane, one);
+                }
+                __syncwarp();
             }
         }
+    }
 }
 
 template <bool BF16, bool VECTOR>
@@ -153,66 +238,28 @@ __global__ void __launch_bounds__(MQ_THREADS)
 mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int64_t K,
                       void *__restrict__ Y, int64_t ldy, int64_t group_stride, const MqGrid q)
 {
-    __shared__ float turn[VECTOR ? 1 : MQ_WARPS][VECTOR ? 4 : MQ_COLS];
+    constexpr int ES = BF16 ? 2 : 4;
+    __shared__ __align__(16) float turn[VECTOR ? 1 : MQ_WARPS][VECTOR ? 4 : MQ_COLS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float *const mine = turn[VECTOR ? 0 : warp];
     const int64_t c0 = ((int64_t)blockIdx.x * q.across + (warp & (q.across - 1))) * MQ_COLS, c = c0 + lane * 8;
     const int64_t pitch = mx4_pitch(K), k_tiles = mx4_k_tiles(K);
-    const int64_t first = (int64_t)blockIdx.y * (MQ_WARPS / q.across) + warp / q.across;
-    for (int64_t g = blockIdx.z; g < q.groups; g += gridDim.z)
-        for (int64_t rg = first; rg < q.row_groups; rg += (int64_t)gridDim.y * (MQ_WARPS / q.across)) {
-            const int64_t r0 = rg * MQ_ROWS;
-            const uint8_t *const gcodes = codes + (g * rows + r0) * pitch + c / 2;
-            const uint8_t *const gscales = scales + g * mx4_row_tiles(rows) * k_tiles * MX4_TILE_BYTES + mx4_scale_word(r0, c / MX4_TILE_K, k_tiles) +
-                                           ((c / MX4_BLOCK) & 3);
-            uint32_t x[MQ_ROWS], s[MQ_ROWS];
-#pragma unroll
-            for (int i = 0; i < MQ_ROWS; ++i) {
-                const bool in = r0 + i < rows && c < K;
-                x[i] = in ? DASS_LD_CS(reinterpret_cast<const uint32_t *>(gcodes + i * pitch)) : 0u;
-                s[i] = in ? DASS_LD(gscales + i * 16) : 0u;
-            }
-#pragma unroll
-            for (int i = 0; i < MQ_ROWS; ++i) {
-                if (r0 + i >= rows) break;
-                const int64_t at = g * group_stride + (r0 + i) * ldy;
-                // every value is a bf16 number, or past the range of f32 as well
-                uint32_t w[4];
-                mx4_decode8(x[i], mx4_factor(s[i]), mx4_two(s[i]), w);
-                const uint32_t pairs[4] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632)};
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(pairs[j] << 16); v[2 * j + 1] = __uint_as_float(pairs[j] & 0xffff0000u); }
-                if constexpr (VECTOR) {
-                    if (c + 8 <= K) {
-                        if constexpr (BF16) {
-                            DASS_ST_CS(reinterpret_cast<uint4 *>(static_cast<uint16_t *>(Y) + at + c), make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]));
-                        } else {
-                            const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-                            row_store<false, 4>(Y, at + c, a);
-                            row_store<false, 4>(Y, at + c + 4, b);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float one[1] = {v[j]};
-                            if (c + j < K) row_store<BF16, 1>(Y, at + c + j, one);
-                        }
-                    }
-                } else {
-                    float *const mine = turn[warp];
-                    *reinterpret_cast<float4 *>(mine + lane * 8) = make_float4(v[0], v[1], v[2], v[3]);
-                    *reinterpret_cast<float4 *>(mine + lane * 8 + 4) = make_float4(v[4], v[5], v[6], v[7]);
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float one[1] = {mine[j * 32 + lane]};
-                        if (c0 + j * 32 + lane < K) row_store<BF16, 1>(Y, at + c0 + j * 32 + lane, one);
-                    }
-                    __syncwarp();
-                }
-            }
+    const int64_t first = (int64_t)blockIdx.y * (MQ_WARPS / q.across) + warp / q.across, step = (int64_t)gridDim.y * (MQ_WARPS / q.across);
+    for (int64_t g = blockIdx.z; g < q.groups; g += gridDim.z) {
+        char *dst = static_cast<char *>(Y) + (g * group_stride + first * MQ_ROWS * ldy + c0) * ES;
+        const uint8_t *src = codes + (g * rows + first * MQ_ROWS) * pitch + c / 2;
+        const uint8_t *const gscales = scales + (g * mx4_row_tiles(rows) * k_tiles + c / MX4_TILE_K) * MX4_TILE_BYTES + ((c / MX4_BLOCK) & 3);
+        for (int64_t rg = first; rg < q.row_groups; rg += step, src += step * MQ_ROWS * pitch, dst += step * MQ_ROWS * ldy * ES) {
+            const uint8_t *const byte = gscales + mx4_scale_word(rg * MQ_ROWS, 0, k_tiles);
+            if (VECTOR && c0 + MQ_COLS <= K && rg * MQ_ROWS + MQ_ROWS <= rows)
+                mq_decode<BF16, VECTOR, VECTOR>(src, pitch, byte, c0, MQ_ROWS, K, lane, mine, dst, ldy * ES);
+            else
+                mq_decode<BF16, VECTOR, false>(src, pitch, byte, c0, rows - rg * MQ_ROWS, K, lane, mine, dst, ldy * ES);
         }
+    }
 }
+
+int device_sm_count();   // dass_abi.cu
 
 static dass_status mq_check(int64_t groups, int64_t rows, int64_t K, int64_t ld, int64_t group_stride, int dt)
 {
@@ -229,8 +276,11 @@ static dim3 mq_grid(int64_t groups, int64_t padded_rows, int64_t K, MqGrid &q)
     q.across = chunks >= 4 ? 4 : chunks >= 2 ? 2 : 1;
     q.row_groups = (padded_rows + MQ_ROWS - 1) / MQ_ROWS;
     q.groups = groups;
-    const int64_t y = (q.row_groups + MQ_WARPS / q.across - 1) / (MQ_WARPS / q.across);
-    return dim3((unsigned)((chunks + q.across - 1) / q.across), (unsigned)(y < 65535 ? y : 65535), (unsigned)(groups < 65535 ? groups : 65535));
+    const int64_t x = (chunks + q.across - 1) / q.across, z = groups < 65535 ? groups : 65535;
+    int64_t y = (q.row_groups + MQ_WARPS / q.across - 1) / (MQ_WARPS / q.across);
+    const int64_t turns = x * y * z / (32 * (int64_t)device_sm_count());   // a block's set-up is spread over up to 8 groups of rows
+    y = (y + (turns < 1 ? 1 : turns < 8 ? turns : 8) - 1) / (turns < 1 ? 1 : turns < 8 ? turns : 8);
+    return dim3((unsigned)x, (unsigned)(y < 65535 ? y : 65535), (unsigned)z);
 }
 
 }  // namespace dass

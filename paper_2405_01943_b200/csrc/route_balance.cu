@@ -165,6 +165,7 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
     float *sums = rb_smem;                                          // [WARPS x E], then the block's in the first row
     int *count = reinterpret_cast<int *>(rb_smem + WARPS * E);      // [E + 1]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = threadIdx.x & (L - 1);
+    if (partial) grid_dependents_launch();                           // the second kernel may take its place and wait there
     for (int e = threadIdx.x; e <= E; e += RB_THREADS) count[e] = 0;
     __syncthreads();
     float acc[V];
@@ -239,6 +240,7 @@ route_balance_finish_kernel(const float *__restrict__ partial, const int32_t *__
                             float *loss, int32_t *counts, float *share)
 {
     extern __shared__ float rb_smem[];
+    grid_dependency_wait();                                          // the partial sums
     const int lanes = E < 1024 ? E : 1024;                           // threads of a row
     const int deep = 1024 / lanes;                                   // rows at a time
     float *sums = rb_smem;                                           // [deep x E]
@@ -471,9 +473,9 @@ dass_status dass_route_balance(const void *logits, int64_t T, int64_t E, int64_t
     if (rb_dispatch(a, bf16) != cudaSuccess) return DASS_ERR_CUDA;
     if (a.blocks > 1) {
         const int deep = 1024 / (int)E;                              // E <= 1024
-        route_balance_finish_kernel<<<1, 1024, (size_t)deep * (2 * E + 1) * 4, a.st>>>(a.partial, a.partial_counts, partial_rows, (int)E, (int)k,
-                                                                                      loss, counts, share);
-        if (cudaGetLastError() != cudaSuccess) return DASS_ERR_CUDA;
+        if (launch_dependent(route_balance_finish_kernel, dim3(1), dim3(1024), (size_t)deep * (2 * E + 1) * 4, a.st, (const float *)a.partial,
+                             (const int32_t *)a.partial_counts, partial_rows, (int)E, (int)k, loss, counts, share) != cudaSuccess)
+            return DASS_ERR_CUDA;
     }
     return DASS_OK;
 }
