@@ -21,6 +21,24 @@ __host__ __device__ __forceinline__ Mx4Matrix mx4_group(const Mx4Matrix &m, int6
     return {m.codes + g * N * mx4_pitch(K), m.scales + g * ((N + MX4_TILE_ROWS - 1) / MX4_TILE_ROWS) * mx4_k_tiles(K) * MX4_TILE_BYTES};
 }
 
+// ------------------------------------------------------------------ waits of the warp that issues the products
+// A wait that finds its barrier complete still takes 130 cycles, as long as a short slab's products.  So the issuing warp
+// asks for the next stage's barrier before it issues this one's products, and looks at the answer after them.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// A ring's place: stage and the parity of its barriers' phase.
+struct Mx4Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void step(uint32_t stages) { if (++stage == stages) { stage = 0; phase ^= 1u; } }
+};
+
 // ------------------------------------------------------------------ descriptors of the block-scaled products
 // Descriptor of 32 rows of 16 bytes, one after the other, for tcgen05.cp: 8-row groups 128 bytes apart, no swizzle.
 __device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr)

@@ -220,15 +220,19 @@ mx4_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ scale copies and MMAs
-        uint32_t stage = 0, phase = 0, tile = 0, slot = 0;
+        Mx4Ring r;
+        uint32_t tile = 0, slot = 0;
+        bool ready = false;
         for (int64_t idx = blockIdx.x; ok && idx < items; idx += gridDim.x, ++tile) {
             const uint32_t as = tile % S::ACCS;
             if (!warp_wait(acc_empty + 8 * as, ((tile / S::ACCS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-            tc_fence_after();
             const uint32_t acc = tmem_base + as * (M * NT);
             for (int kb = 0; kb < p.k_stages; ++kb) {
-                if (!warp_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                if (!ready && !warp_wait(bar_full + 8 * r.stage, r.phase, abort_flag)) { ok = false; break; }
                 tc_fence_after();
+                const uint32_t stage = r.stage;
+                r.step(STAGES);
+                const bool next = mbar_test(bar_full + 8 * r.stage, r.phase);
                 const uint32_t sbase = base + stage * S::STAGE;
                 const uint32_t sfx = tmem_base + MS_SF_COL + slot * S::SF_COLS, sfw = sfx + 8;
                 if (elect_one()) {
@@ -252,8 +256,7 @@ mx4_mid_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     umma_commit(bar_empty + 8 * stage);
                     if (kb + 1 == p.k_stages) umma_commit(acc_full + 8 * as);
                 }
-                __syncwarp();
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                ready = __all_sync(FULL_MASK, next);
                 if (++slot == MS_SF_SLOTS) slot = 0;
             }
         }

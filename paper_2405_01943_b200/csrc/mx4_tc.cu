@@ -164,17 +164,20 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     } else if (warp == 1) {
         // ------------------------------------------------------------ scale copies and MMAs (leader CTA only)
         if (rank == 0) {
-            uint32_t stage = 0, phase = 0, tile = 0;
-            bool ok = true;
+            Mx4Ring r;
+            uint32_t tile = 0;
+            bool ok = true, ready = false;
             const int64_t items = (int64_t)first_tile[p.groups] * p.col_tiles;
             for (int64_t idx = pair; ok && idx < items; idx += pairs, ++tile) {
                 const uint32_t as = tile % S::ACCS;
                 if (!warp_wait(bar_acc_empty + 8 * as, ((tile / S::ACCS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                tc_fence_after();
                 const uint32_t acc_addr = tmem_base + as * BN;
                 for (int kb = 0; kb < p.k_stages; ++kb) {
-                    if (!warp_wait(bar_full + 8 * stage, phase, abort_flag)) { ok = false; break; }
+                    if (!ready && !warp_wait(bar_full + 8 * r.stage, r.phase, abort_flag)) { ok = false; break; }
                     tc_fence_after();
+                    const uint32_t stage = r.stage;
+                    r.step(STAGES);
+                    const bool next = mbar_test(bar_full + 8 * r.stage, r.phase);
                     const uint32_t sbase = base + stage * S::STAGE, scales = sbase + MT_A_BYTES + S::B_BYTES;
                     const uint32_t sfa = tmem_base + MT_SF_COL + stage * S::SF_COLS, sfb = sfa + 8;
                     if (elect_one()) {
@@ -195,8 +198,7 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                         umma_commit_pair(bar_empty + 8 * stage, (uint16_t)3);   // slot free in both CTAs
                         if (kb + 1 == p.k_stages) umma_commit_pair(bar_acc_full + 8 * as, (uint16_t)3);   // accumulator ready in both CTAs
                     }
-                    __syncwarp();
-                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                    ready = __all_sync(FULL_MASK, next);
                 }
             }
             if (!ok && lane == 0) { *abort_flag = 1; atomicAdd(p.timeouts, 1); }

@@ -201,13 +201,18 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         } else if (warp == 1 && rank == 0) {
             // -------------------------------------------------------- MMA issuer (leader CTA only)
             constexpr uint32_t idesc = idesc_bf16_f32(2 * MW_ROWS, NT);
-            uint32_t xs = 0, xp = 0, as = 0, ap = 0, tile = 0;
+            Mx4Ring x, r;                                         // of X and of the decoded slabs
+            uint32_t tile = 0;
+            bool ready = false;
             for (int64_t idx = pair; ok && idx < items; idx += pairs, ++tile) {
                 if (!warp_wait(acc_empty, (tile & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                tc_fence_after();
                 for (int s = 0; s < p.slabs; ++s) {
-                    if (!warp_wait(x_full + 8 * xs, xp, abort_flag) || !warp_wait(a_full + 8 * as, ap, abort_flag)) { ok = false; break; }
+                    if (!ready && (!warp_wait(x_full + 8 * x.stage, x.phase, abort_flag) || !warp_wait(a_full + 8 * r.stage, r.phase, abort_flag))) { ok = false; break; }
                     tc_fence_after();
+                    const uint32_t xs = x.stage, as = r.stage;
+                    x.step(XS);
+                    r.step(AS);
+                    const bool next_x = mbar_test(x_full + 8 * x.stage, x.phase), next_a = mbar_test(a_full + 8 * r.stage, r.phase);
                     if (elect_one()) {
                         const uint64_t db = smem_desc_sw128(base + xs * S::X_BYTES);
                         const uint32_t ring = tmem_base + MW_RING_COL + as * (32 * M);
@@ -220,9 +225,7 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                         umma_commit_pair(a_empty + 8 * as, (uint16_t)3);
                         if (s + 1 == p.slabs) umma_commit_pair(acc_full, (uint16_t)3);
                     }
-                    __syncwarp();
-                    if (++xs == XS) { xs = 0; xp ^= 1u; }
-                    if (++as == AS) { as = 0; ap ^= 1u; }
+                    ready = __all_sync(FULL_MASK, next_x && next_a);
                 }
             }
         }
