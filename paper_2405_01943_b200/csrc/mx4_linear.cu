@@ -75,7 +75,7 @@ static Mx4Plan mx4_plan(const Mx4Sizes &z)
     for (int r = 64; r <= 256; r *= 2) {
         if (z.glu && r == 256) continue;
         const double items = tiles((double)r, 0.5) * (double)((z.N + 255) / 256);
-        const double t = mx4_rounds(items, sms / 2) * (slabs * (z.glu ? (r == 64 ? 0.47 : 0.50) : r == 256 ? 0.41 : 0.35) + 0.01 * r);
+        const double t = mx4_rounds(items, sms / 2) * (slabs * (z.glu ? (r == 64 ? 0.40 : 0.48) : r == 256 ? 0.36 : 0.29) + 0.01 * r);
         take(6.0 + (t > bytes ? t : bytes), {MX4_WIDE, r, 0, 0});
     }
     return best;

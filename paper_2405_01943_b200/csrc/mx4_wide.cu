@@ -237,8 +237,11 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         const int r = (warp & 3) * 32 + lane;
         const uint32_t lane_addr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + MW_RING_COL;
         const uint32_t leader_full = map_to_cta(a_full, 0);
-        uint32_t ws = 0, wp = 0, as = 0, ap = 0;
-        int stored = -1;                                          // the slab whose store has not been announced: done one slab
+        const int chunk = r & 7;                                  // of the swizzle
+        constexpr int OFF = GLU ? 1 : 2;                          // slabs from one of this warp's units to the next
+        Mx4Ring wr;
+        uint32_t as = 0, ap = 0;                                  // place of a stage's first slab in the ring of decoded ones
+        int stored = -1;                                          // the slab whose store has not been announced: done one unit
         auto announce = [&]() {                                   // later, so that the next one is decoded meanwhile
             if (stored < 0) return;
             tmem_wait_st();
@@ -249,31 +252,42 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         };
         for (int64_t idx = pair; ok && idx < items; idx += pairs) {
             for (int s4 = 0; ok && s4 < w_stages; ++s4) {
-                if (!warp_wait(w_full + 8 * ws, wp, abort_flag)) { ok = false; break; }
-                const uint8_t *codes = aligned + S::W_AT + ws * S::W_BYTES + (GLU ? second * (MW_CODES + MW_SCALES) : 0u);
+                if (!warp_wait(w_full + 8 * wr.stage, wr.phase, abort_flag)) { ok = false; break; }
+                const uint8_t *codes = aligned + S::W_AT + wr.stage * S::W_BYTES + (GLU ? second * (MW_CODES + MW_SCALES) : 0u);
                 const uint8_t *scales = codes + MW_CODES + (r & 31) * 16 + (r >> 5) * 4;
                 const uint32_t sw[2] = {*reinterpret_cast<const uint32_t *>(scales), *reinterpret_cast<const uint32_t *>(scales + MX4_TILE_BYTES)};
+                const int n = p.slabs - 4 * s4 < 4 ? p.slabs - 4 * s4 : 4;                     // slabs of this stage
 #pragma unroll 1
-                for (int s = 0; s < 4; ++s) {
-                    if (4 * s4 + s >= p.slabs) break;
-                    if (GLU || (((4 * s4 + s) & 1) == second)) {
-                        // 16 bytes of this row (a swizzled chunk) and their scale
-                        const uint4 c = *reinterpret_cast<const uint4 *>(codes + r * 128 + (((2 * s + block) ^ (r & 7)) * 16));
-                        const uint32_t e = ((s < 2 ? sw[0] : sw[1]) >> (8 * (2 * (s & 1) + block))) & 255u;
+                for (int half = 0; half < (GLU ? 2 : 1); ++half) {
+                    const int s0 = GLU ? 2 * half : second;       // two units, slabs s0 and s0 + OFF: 16 bytes of this row (a swizzled chunk) each
+                    const uint4 c[2] = {*reinterpret_cast<const uint4 *>(codes + r * 128 + (((2 * s0 + block) ^ chunk) * 16)),
+                                        *reinterpret_cast<const uint4 *>(codes + r * 128 + (((2 * (s0 + OFF) + block) ^ chunk) * 16))};
+                    if (!GLU || half == 1) {                      // this warp has all it needs of the stage
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(w_empty + 8 * wr.stage);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int s = s0 + j * OFF;
+                        if (s >= n) break;
+                        const bool over = as + s >= AS;           // a stage's slabs may go round the ring
+                        const uint32_t at = over ? as + s - AS : as + s, par = over ? ap ^ 1u : ap;
+                        const bool free_now = mbar_test(a_empty + 8 * at, par ^ 1u);
+                        const uint32_t e = ((GLU ? (half ? sw[1] : sw[0]) : sw[j]) >> (8 * (2 * (s & 1) + block))) & 255u;
                         const bool two = __any_sync(FULL_MASK, mx4_two(e));
                         uint32_t out[16];
-                        mw_decode32(c, mx4_factor(e), two, out);
+                        mw_decode32(c[j], mx4_factor(e), two, out);
                         announce();
-                        if (!warp_wait(a_empty + 8 * as, ap ^ 1u, abort_flag)) { ok = false; break; }
+                        if (!__all_sync(FULL_MASK, free_now) && !warp_wait(a_empty + 8 * at, par ^ 1u, abort_flag)) { ok = false; break; }
                         tc_fence_after();
-                        tmem_st_16(lane_addr + as * (32 * M) + (GLU ? second * 32 : 0) + block * 16, out);
-                        stored = (int)as;
+                        tmem_st_16(lane_addr + at * (32 * M) + (GLU ? second * 32 : 0) + block * 16, out);
+                        stored = (int)at;
                     }
-                    if (++as == AS) { as = 0; ap ^= 1u; }
+                    if (!ok) break;
                 }
-                __syncwarp();
-                if (ok && lane == 0) mbar_arrive(w_empty + 8 * ws);
-                if (++ws == WS) { ws = 0; wp ^= 1u; }
+                wr.step(WS);
+                as += n;
+                if (as >= AS) { as -= AS; ap ^= 1u; }
             }
             announce();
         }
