@@ -33,6 +33,12 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
+// Arrives on a barrier of the pair's leader for what is in TMEM: its order is the tcgen05 fence's before it, and there is no
+// memory to be made visible (a release at cluster scope also waits for the warp's stores to Y: 1000 cycles).
+__device__ __forceinline__ void mbar_arrive_tmem(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // A ring's place: stage and the parity of its barriers' phase.
 struct Mx4Ring {
     uint32_t stage = 0, phase = 0;

@@ -237,10 +237,7 @@ mx4_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             tmem_wait_ld();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {                                     // release the accumulator to the leader's MMA warp
-                if (rank == 0) mbar_arrive(bar_acc_empty + 8 * as);
-                else mbar_arrive_cluster(leader_acc_empty + 8 * as);
-            }
+            if (lane == 0) mbar_arrive_tmem(leader_acc_empty + 8 * as);   // release the accumulator to the leader's MMA warp
             if (r_lo >= r_hi) continue;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {

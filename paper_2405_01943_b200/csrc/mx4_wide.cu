@@ -63,12 +63,6 @@ __device__ __forceinline__ void tmem_st_16(uint32_t taddr, const uint32_t (&r)[1
                    "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Arrives on a barrier of the pair's leader for what is in TMEM: its order is the tcgen05 fence's before it, and there is no
-// memory to be made visible (a release at cluster scope costs hundreds of cycles a slab).
-__device__ __forceinline__ void mbar_arrive_tmem(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
 // left operand in TMEM (16-bit elements, two to a column)
 __device__ __forceinline__ void umma_bf16_ts_pair(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
