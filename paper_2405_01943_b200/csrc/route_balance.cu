@@ -17,8 +17,7 @@ constexpr int RB_BACK_THREADS = 256;       // of the gradient
 constexpr int RB_MAX_E = 1024;
 constexpr int RB_MAX_K = 32;
 constexpr int RB_BLOCKS = 296;             // at most: two to each of 148 SMs
-constexpr int RB_CLUSTER = 8;             // blocks whose sums make one row
-constexpr int RB_ONE_BLOCK = 1 << 14;      // logits that one block takes alone
+constexpr int RB_CLUSTER = 8;              // blocks whose sums make one row
 
 // -inf and NaN are masked (fmaxf drops a NaN); +inf counts as the largest finite value.
 __device__ __forceinline__ float rb_logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.402823466e38f); }
@@ -154,7 +153,7 @@ __device__ __forceinline__ void rb_finish(const float *sum, const int *count, in
     }
 }
 
-// One row of partial sums and counts per cluster of blocks (partial null: the only block, which finishes).
+// One row of partial sums and counts per cluster of blocks (partial null: the only cluster, whose first block finishes).
 template <bool BF16, int W, int V, int L, bool FULL>
 __global__ void __launch_bounds__(RB_THREADS, V <= 16 ? 2 : 1)
 route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t ld, int k, const int32_t *__restrict__ expert,
@@ -163,7 +162,7 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
     constexpr int TOKENS = RB_THREADS / L, WARPS = RB_THREADS / 32;
     extern __shared__ float rb_smem[];
     float *sums = rb_smem;                                          // [WARPS x E], then the block's in the first row
-    int *count = reinterpret_cast<int *>(rb_smem + WARPS * E);      // [E + 1]
+    int *count = reinterpret_cast<int *>(rb_smem + WARPS * E);      // [E + 1], then the cluster's
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = threadIdx.x & (L - 1);
     if (partial) grid_dependents_launch();                           // the second kernel may take its place and wait there
     for (int e = threadIdx.x; e <= E; e += RB_THREADS) count[e] = 0;
@@ -209,40 +208,45 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
         for (int w = 1; w < WARPS; ++w) s += sums[w * E + e];
         sums[e] = s;
     }
-    if (!partial) {
-        __syncthreads();
-        rb_finish(sums, count, E, k, loss, counts, share);
-        return;
-    }
     __syncwarp();                                                    // the cluster barrier wants whole warps
     if (cluster > 1) cluster_sync_all(); else __syncthreads();
     const int rank = (int)(blockIdx.x % cluster);
     const int64_t out = blockIdx.x / cluster;
     const uint32_t sums_addr = smem_u32(sums), count_addr = smem_u32(count);
-    for (int e = threadIdx.x + rank * RB_THREADS; e < 2 * E + 1; e += cluster * RB_THREADS) {
+    // the cluster's blocks share the columns of its row, or the first block has them all
+    const int from = partial ? threadIdx.x + rank * RB_THREADS : rank == 0 ? threadIdx.x : 2 * E + 1, by = partial ? cluster * RB_THREADS : RB_THREADS;
+    for (int e = from; cluster > 1 && e < 2 * E + 1; e += by) {
         if (e < E) {
             float s = 0.f;
-            for (int r = 0; r < cluster; ++r) s += cluster > 1 ? ld_cluster(map_to_cta(sums_addr + 4 * e, r)) : sums[e];
-            DASS_ST(partial + out * E + e, s);
+            for (int r = 0; r < cluster; ++r) s += ld_cluster(map_to_cta(sums_addr + 4 * e, r));
+            if (partial) DASS_ST(partial + out * E + e, s);
+            else sums[E + e] = s;                                    // the second warp's place: a block has several
         } else {
             int c = 0;
-            for (int r = 0; r < cluster; ++r) c += cluster > 1 ? __float_as_int(ld_cluster(map_to_cta(count_addr + 4 * (e - E), r))) : count[e - E];
-            DASS_ST(partial_counts + out * (E + 1) + e - E, (int32_t)c);
+            for (int r = 0; r < cluster; ++r) c += __float_as_int(ld_cluster(map_to_cta(count_addr + 4 * (e - E), r)));
+            if (partial) DASS_ST(partial_counts + out * (E + 1) + e - E, (int32_t)c);
+            else count[E + 1 + e - E] = c;                           // past the block's own
         }
     }
     __syncwarp();
     if (cluster > 1) cluster_sync_all();                             // the others may still read this block's sums
+    if (!partial && rank == 0) {
+        if (cluster > 1) rb_finish(sums + E, count + E + 1, E, k, loss, counts, share);
+        else rb_finish(sums, count, E, k, loss, counts, share);
+    }
 }
 
-// The rows of partial sums added up: warps take rows in turn, lanes columns.
+// Rows that the second kernel reads at a time, each by E of its 1024 threads.
+__host__ __device__ __forceinline__ int rb_deep(int E, int rows) { return 1024 / E < rows ? 1024 / E : rows; }
+
+// The rows of partial sums added up.
 __global__ void __launch_bounds__(1024)
 route_balance_finish_kernel(const float *__restrict__ partial, const int32_t *__restrict__ partial_counts, int rows, int E, int k,
                             float *loss, int32_t *counts, float *share)
 {
     extern __shared__ float rb_smem[];
     grid_dependency_wait();                                          // the partial sums
-    const int lanes = E < 1024 ? E : 1024;                           // threads of a row
-    const int deep = 1024 / lanes;                                   // rows at a time
+    const int lanes = E, deep = rb_deep(E, rows);
     float *sums = rb_smem;                                           // [deep x E]
     int *count = reinterpret_cast<int *>(rb_smem + deep * E);        // [deep x (E + 1)]
     const int d = threadIdx.x / lanes, e = threadIdx.x - d * lanes;
@@ -342,17 +346,16 @@ struct BalanceArgs {
 
 int device_sm_count();   // dass_abi.cu
 
-// Blocks that share T tokens: enough to fill the SMs, one for what one block does sooner than a second launch; and how many
-// of them add up in a cluster, which leaves the second kernel fewer rows.
+// Blocks that share T tokens.  Up to three rounds each of one cluster's blocks are done sooner than a second kernel; else
+// enough to fill the SMs, in clusters whose blocks add up, which leaves the second kernel few rows.
 static int rb_blocks(int64_t T, int64_t E)
 {
-    if (T * E <= RB_ONE_BLOCK) return 1;
     const int64_t lanes = E <= 8 ? 1 : E <= 16 ? 2 : E <= 32 ? 4 : E <= 128 ? 8 : E <= 256 ? 16 : 32;
     const int64_t rounds = (T * lanes + RB_THREADS - 1) / RB_THREADS;
-    const int64_t blocks = rounds < RB_BLOCKS ? rounds : RB_BLOCKS;
-    return (int)(blocks < RB_CLUSTER ? blocks : blocks / RB_CLUSTER * RB_CLUSTER);
+    if (rounds <= 3 * RB_CLUSTER) return rounds >= 8 ? 8 : rounds >= 4 ? 4 : rounds >= 2 ? 2 : 1;
+    return (int)((rounds < RB_BLOCKS ? rounds : RB_BLOCKS) / RB_CLUSTER * RB_CLUSTER);
 }
-static int rb_cluster(int blocks) { return blocks >= RB_CLUSTER ? RB_CLUSTER : 1; }
+static int rb_cluster(int blocks) { return blocks < RB_CLUSTER ? blocks : RB_CLUSTER; }
 
 template <bool BF16, int W, int V, int L, bool FULL>
 static cudaError_t rb_go(const BalanceArgs &a)
@@ -364,10 +367,10 @@ static cudaError_t rb_go(const BalanceArgs &a)
             a.logits, a.T, a.E, a.ld, a.k, a.expert, a.load, a.dloss, a.add, a.lda, a.dlogits, a.ldd);
         return cudaGetLastError();
     }
-    const size_t smem = ((size_t)(RB_THREADS / 32) * a.E + a.E + 1) * 4;       // at most 68 KB
-    if (smem > 48 * 1024) {                                                      // E above 722
+    const size_t smem = ((size_t)(RB_THREADS / 32) * a.E + 2 * (a.E + 1)) * 4;   // at most 72 KB
+    if (smem > 48 * 1024) {                                                      // E above 682
         static DeviceMask configured{0ull};                                      // per device
-        const cudaError_t e = ensure_dynamic_smem(route_balance_kernel<BF16, W, V, L, FULL>, 68 * 1024 + 8, configured);
+        const cudaError_t e = ensure_dynamic_smem(route_balance_kernel<BF16, W, V, L, FULL>, 72 * 1024 + 8, configured);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
@@ -418,7 +421,7 @@ static dass_status rb_check(int64_t T, int64_t E, int64_t ld, int dt, int64_t k)
 static size_t rb_workspace(int64_t T, int64_t E)
 {
     const int blocks = rb_blocks(T, E);
-    return blocks > 1 ? (size_t)(blocks / rb_cluster(blocks)) * (2 * E + 1) * 4 : 0;
+    return blocks > RB_CLUSTER ? (size_t)(blocks / RB_CLUSTER) * (2 * E + 1) * 4 : 0;
 }
 
 }  // namespace dass
@@ -456,7 +459,7 @@ dass_status dass_route_balance(const void *logits, int64_t T, int64_t E, int64_t
     const int partial_rows = a.blocks / a.cluster;
     a.vector = rows_vec_ok(logits, ld, bf16);
     a.st = static_cast<cudaStream_t>(cuda_stream);
-    if (a.blocks > 1) {
+    if (a.blocks > RB_CLUSTER) {
         a.partial = static_cast<float *>(workspace);
         a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (int64_t)partial_rows * E);
     }
@@ -471,8 +474,8 @@ dass_status dass_route_balance(const void *logits, int64_t T, int64_t E, int64_t
     DASS_BOUNDS_ADD(bs, workspace, need);
     DASS_BOUNDS_COMMIT(bs, a.st);
     if (rb_dispatch(a, bf16) != cudaSuccess) return DASS_ERR_CUDA;
-    if (a.blocks > 1) {
-        const int deep = 1024 / (int)E;                              // E <= 1024
+    if (a.blocks > RB_CLUSTER) {
+        const int deep = rb_deep((int)E, partial_rows);
         if (launch_dependent(route_balance_finish_kernel, dim3(1), dim3(1024), (size_t)deep * (2 * E + 1) * 4, a.st, (const float *)a.partial,
                              (const int32_t *)a.partial_counts, partial_rows, (int)E, (int)k, loss, counts, share) != cudaSuccess)
             return DASS_ERR_CUDA;
