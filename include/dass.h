@@ -395,7 +395,9 @@ dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int
  * bf16 rows meet the weights as they are, or, where few of them meet many weights, as sums of 4-bit rows that hold every
  * value of a block of 32 to 2^-24 of the largest in it; those rows go to the workspace: dass_linear_mx4_workspace_bytes(..)
  * bytes (may be 0), 16-byte aligned.  groups = 1 and has_offsets = 0 for a dense product.
- * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (X in both forms; limits of dass_linear) / WORKSPACE / CUDA. */
+ * (There a row's block that holds a NaN or an infinity is NaN.)
+ * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (X in both forms; more than 2^26 rows; other limits of dass_linear) /
+ * WORKSPACE / CUDA. */
 dass_status dass_linear_mx4_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t groups, int has_offsets, int has_up, int x_in_4_bits,
                                             size_t *bytes /* HOST */);
 dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, const uint8_t *x_scales, int64_t T, int64_t K,

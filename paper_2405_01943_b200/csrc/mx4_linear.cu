@@ -87,7 +87,7 @@ static size_t mx4_workspace(const Mx4Sizes &z, const Mx4Plan &p)
 static bool mx4_too_large(int64_t T, int64_t K, int64_t N, int64_t groups)
 {
     const int64_t lim = 0x7fffffffll - 512;                // 32-bit tile coordinates
-    const int64_t most_rows = 1ll << 28;                   // so are sums of tile counts, whatever the offsets hold
+    const int64_t most_rows = 1ll << 26;                   // so are sums of the counts of 64-row tiles, whatever the offsets hold
     return T > most_rows || K > lim || N > lim || groups > LIN_MAX_GROUPS;
 }
 

@@ -88,7 +88,7 @@ mx4_split_kernel(const SplitArgs a)
         most = max(most, __shfl_xor_sync(FULL_MASK, most, 1));
         most = max(most, __shfl_xor_sync(FULL_MASK, most, 2));
         // the scale that takes the largest value into (3, 6], so that none is cut: one more where its mantissa is above 1.5
-        const uint32_t e = (most + 0x003fffffu) >> 23;
+        const uint32_t up_e = (most + 0x003fffffu) >> 23, e = up_e < 254u ? up_e : 254u;   // 6 x 2^125 is still a number
         bad |= most >= 0x7f800000u;                                    // NaN or infinity: the whole block is NaN, in its first piece
         const uint32_t s = bad ? (j == 0 ? 255u : 0u) : e > 2u ? e - 2u : 0u;
         const float up = __uint_as_float((254u - (bad ? 127u : s)) << 23), down = mx4_scale(bad ? 127u : s);

@@ -217,13 +217,19 @@ route_balance_kernel(const void *__restrict__ logits, int64_t T, int E, int64_t 
     const int from = partial ? threadIdx.x + rank * RB_THREADS : rank == 0 ? threadIdx.x : 2 * E + 1, by = partial ? cluster * RB_THREADS : RB_THREADS;
     for (int e = from; cluster > 1 && e < 2 * E + 1; e += by) {
         if (e < E) {
-            float s = 0.f;
-            for (int r = 0; r < cluster; ++r) s += ld_cluster(map_to_cta(sums_addr + 4 * e, r));
+            float v[RB_CLUSTER], s = 0.f;                            // all loads in flight, then their sum in order
+#pragma unroll
+            for (int r = 0; r < RB_CLUSTER; ++r) v[r] = r < cluster ? ld_cluster(map_to_cta(sums_addr + 4 * e, r)) : 0.f;
+#pragma unroll
+            for (int r = 0; r < RB_CLUSTER; ++r) s += v[r];
             if (partial) DASS_ST(partial + out * E + e, s);
             else sums[E + e] = s;                                    // the second warp's place: a block has several
         } else {
-            int c = 0;
-            for (int r = 0; r < cluster; ++r) c += __float_as_int(ld_cluster(map_to_cta(count_addr + 4 * (e - E), r)));
+            int v[RB_CLUSTER], c = 0;
+#pragma unroll
+            for (int r = 0; r < RB_CLUSTER; ++r) v[r] = r < cluster ? __float_as_int(ld_cluster(map_to_cta(count_addr + 4 * (e - E), r))) : 0;
+#pragma unroll
+            for (int r = 0; r < RB_CLUSTER; ++r) c += v[r];
             if (partial) DASS_ST(partial_counts + out * (E + 1) + e - E, (int32_t)c);
             else count[E + 1 + e - E] = c;                           // past the block's own
         }

@@ -271,6 +271,22 @@ def test_nan_and_infinity_in_rows_that_are_split():
     assert bool(torch.isfinite(Y[0]).all()) and not bool(torch.isfinite(Y[1:]).any())
 
 
+def test_values_at_the_end_of_the_range_in_rows_that_are_split():
+    X = _randn((2, 4096), 1)
+    X[0, 5], X[0, 700], X[1, 33] = 3.38e38, -3.2e38, 2.0 ** -133
+    W = b.mx4_quantize(_randn((14336, 4096), 2, 2.0 ** -20))
+    assert b.linear_mx4_workspace_bytes(2, 4096, 14336, has_up=True) > 0
+    ones = torch.zeros((14336, 4096), dtype=BF16, device=DEV)          # the gate: relu(1 * x[7]) is x[7]
+    X[:, 7], ones[:, 7] = 1.0, 1.0
+    Y = b.linear_mx4(X, b.mx4_quantize(ones), act=b.ACT_RELU, W_up=W)
+    x, w = X.double(), b.mx4_dequantize(W, F32).double()
+    want = x @ w.t()
+    amax = x.abs().view(2, 128, 32).amax(2, keepdim=True).expand(2, 128, 32).reshape(2, 4096)
+    bound = (4097 + 12) * 2 * eref.EPS24 * (x.abs() @ w.abs().t()) + 2.0 ** -22 * (amax @ w.abs().t())      # the range's end costs a bit of the 24
+    bound = bound * 1.01 + 2.0 ** -8 * want.abs()
+    assert bool(torch.isfinite(Y).all()) and bool(((Y.double() - want).abs() <= bound).all())
+
+
 @forms
 @pytest.mark.parametrize("T,K,N", [(1, 3, 5), (5, 70, 33), (40, 1001, 131), (260, 133, 390)])
 def test_odd_lengths_and_an_output_off_alignment(T, K, N, both4):
