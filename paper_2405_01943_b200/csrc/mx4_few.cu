@@ -1,7 +1,7 @@
 // dass_linear_mx4 for few rows (a decode step): every weight is read once, 4.25 bits of it, and meets at most 32 rows of X,
 // given in bf16 or in 4 bits.
 //
-// A block of 8 warps owns MT * 16 weight rows (columns of Y); the warps take k in turns of 128.  A lane loads 16 bytes of
+// A block of 8 or 16 warps owns MT * 16 weight rows (columns of Y); the warps take k in turns of 128.  A lane loads 16 bytes of
 // codes of a weight row, which are the 32 k of one scale, and decodes them in registers to bf16 fragments of mma.m16n8k16.
 // A dot product may take its k in any order as long as both sides agree: a word of 8 codes gives pairs (p, p + 4), since
 // those are 16 bits apart, and the rows of X are paired the same way (one byte permutation a word; rows in 4 bits come out
@@ -15,8 +15,6 @@
 
 namespace dass {
 
-constexpr int MF_WARPS = 8;
-constexpr int MF_THREADS = MF_WARPS * 32;
 constexpr int MF_STEP = 128;         // k of a warp's turn: a scale tile
 
 __device__ __forceinline__ void mma_bf16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -36,24 +34,24 @@ __device__ __forceinline__ uint4 mf_load8(const uint16_t *row, int64_t k, int64_
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// NT: rows of X in eights; MT: weight rows in sixteens; XQ: X in 4 bits.  Grid: SPLIT x column tiles x row tiles, clusters
+// NT: rows of X in eights; MT: weight rows in sixteens; XQ: X in 4 bits; WARPS of a block.  Grid: SPLIT x column tiles x row tiles, clusters
 // of SPLIT along x.
-template <int NT, int MT, bool GLU, bool XQ>
-__global__ void __launch_bounds__(MF_THREADS)
+template <int NT, int MT, bool GLU, bool XQ, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32)
 mx4_few_kernel(const Mx4Args p, int col_tiles, int split)
 {
-    constexpr int M = GLU ? 2 : 1;
+    constexpr int M = GLU ? 2 : 1, THREADS = WARPS * 32;
     constexpr int COLS = MT * 16;
     constexpr int SUMS = M * COLS * NT * 8;
-    __shared__ float part[MF_WARPS][SUMS];
+    __shared__ float part[WARPS][SUMS];
     __shared__ float sum[SUMS];
     const LinearArgs &a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, q = lane & 3;
     const int64_t block = blockIdx.x / split;
     const int rank = blockIdx.x - (int)block * split;
-    lin_zero_outside<true>(a.offsets, a.groups, a.T, a.N, a.Y, a.ldy, false, (int64_t)blockIdx.x * MF_THREADS + threadIdx.x,
-                           (int64_t)gridDim.x * MF_THREADS);
+    lin_zero_outside<true>(a.offsets, a.groups, a.T, a.N, a.Y, a.ldy, false, (int64_t)blockIdx.x * THREADS + threadIdx.x,
+                           (int64_t)gridDim.x * THREADS);
     const LinTile tile = lin_find_tile(a.offsets, a.groups, a.T, NT * 8, block / col_tiles);
     if (tile.g < 0) return;                                  // the whole cluster
     const int64_t n0 = (block % col_tiles) * COLS;
@@ -96,7 +94,7 @@ mx4_few_kernel(const Mx4Args p, int col_tiles, int split)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) acc[m][j][i][c] = 0.f;
 
-    for (int64_t kt = rank * MF_WARPS + warp; kt < k_tiles; kt += split * MF_WARPS) {
+    for (int64_t kt = rank * WARPS + warp; kt < k_tiles; kt += split * WARPS) {
         const int64_t k0 = kt * MF_STEP;
         const bool inside = k0 + q * 32 < a.K;                // this lane's block of 32
         const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -176,17 +174,17 @@ mx4_few_kernel(const Mx4Args p, int col_tiles, int split)
                 for (int c = 0; c < 4; ++c)
                     part[warp][(m * NT * 8 + i * 8 + 2 * q + (c & 1)) * COLS + 16 * j + g + 8 * (c >> 1)] = acc[m][j][i][c];
     __syncthreads();
-    for (int o = threadIdx.x; o < SUMS; o += MF_THREADS) {
+    for (int o = threadIdx.x; o < SUMS; o += THREADS) {
         float s = part[0][o];
 #pragma unroll
-        for (int v = 1; v < MF_WARPS; ++v) s += part[v][o];
+        for (int v = 1; v < WARPS; ++v) s += part[v][o];
         sum[o] = s;
     }
     __syncwarp();                                            // the cluster barrier wants whole warps
     if (split > 1) cluster_sync_all(); else __syncthreads();
     const int rows = (int)(tile.hi - tile.lo);
     const uint32_t sum_addr = smem_u32(sum);
-    for (int o = threadIdx.x + rank * MF_THREADS; o < rows * COLS; o += split * MF_THREADS) {
+    for (int o = threadIdx.x + rank * THREADS; o < rows * COLS; o += split * THREADS) {
         const int64_t t = tile.lo + o / COLS, n = n0 + o % COLS;
         if (n >= a.N) continue;
         float s[M];
@@ -215,14 +213,14 @@ mx4_few_kernel(const Mx4Args p, int col_tiles, int split)
     if (split > 1) cluster_sync_all();                       // the others may still read this block's sums
 }
 
-template <int NT, int MT, bool GLU, bool XQ>
+template <int NT, int MT, bool GLU, bool XQ, int WARPS>
 static cudaError_t mf_launch(const Mx4Args &p, int64_t row_tiles, int split)
 {
     const int col_tiles = (int)((p.a.N + MT * 16 - 1) / (MT * 16));
     if (row_tiles * col_tiles * split > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(row_tiles * col_tiles * split));
-    cfg.blockDim = dim3(MF_THREADS);
+    cfg.blockDim = dim3(WARPS * 32);
     cfg.stream = p.a.st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -230,14 +228,22 @@ static cudaError_t mf_launch(const Mx4Args &p, int64_t row_tiles, int split)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, mx4_few_kernel<NT, MT, GLU, XQ>, p, col_tiles, split);
+    return cudaLaunchKernelEx(&cfg, mx4_few_kernel<NT, MT, GLU, XQ, WARPS>, p, col_tiles, split);
+}
+// 16 warps hide the decoding's latency where each of them has two turns of k at least (up to 8 rows, 1 x 4096 x 4096: 6.8 against
+// 7.2 us, 1 x 14336 x 4096 15.2 against 18.2; but 1 x 2048 x 2048 gated 8.3 against 6.4).
+template <int MT, bool GLU, bool XQ>
+static cudaError_t mf_one(const Mx4Args &p, int64_t row_tiles, int split)
+{
+    if (mx4_k_tiles(p.a.K) >= 32 * split) return mf_launch<1, MT, GLU, XQ, 16>(p, row_tiles, split);
+    return mf_launch<1, MT, GLU, XQ, 8>(p, row_tiles, split);
 }
 template <bool GLU, bool XQ>
 static cudaError_t mf_pick(const Mx4Args &p, int64_t row_tiles, int nt, int mt, int split)
 {
-    if (nt == 1) return mt == 2 ? mf_launch<1, 2, GLU, XQ>(p, row_tiles, split) : mf_launch<1, 1, GLU, XQ>(p, row_tiles, split);
-    if (nt == 2) return mf_launch<2, 1, GLU, XQ>(p, row_tiles, split);
-    return mf_launch<4, 1, GLU, XQ>(p, row_tiles, split);
+    if (nt == 1) return mt == 2 ? mf_one<2, GLU, XQ>(p, row_tiles, split) : mf_one<1, GLU, XQ>(p, row_tiles, split);
+    if (nt == 2) return mf_launch<2, 1, GLU, XQ, 8>(p, row_tiles, split);
+    return mf_launch<4, 1, GLU, XQ, 8>(p, row_tiles, split);
 }
 
 // nt: rows of X in eights (1, 2 or 4); mt: weight rows in sixteens (2 only with nt 1); split: blocks that share the contraction
