@@ -256,10 +256,6 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                     const int s0 = GLU ? 2 * half : second;       // two units, slabs s0 and s0 + OFF: 16 bytes of this row (a swizzled chunk) each
                     const uint4 c[2] = {*reinterpret_cast<const uint4 *>(codes + r * 128 + (((2 * s0 + block) ^ chunk) * 16)),
                                         *reinterpret_cast<const uint4 *>(codes + r * 128 + (((2 * (s0 + OFF) + block) ^ chunk) * 16))};
-                    if (!GLU || half == 1) {                      // this warp has all it needs of the stage
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(w_empty + 8 * wr.stage);
-                    }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int s = s0 + j * OFF;
@@ -279,6 +275,11 @@ mx4_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                     }
                     if (!ok) break;
                 }
+                // The stage goes back when its last codes are in TMEM: a load that has only been issued may still read the
+                // memory when the next copy writes it.  The fence orders those reads before the copy's writes.
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(w_empty + 8 * wr.stage);
                 wr.step(WS);
                 as += n;
                 if (as >= AS) { as -= AS; ap ^= 1u; }
