@@ -251,6 +251,18 @@ def _new(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> Callable[..., 
     return t.new_empty if stream is None else lambda shape, dtype=None: _made(stream, t.device, lambda: t.new_empty(shape, dtype=dtype))
 
 
+# torch's allocation of a dense tensor on the current device from its sizes, strides and dtype, without the general dispatch: 0.9
+# instead of 2 us, of which a call of the section below has up to three.  None where a torch version has no such function.
+_cuda_empty = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+
+
+def _empty(t: torch.Tensor, stream: Optional[torch.cuda.Stream], shape: Tuple[int, ...], strides: Tuple[int, ...], dtype: torch.dtype) -> torch.Tensor:
+    """An output of a call on `stream` with tensor t, whose device is the current one (_stream_of has seen to that)."""
+    if stream is None and _cuda_empty is not None and type(t) is torch.Tensor:
+        return _cuda_empty(shape, strides, dtype)
+    return _new(t, stream)(shape, dtype=dtype)
+
+
 def _workspace(t: torch.Tensor, device: torch.device) -> None:
     """Checks a caller's workspace: kernels write to its address."""
     if not t.is_cuda or t.dtype != torch.uint8 or t.device != device or not t.is_contiguous():
@@ -849,30 +861,28 @@ def route_balance(logits: torch.Tensor, expert: torch.Tensor, loss: Optional[tor
     entries outside [0, E) are no choices).  Returns (loss float32 [], counts int32 [E + 1], share float32 [E]): counts[:E]
     choices per expert, counts[E] the tokens with a choice, share the mean probability of each expert over those."""
     T, E, ld = _rows(logits, "logits")
-    dt, dev = _code(logits), logits.device
+    dt, dev, handle = _code(logits), logits.device, _stream_of(logits, stream)
     k = expert.shape[1] if expert.dim() == 2 else -1
     ids = _same(expert, "expert", (T, k), torch.int32, dev)
-    new = _new(logits, stream)
     if loss is None:
-        loss = new((), dtype=torch.float32)
+        loss = _empty(logits, stream, (), (), torch.float32)
     else:
         _same(loss, "loss", (), torch.float32, dev)
     if counts is None:
-        counts = new(E + 1, dtype=torch.int32)
+        counts = _empty(logits, stream, (E + 1,), (1,), torch.int32)
     else:
         _same(counts, "counts", (E + 1,), torch.int32, dev)
     if share is None:
-        share = new(E, dtype=torch.float32)
+        share = _empty(logits, stream, (E,), (1,), torch.float32)
     else:
         _same(share, "share", (E,), torch.float32, dev)
     if workspace is None:
         need = _balance_bytes(T, E)
-        workspace = new(need, dtype=torch.uint8) if need else None
+        workspace = _empty(logits, stream, (need,), (1,), torch.uint8) if need else None
     else:
         _workspace(workspace, dev)
     _check(load().dass_route_balance(logits.data_ptr(), T, E, ld, dt, ids, k, loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
-                                     _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream_of(logits, stream)),
-           "dass_route_balance")
+                                     _ptr(workspace), workspace.numel() if workspace is not None else 0, handle), "dass_route_balance")
     return loss, counts, share
 
 
@@ -888,12 +898,13 @@ def route_balance_backward(logits: torch.Tensor, expert: torch.Tensor, counts: t
     load_ = _same(counts, "counts", (E + 1,), torch.int32, dev)
     scale = _same(dloss, "dloss", (), torch.float32, dev) if dloss is not None else None
     lda = _like(add, "add", T, E, logits) if add is not None else 0
+    handle = _stream_of(logits, stream)
     if dlogits is None:
-        dlogits, ldd = _new(logits, stream)((T, E)), E
+        dlogits, ldd = _empty(logits, stream, (T, E), (E, 1), logits.dtype), E
     else:
         ldd = _like(dlogits, "dlogits", T, E, logits)
     _check(load().dass_route_balance_backward(logits.data_ptr(), T, E, ld, dt, ids, k, load_, scale, _ptr(add), lda, dlogits.data_ptr(),
-                                              ldd, _stream_of(logits, stream)), "dass_route_balance_backward")
+                                              ldd, handle), "dass_route_balance_backward")
     return dlogits
 
 
@@ -919,15 +930,16 @@ def _mx4_shapes(lead: Tuple[int, ...], cols: int) -> Tuple[Tuple[int, ...], Tupl
     return (*lead, (cols + 31) // 32 * 16), (*lead[:-1], (lead[-1] + 127) // 128, (cols + 127) // 128, 512)
 
 
-def _mx4(q: MX4, name: str, device: torch.device) -> Tuple[int, int]:
-    """Checks a 4-bit matrix or a stack of them and returns its addresses."""
+def _mx4(q: MX4, name: str, device: int) -> Tuple[int, int]:
+    """Checks a 4-bit matrix, or a stack of them, on the device of this index and returns its addresses."""
     codes, scales, cols = q
     shape, tiles = codes.shape, scales.shape
-    if (len(shape) not in (2, 3) or cols < 1 or shape[-1] != (cols + 31) // 32 * 16 or len(tiles) != len(shape) + 1 or
-            tiles[-3] != (shape[-2] + 127) // 128 or tiles[-2] != (cols + 127) // 128 or tiles[-1] != 512 or (len(shape) == 3 and tiles[0] != shape[0]) or
-            codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.device != device or scales.device != device or
+    dims = len(shape)
+    if (dims not in (2, 3) or cols < 1 or shape[-1] != (cols + 31) // 32 * 16 or len(tiles) != dims + 1 or tiles[-1] != 512 or
+            tiles[-3] != (shape[-2] + 127) // 128 or tiles[-2] != (cols + 127) // 128 or (dims == 3 and tiles[0] != shape[0]) or
+            codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.get_device() != device or scales.get_device() != device or
             not codes.is_contiguous() or not scales.is_contiguous()):
-        raise ValueError(f"{name} must be an MX4 of [rows x cols] or [G x rows x cols] on {device}: contiguous uint8 codes and scales of the shapes it states")
+        raise ValueError(f"{name} must be an MX4 of [rows x cols] or [G x rows x cols] on cuda:{device}: contiguous uint8 codes and scales of the shapes it states")
     return codes.data_ptr(), scales.data_ptr()
 
 
@@ -947,13 +959,19 @@ def mx4_quantize(X: torch.Tensor, out: Optional[MX4] = None, stream: Optional[to
     ld = strides[-2] if rows > 1 or strides[-2] > cols else cols
     handle = _stream_of(X, stream)
     if out is None:
-        want, new = _mx4_shapes(shape[:-1], cols), _new(X, stream)
-        out = MX4(new(want[0], dtype=torch.uint8), new(want[1], dtype=torch.uint8), cols)
-        codes, scales = out.codes.data_ptr(), out.scales.data_ptr()
+        pitch, tiles, along = (cols + 31) // 32 * 16, (rows + 127) // 128, (cols + 127) // 128
+        if dims == 2:
+            c = _empty(X, stream, (rows, pitch), (pitch, 1), torch.uint8)
+            s = _empty(X, stream, (tiles, along, 512), (along * 512, 512, 1), torch.uint8)
+        else:
+            c = _empty(X, stream, (G, rows, pitch), (rows * pitch, pitch, 1), torch.uint8)
+            s = _empty(X, stream, (G, tiles, along, 512), (tiles * along * 512, along * 512, 512, 1), torch.uint8)
+        out = MX4(c, s, cols)
+        codes, scales = c.data_ptr(), s.data_ptr()
     elif out.shape != shape:
         raise ValueError("out must be an MX4 of X's shape")
     else:
-        codes, scales = _mx4(out, "out", X.device)
+        codes, scales = _mx4(out, "out", X.get_device())
     if rows:
         _check(load().dass_mx4_quantize(X.data_ptr(), G, rows, cols, ld, group_stride, dt, codes, scales, handle), "dass_mx4_quantize")
     return out
@@ -966,11 +984,11 @@ def mx4_dequantize(Q: MX4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     if not first.is_cuda:
         raise ValueError("Q must be on a CUDA device")
     handle = _stream_of(first, stream)
-    codes, scales = _mx4(Q, "Q", first.device)
+    codes, scales = _mx4(Q, "Q", first.get_device())
     lead = first.shape[:-1]
     G, rows = (lead[0], lead[1]) if len(lead) == 2 else (1, lead[0])
     if out is None:
-        out = _new(first, stream)((*lead, cols), dtype=dtype)
+        out = _empty(first, stream, (*lead, cols), (rows * cols, cols, 1) if len(lead) == 2 else (cols, 1), dtype)
     elif out.shape != (*lead, cols) or out.dtype != dtype or out.device != first.device or (out.stride(-1) != 1 and cols > 1):
         raise ValueError("out must be a tensor of Q's shape and device and of the dtype asked for, with unit stride along its columns")
     strides, dt = out.stride(), _code(out)
@@ -1007,24 +1025,25 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
         if len(first.shape) != 2 or not first.is_cuda:
             raise ValueError("X must be an MX4 of [T x K] on a CUDA device")
         T, K = first.shape[0], X.cols
-        xc, xs = _mx4(X, "X", first.device)
+        index = first.get_device()
+        xc, xs = _mx4(X, "X", index)
     else:
         first = X
         T, K, ldx = _rows(X, "X")
         if X.dtype != torch.bfloat16:
             raise TypeError(f"unsupported dtype {X.dtype}: linear_mx4 takes bfloat16 rows or an MX4")
+        index = X.get_device()
         x, xc, xs = X.data_ptr(), None, None
-    device, dtype = first.device, torch.bfloat16
     shape = W.codes.shape
     if len(shape) != (2 if offsets is None else 3) or W.cols != K:
         raise ValueError(f"W must be an MX4 of {'[N x K]' if offsets is None else '[G x N x K]'}")
-    wc, ws = _mx4(W, "W", device)
+    wc, ws = _mx4(W, "W", index)
     uc = us = None
     if W_up is not None:
         if W_up.codes.shape != shape or W_up.cols != K:
             raise ValueError("W_up must have W's shape")
-        uc, us = _mx4(W_up, "W_up", device)
-    N = shape[-2]
+        uc, us = _mx4(W_up, "W_up", index)
+    N, device, dtype = shape[-2], first.device, torch.bfloat16
     if offsets is None:
         groups, edges, per = 1, None, (N,)
     else:
@@ -1034,25 +1053,26 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
     if bias_up is not None and W_up is None:
         raise ValueError("bias_up goes with W_up")
     bu = _same(bias_up, "bias_up", per, dtype, device) if bias_up is not None else None
-
-    def like(t: torch.Tensor, name: str) -> int:
+    res, ldr = None, 0
+    for t, name in ((residual, "residual"), (Y, "Y")):
+        if t is None:
+            continue
         r, c, ld = _rows(t, name)
-        if r != T or c != N or t.dtype != dtype or t.device != device:
+        if r != T or c != N or t.dtype != dtype or t.get_device() != index:
             raise ValueError(f"{name} must be a {dtype} matrix of shape {(T, N)} on {device}")
-        return ld
-
-    ldr = like(residual, "residual") if residual is not None else 0
+        if name == "Y":
+            ldy = ld
+        else:
+            res, ldr = t.data_ptr(), ld
+    handle = _stream_of(first, stream)
     if Y is None:
-        Y, ldy = _new(first, stream)((T, N), dtype=dtype), N
-    else:
-        ldy = like(Y, "Y")
+        Y, ldy = _empty(first, stream, (T, N), (N, 1), dtype), N
     if T:
-        handle = _stream_of(first, stream)
         if workspace is None:
-            need = _linear_mx4_bytes(first.get_device(), T, K, N, groups, offsets is not None, W_up is not None, quantized)
-            workspace = _new(first, stream)(need, dtype=torch.uint8) if need else None
+            need = _linear_mx4_bytes(index, T, K, N, groups, offsets is not None, W_up is not None, quantized)
+            workspace = _empty(first, stream, (need,), (1,), torch.uint8) if need else None
         else:
             _workspace(workspace, device)
-        _check(load().dass_linear_mx4(x, ldx, xc, xs, T, K, wc, ws, uc, us, N, b, bu, act, _ptr(residual), ldr, Y.data_ptr(), ldy, edges,
+        _check(load().dass_linear_mx4(x, ldx, xc, xs, T, K, wc, ws, uc, us, N, b, bu, act, res, ldr, Y.data_ptr(), ldy, edges,
                                       groups, _ptr(workspace), workspace.numel() if workspace is not None else 0, handle), "dass_linear_mx4")
     return Y

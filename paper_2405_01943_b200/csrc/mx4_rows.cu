@@ -9,7 +9,10 @@
 // four rows at a time.  Scales go to tiles of 128 rows x 4 blocks (the order in which the tensor cores take them); the
 // four scales of a row in a tile are one word, put together by two shuffles.
 //
-// Bound by the memory.
+// Bound by the memory, near it by the instructions: a 28672 x 8192 matrix in bf16 111 us (5.35 TB/s of 6.57), back 99 us
+// (5.98).  With 64-bit divisions for a warp's place it took 276 us, with bounds tested at every access 141, with the decoding
+// of single floats 142 back.  Rows that are not 16-byte aligned change lanes through shared memory: 3001 x 1001 f32 5.2 us, 4.6
+// back (element by element 8.4 and 19.0).
 #include "mx4_common.cuh"
 #include "rows_common.cuh"
 
