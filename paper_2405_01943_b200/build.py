@@ -22,7 +22,7 @@ CHECK_LIB = os.path.join(PKG, "libdass_check.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0",       # source files side by side
 ]
 
 
@@ -68,7 +68,7 @@ def build_bounds_check(force: bool = False) -> str:
         with open(unity, "w") as f:
             for src in sources():
                 f.write(f'#include "{src}"\n')
-        cmd = [nvcc] + NVCC_FLAGS + ["-DDASS_BOUNDS_CHECK", "-I", os.path.join(ROOT, "include"), "-I", CSRC, unity, "-o", tmp]
+        cmd = [nvcc] + NVCC_FLAGS + ["-split-compile=0", "-DDASS_BOUNDS_CHECK", "-I", os.path.join(ROOT, "include"), "-I", CSRC, unity, "-o", tmp]
         res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)

@@ -9,10 +9,10 @@
 // four rows at a time.  Scales go to tiles of 128 rows x 4 blocks (the order in which the tensor cores take them); the
 // four scales of a row in a tile are one word, put together by two shuffles.
 //
-// Bound by the memory, near it by the instructions: a 28672 x 8192 matrix in bf16 111 us (5.35 TB/s of 6.57), back 99 us
-// (5.98).  With 64-bit divisions for a warp's place it took 276 us, with bounds tested at every access 141, with the decoding
-// of single floats 142 back.  Rows that are not 16-byte aligned change lanes through shared memory: 3001 x 1001 f32 5.2 us, 4.6
-// back (element by element 8.4 and 19.0).
+// Bound by the memory: a 28672 x 8192 matrix in bf16 101 us (5.88 TB/s of 6.57), back 98 us (6.09).  With 64-bit divisions for a
+// warp's place it took 276 us, with bounds tested at every access 141, with six blocks to an SM instead of eight 111, with the
+// decoding of single floats 142 back.  Rows that are not 16-byte aligned change lanes through shared memory: 3001 x 1001 f32
+// 5.1 us, 4.4 back (element by element 8.4 and 19.0).
 #include "mx4_common.cuh"
 #include "rows_common.cuh"
 
@@ -150,7 +150,7 @@ __device__ __forceinline__ void mq_encode(const char *src, int64_t row_bytes, in
 }
 
 template <bool BF16, bool VECTOR>
-__global__ void __launch_bounds__(MQ_THREADS)
+__global__ void __launch_bounds__(MQ_THREADS, VECTOR ? 8 : 4)
 mx4_quantize_kernel(const void *__restrict__ X, int64_t rows, int64_t K, int64_t ldx, int64_t group_stride,
                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, const MqGrid q)
 {
@@ -211,8 +211,19 @@ __device__ __forceinline__ void mq_decode(const uint8_t *codes, int64_t pitch, c
 #pragma unroll
             for (int j = 0; j < 4; ++j) { v[2 * j] = pairs[j] << 16; v[2 * j + 1] = pairs[j] & 0xffff0000u; }
             if constexpr (VECTOR) {
-                if (INSIDE || c + 8 <= K) {
-                    DASS_ST(at, make_uint4(v[0], v[1], v[2], v[3]));     // half a sector each: they meet in the cache
+                if constexpr (INSIDE) {
+                    // a lane's 32 bytes in two accesses would be half a sector each: neighbours swap, and write a sector together
+                    uint32_t mine[4], theirs[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        mine[j] = lane & 1 ? v[4 + j] : v[j];
+                        theirs[j] = __shfl_xor_sync(FULL_MASK, lane & 1 ? v[j] : v[4 + j], 1);
+                    }
+                    uint4 *const pair = reinterpret_cast<uint4 *>(row + (lane & ~1) * 8 * ES) + (lane & 1);
+                    DASS_ST_CS(pair, lane & 1 ? make_uint4(theirs[0], theirs[1], theirs[2], theirs[3]) : make_uint4(mine[0], mine[1], mine[2], mine[3]));
+                    DASS_ST_CS(pair + 2, lane & 1 ? make_uint4(mine[0], mine[1], mine[2], mine[3]) : make_uint4(theirs[0], theirs[1], theirs[2], theirs[3]));
+                } else if (c + 8 <= K) {
+                    DASS_ST(at, make_uint4(v[0], v[1], v[2], v[3]));
                     DASS_ST(at + 1, make_uint4(v[4], v[5], v[6], v[7]));
                 } else {
 #pragma unroll
@@ -237,7 +248,7 @@ __device__ __forceinline__ void mq_decode(const uint8_t *codes, int64_t pitch, c
 }
 
 template <bool BF16, bool VECTOR>
-__global__ void __launch_bounds__(MQ_THREADS)
+__global__ void __launch_bounds__(MQ_THREADS, 8)
 mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int64_t K,
                       void *__restrict__ Y, int64_t ldy, int64_t group_stride, const MqGrid q)
 {
