@@ -94,6 +94,30 @@ def test_quantize_strides_offsets_and_stacks(rows, K, dtype):
         assert torch.equal(out[g, :rows, 1:1 + K], b.mx4_dequantize(b.MX4(Q.codes[g], Q.scales[g], K), dtype))
 
 
+def _nearest(x):
+    """Rows [n x 32 b] of doubles rounded to 4 bits and back, on the device (for sizes that numpy is slow at)."""
+    blocks = x.view(len(x), -1, 32)
+    scale = torch.ldexp(torch.ones_like(blocks[:, :, :1]), (torch.frexp(blocks.abs().amax(2, keepdim=True)).exponent - 3).clamp_min(-127))
+    y = (blocks / scale).abs().clamp_max(6.0)
+    step = torch.where(y < 2.0, 0.5, torch.where(y < 4.0, 1.0, 2.0))
+    return (torch.round(y / step) * step * blocks.sign() * scale).view_as(x)       # half to even is the even code: steps are its last bit
+
+
+@both
+@pytest.mark.parametrize("groups,rows,K", [(1, 1100077, 32), (70001, 3, 64), (3, 40000, 96)])
+def test_more_rows_and_matrices_than_a_grid_has_places(groups, rows, K, dtype):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    X = torch.randn((groups, rows, K), generator=g, device=DEV).to(dtype)
+    X = X[0] if groups == 1 else X
+    Q = b.mx4_quantize(X)
+    got = b.mx4_dequantize(Q, dtype)
+    assert torch.equal(got.view(-1, K).double(), _nearest(X.view(-1, K).double()))
+    if groups > 1:
+        last = b.mx4_quantize(X[-1])
+        assert torch.equal(Q.codes[-1], last.codes) and torch.equal(Q.scales[-1], last.scales)
+
+
 def test_every_code_and_scale():
     """All 16 codes under all 256 scales: exact, infinite only where the value passes bf16's range, NaN for scale 255."""
     codes = np.tile(np.arange(32, dtype=np.uint8) % 16, (256, 1))
