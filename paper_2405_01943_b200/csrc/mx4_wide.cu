@@ -79,8 +79,8 @@ __device__ __forceinline__ void umma_bf16_ts_pair(uint32_t d_tmem, uint32_t a_tm
 template <int REGS> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
 template <int REGS> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
 // The launch has 896 x 72 registers; the warpgroups' shares below add up to 128 x (40 + 4 x 64 + 2 x 104) = 64512, all of them.
-constexpr int MW_REGS_ISSUE = 40, MW_REGS_DECODE = 64, MW_REGS_EPILOGUE = 104;
-static_assert(128 * (MW_REGS_ISSUE + 4 * MW_REGS_DECODE + 2 * MW_REGS_EPILOGUE) <= MW_THREADS * 72, "");
+constexpr int MW_REGS_LAUNCH = 72, MW_REGS_ISSUE = 40, MW_REGS_DECODE = 64, MW_REGS_EPILOGUE = 104;
+static_assert(128 * (MW_REGS_ISSUE + 4 * MW_REGS_DECODE + 2 * MW_REGS_EPILOGUE) <= MW_THREADS * MW_REGS_LAUNCH, "");
 
 // 32 codes of one block (16 bytes) as 16 bf16 pairs, in order.
 __device__ __forceinline__ void mw_decode32(const uint4 &v, const Mx4Factor &f, bool two, uint32_t (&out)[16])
@@ -363,6 +363,16 @@ static cudaError_t mw_launch(const MwMaps &m, const MwParams &p, int grid, cudaS
     static DeviceMask configured{0ull};               // per device
     const cudaError_t ce = ensure_dynamic_smem(mx4_wide_kernel<NT, GLU, ACT>, (int)MwShape<NT, GLU>::BYTES, configured);
     if (ce != cudaSuccess) return ce;
+    // The warpgroups' shares are drawn on what the kernel is launched with: a build with fewer registers would wait for good.
+    static std::atomic<int> registers{0};
+    int have = registers.load(std::memory_order_relaxed);
+    if (!have) {
+        cudaFuncAttributes attr;
+        const cudaError_t e = cudaFuncGetAttributes(&attr, mx4_wide_kernel<NT, GLU, ACT>);
+        if (e != cudaSuccess) return e;
+        registers.store(have = attr.numRegs, std::memory_order_relaxed);
+    }
+    if (have < MW_REGS_LAUNCH) return cudaErrorLaunchOutOfResources;
     mx4_wide_kernel<NT, GLU, ACT><<<grid, MW_THREADS, MwShape<NT, GLU>::BYTES, st>>>(m.x, m.w, m.up, m.ws, m.us, p);
     return cudaGetLastError();
 }
