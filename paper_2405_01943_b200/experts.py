@@ -76,7 +76,10 @@ class ExpertLayer:
         """Y[t] = residual[t] + sum_j weight[t,j] * expert_j(X[t]).  With ``keep`` also what router_gradient needs.
 
         An expert's intermediate H and its output are rounded to X's dtype between the calls, as a dense layer's are: in bf16
-        an expert's output is 2.3e-3 off the exact one, of which the last rounding alone is 1.7e-3."""
+        an expert's output is 2.3e-3 off the exact one, of which the last rounding alone is 1.7e-3.  Experts in 4 bits take
+        bfloat16 tokens alone, also where rows_in_4_bits quantises them."""
+        if self.quantized and X.dtype != torch.bfloat16:
+            raise TypeError(f"experts in 4 bits take bfloat16 tokens, not {X.dtype}")
         r = routed if routed is not None else self.route(X)
         Xs = b.expert_gather(X, r.slot, r.offsets)
         H = self._product(Xs, self.Wg, r.offsets, act=self.act, W_up=self.Wu)
@@ -112,9 +115,12 @@ class ExpertLayer:
     # ------------------------------------------------------------------ 4-bit weights
     def quantize(self, rows_in_4_bits: bool = False) -> "ExpertLayer":
         """The layer with its experts in microscaled 4-bit values (a quarter of the bytes; what pruning set to zero stays zero).
-        With ``rows_in_4_bits`` tokens and intermediate rows are quantised as well, which the 4-bit tensor pipe needs."""
+        With ``rows_in_4_bits`` tokens and intermediate rows are quantised as well, which the 4-bit tensor pipe needs.
+        For bfloat16 layers: the products with 4-bit weights take bfloat16 rows and give bfloat16."""
         if self.quantized:
             raise RuntimeError("the experts are in 4 bits already")
+        if self.Wg.dtype != torch.bfloat16:
+            raise TypeError(f"a layer of {self.Wg.dtype} cannot be quantised: products with 4-bit weights take bfloat16 rows")
         out = ExpertLayer(self.Wr, *(b.mx4_quantize(W) for W in (self.Wg, self.Wu, self.Wd)), self.k, renormalise=self.renormalise,
                           router_bias=self.router_bias, rows_in_4_bits=rows_in_4_bits)
         out.act = self.act

@@ -146,12 +146,15 @@ class LayerPruner:
     # ------------------------------------------------------------------ the pruned layer in 4 bits
     def quantize_pruned(self) -> Dict[str, b.MX4]:
         """The pruned copies the last prune() / score_nm() / select_unstructured() wrote, in microscaled 4-bit values: zeros stay
-        zeros, what is left takes 4.25 bits a weight."""
+        zeros, what is left takes 4.25 bits a weight.  (Copies in float32 too, but forward_quantized takes bfloat16 tokens.)"""
         return {name: b.mx4_quantize(self.out[name]["pruned"]) for name in _PROJECTIONS}
 
     def forward_quantized(self, X: torch.Tensor, weights: Dict[str, b.MX4], rows_in_4_bits: bool = False) -> torch.Tensor:
         """The layer's output (Eq. 2 then Eq. 3) for weights in 4 bits, the intermediate rounded to bfloat16 as forward_with
-        rounds it; with ``rows_in_4_bits`` the rows of both products are quantised too."""
+        rounds it; with ``rows_in_4_bits`` the rows of both products are quantised too.  X is in bfloat16, as the output is, whatever
+        type the layer was pruned in."""
+        if X.dtype != torch.bfloat16:
+            raise TypeError(f"forward_quantized takes bfloat16 tokens, not {X.dtype}")
         rows = b.mx4_quantize if rows_in_4_bits else lambda x: x
         H = b.linear_mx4(rows(X), weights["gate"], act=self.act, W_up=weights["up"])
         return b.linear_mx4(rows(H), weights["down"])
