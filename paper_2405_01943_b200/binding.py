@@ -1011,6 +1011,12 @@ def linear_mx4_workspace_bytes(T: int, K: int, N: int, groups: int = 1, has_offs
 _linear_mx4_bytes = functools.lru_cache(maxsize=4096)(lambda device, *sizes: linear_mx4_workspace_bytes(*sizes))
 
 
+def mx4_rows(T: int, cols: int, device: torch.device) -> Optional[torch.Tensor]:
+    """A bfloat16 matrix [T x cols] whose rows begin on 16 bytes, as linear_mx4 wants its rows, for columns that are no multiple of
+    8; None for others, whose dense rows do so."""
+    return torch.empty((T, (cols + 7) // 8 * 8), dtype=torch.bfloat16, device=device)[:, :cols] if cols % 8 else None
+
+
 def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, W_up: Optional[MX4] = None,
                bias_up: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
                Y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,

@@ -81,8 +81,9 @@ class ExpertLayer:
         if self.quantized and X.dtype != torch.bfloat16:
             raise TypeError(f"experts in 4 bits take bfloat16 tokens, not {X.dtype}")
         r = routed if routed is not None else self.route(X)
-        Xs = b.expert_gather(X, r.slot, r.offsets)
-        H = self._product(Xs, self.Wg, r.offsets, act=self.act, W_up=self.Wu)
+        Xs = b.expert_gather(X, r.slot, r.offsets, Xs=b.mx4_rows(r.slot.numel(), self.d, X.device) if self.quantized else None)
+        H = b.mx4_rows(Xs.shape[0], self.I, X.device) if self.quantized else None
+        H = self._product(Xs, self.Wg, r.offsets, act=self.act, W_up=self.Wu, Y=H)
         Ys = self._product(H, self.Wd, r.offsets)
         Y = b.expert_combine(Ys, r.slot, r.weight, residual=residual)
         return (Y, Saved(r, Ys)) if keep else Y

@@ -156,5 +156,6 @@ class LayerPruner:
         if X.dtype != torch.bfloat16:
             raise TypeError(f"forward_quantized takes bfloat16 tokens, not {X.dtype}")
         rows = b.mx4_quantize if rows_in_4_bits else lambda x: x
-        H = b.linear_mx4(rows(X), weights["gate"], act=self.act, W_up=weights["up"])
+        H = b.mx4_rows(X.shape[0], weights["gate"].shape[0], X.device)
+        H = b.linear_mx4(rows(X), weights["gate"], act=self.act, W_up=weights["up"], Y=H)
         return b.linear_mx4(rows(H), weights["down"])

@@ -60,3 +60,13 @@ def test_float32_is_refused_before_any_call(calls, rows4):
         pruner.forward_quantized(torch.zeros(5, D), weights, rows_in_4_bits=rows4)
     assert not calls
     assert pruner.forward_quantized(torch.zeros(5, D, dtype=BF16), weights, rows_in_4_bits=rows4).shape == (5, D)
+
+
+@pytest.mark.parametrize("rows4", [False, True], ids=["bf16-rows", "4-bit-rows"])
+@pytest.mark.parametrize("I", [4, 32, 36, 356])
+def test_rows_of_any_length_reach_the_second_product(calls, I, rows4):
+    pruner = LayerPruner(5, D, I, BF16, device="cpu", overlap_projections=False)
+    weights = pruner.quantize_pruned()
+    for T in (1, 5):
+        assert pruner.forward_quantized(torch.zeros(T, D, dtype=BF16), weights, rows_in_4_bits=rows4).shape == (T, D)
+        assert _layer(BF16, I).quantize(rows_in_4_bits=rows4).forward(torch.zeros(T, D, dtype=BF16), routed=_routed).shape == (T, D)
