@@ -252,13 +252,16 @@ def _new(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> Callable[..., 
 
 
 # torch's allocation of a dense tensor on the current device from its sizes, strides and dtype, without the general dispatch: 0.9
-# instead of 2 us, of which a call of the section below has up to three.  None where a torch version has no such function.
+# instead of 2 us, of which a call of the section below has up to three.  None where a torch version has no such function.  It
+# passes by what the dispatch does on request: other modes' allocation and the filling of new memory under deterministic
+# algorithms; where either is on, _empty takes the general way, as the calls above do.
 _cuda_empty = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+_dispatch_modes = getattr(torch._C, "_len_torch_dispatch_stack", lambda: 1)
 
 
 def _empty(t: torch.Tensor, stream: Optional[torch.cuda.Stream], shape: Tuple[int, ...], strides: Tuple[int, ...], dtype: torch.dtype) -> torch.Tensor:
     """An output of a call on `stream` with tensor t, whose device is the current one (_stream_of has seen to that)."""
-    if stream is None and _cuda_empty is not None and type(t) is torch.Tensor:
+    if stream is None and _cuda_empty is not None and type(t) is torch.Tensor and not _dispatch_modes() and not torch.are_deterministic_algorithms_enabled():
         return _cuda_empty(shape, strides, dtype)
     return _new(t, stream)(shape, dtype=dtype)
 
