@@ -929,8 +929,13 @@ class MX4(NamedTuple):
         return self.codes.device
 
 
-def _mx4_shapes(lead: Tuple[int, ...], cols: int) -> Tuple[Tuple[int, ...], Tuple[int, ...]]:
-    return (*lead, (cols + 31) // 32 * 16), (*lead[:-1], (lead[-1] + 127) // 128, (cols + 127) // 128, 512)
+def _mx4_shapes(lead: Tuple[int, ...], cols: int) -> Tuple[Tuple[int, ...], Tuple[int, ...], Tuple[int, ...], Tuple[int, ...]]:
+    """The shapes of codes and scales of a matrix [rows x cols] or a stack [G x rows x cols], then their dense strides."""
+    rows, pitch, along = lead[-1], (cols + 31) // 32 * 16, (cols + 127) // 128
+    tiles = (rows + 127) // 128
+    if len(lead) == 1:
+        return (rows, pitch), (tiles, along, 512), (pitch, 1), (along * 512, 512, 1)
+    return (lead[0], rows, pitch), (lead[0], tiles, along, 512), (rows * pitch, pitch, 1), (tiles * along * 512, along * 512, 512, 1)
 
 
 def _mx4(q: MX4, name: str, device: int) -> Tuple[int, int]:
@@ -962,13 +967,9 @@ def mx4_quantize(X: torch.Tensor, out: Optional[MX4] = None, stream: Optional[to
     ld = strides[-2] if rows > 1 or strides[-2] > cols else cols
     handle = _stream_of(X, stream)
     if out is None:
-        pitch, tiles, along = (cols + 31) // 32 * 16, (rows + 127) // 128, (cols + 127) // 128
-        if dims == 2:
-            c = _empty(X, stream, (rows, pitch), (pitch, 1), torch.uint8)
-            s = _empty(X, stream, (tiles, along, 512), (along * 512, 512, 1), torch.uint8)
-        else:
-            c = _empty(X, stream, (G, rows, pitch), (rows * pitch, pitch, 1), torch.uint8)
-            s = _empty(X, stream, (G, tiles, along, 512), (tiles * along * 512, along * 512, 512, 1), torch.uint8)
+        codes, scales, code_strides, scale_strides = _mx4_shapes(shape[:-1], cols)
+        c = _empty(X, stream, codes, code_strides, torch.uint8)
+        s = _empty(X, stream, scales, scale_strides, torch.uint8)
         out = MX4(c, s, cols)
         codes, scales = c.data_ptr(), s.data_ptr()
     elif out.shape != shape:

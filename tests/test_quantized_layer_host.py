@@ -12,7 +12,7 @@ E, D = 4, 16
 
 def _mx4(shape):
     *lead, cols = shape
-    codes, scales = b._mx4_shapes(tuple(lead), cols)
+    codes, scales = b._mx4_shapes(tuple(lead), cols)[:2]
     return b.MX4(torch.zeros(codes, dtype=torch.uint8), torch.zeros(scales, dtype=torch.uint8), cols)
 
 
