@@ -400,6 +400,12 @@ dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int
  * WORKSPACE / CUDA. */
 dass_status dass_linear_mx4_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t groups, int has_offsets, int has_up, int x_in_4_bits,
                                             size_t *bytes /* HOST */);
+/* The kernel that a call of these sizes takes, for tests and measurements: plan[0] 0 (weights decoded in registers), 1 (weights as
+ * the long side), 2 (CTA pairs, rows in 4 bits) or 3 (CTA pairs, weights decoded into tensor memory); plan[1] the tile: rows in
+ * eights, rows, columns, rows; for 0 also plan[2] the weight rows in sixteens, plan[3] the blocks that share k, plan[4] the warps
+ * of a block (0 elsewhere).  T >= 1. */
+dass_status dass_linear_mx4_plan(int64_t T, int64_t K, int64_t N, int64_t groups, int has_offsets, int has_up, int x_in_4_bits,
+                                 int32_t *plan /* HOST, [5] */);
 dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, const uint8_t *x_scales, int64_t T, int64_t K,
                             const uint8_t *w_codes, const uint8_t *w_scales, const uint8_t *up_codes, const uint8_t *up_scales, int64_t N,
                             const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,

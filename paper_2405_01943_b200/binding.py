@@ -34,7 +34,7 @@ EXPORTS = (
     "dass_route_topk", "dass_route_topk_backward", "dass_expert_sort_workspace_bytes", "dass_expert_sort",
     "dass_expert_gather", "dass_expert_combine", "dass_expert_combine_backward", "dass_linear", "dass_linear_status",
     "dass_route_balance_workspace_bytes", "dass_route_balance", "dass_route_balance_backward",
-    "dass_mx4_bytes", "dass_mx4_quantize", "dass_mx4_dequantize", "dass_linear_mx4_workspace_bytes", "dass_linear_mx4",
+    "dass_mx4_bytes", "dass_mx4_quantize", "dass_mx4_dequantize", "dass_linear_mx4_workspace_bytes", "dass_linear_mx4_plan", "dass_linear_mx4",
     "dass_bounds_report", "dass_bounds_shrink_next",
     "dass_status_string", "dass_version",
 )
@@ -155,6 +155,8 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.dass_linear_mx4.restype = ci
     lib.dass_linear_mx4_workspace_bytes.restype = ci
     lib.dass_linear_mx4_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci, ci, ctypes.POINTER(sz)]
+    lib.dass_linear_mx4_plan.restype = ci
+    lib.dass_linear_mx4_plan.argtypes = [i64, i64, i64, i64, ci, ci, ci, ctypes.POINTER(ctypes.c_int32)]
     lib.dass_linear_mx4.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp, ci, vp, i64, vp, i64, vp, i64, vp, sz, vp]
     lib.dass_status_string.restype = ctypes.c_char_p
     lib.dass_status_string.argtypes = [ctypes.c_int]
@@ -1009,6 +1011,15 @@ def linear_mx4_workspace_bytes(T: int, K: int, N: int, groups: int = 1, has_offs
     _check(load().dass_linear_mx4_workspace_bytes(int(T), int(K), int(N), int(groups), int(has_offsets), int(has_up), int(x_in_4_bits),
                                                   ctypes.byref(out)), "dass_linear_mx4_workspace_bytes")
     return int(out.value)
+
+
+def linear_mx4_plan(T: int, K: int, N: int, groups: int = 1, has_offsets: bool = False, has_up: bool = False,
+                    x_in_4_bits: bool = False) -> Tuple[int, int, int, int, int]:
+    """Which kernel linear_mx4 takes for these sizes, for tests and measurements: (kernel, tile, weight rows in sixteens, blocks that
+    share k, warps of a block), as include/dass.h has it."""
+    out = (ctypes.c_int32 * 5)()
+    _check(load().dass_linear_mx4_plan(int(T), int(K), int(N), int(groups), int(has_offsets), int(has_up), int(x_in_4_bits), out), "dass_linear_mx4_plan")
+    return tuple(out)
 
 
 # The choice of kernel behind it is the same for equal sizes and goes by the device's SMs.

@@ -234,12 +234,10 @@ static cudaError_t mf_launch(const Mx4Args &p, int64_t row_tiles, int split)
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, mx4_few_kernel<NT, MT, GLU, XQ, WARPS>, p, col_tiles, split);
 }
-// 16 warps hide the decoding's latency where each of them has two turns of k at least (up to 8 rows, 1 x 4096 x 4096: 6.8 against
-// 7.2 us, 1 x 14336 x 4096 15.2 against 18.2; but 1 x 2048 x 2048 gated 8.3 against 6.4).
 template <int MT, bool GLU, bool XQ>
 static cudaError_t mf_one(const Mx4Args &p, int64_t row_tiles, int split)
 {
-    if (mx4_k_tiles(p.a.K) >= 32 * split) return mf_launch<1, MT, GLU, XQ, 16>(p, row_tiles, split);
+    if (mx4_few_warps(p.a.K, 1, split) == 16) return mf_launch<1, MT, GLU, XQ, 16>(p, row_tiles, split);
     return mf_launch<1, MT, GLU, XQ, 8>(p, row_tiles, split);
 }
 template <bool GLU, bool XQ>

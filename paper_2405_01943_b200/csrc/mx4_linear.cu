@@ -107,6 +107,21 @@ dass_status dass_linear_mx4_workspace_bytes(int64_t T, int64_t K, int64_t N, int
     return DASS_OK;
 }
 
+dass_status dass_linear_mx4_plan(int64_t T, int64_t K, int64_t N, int64_t groups, int has_offsets, int has_up, int x_in_4_bits, int32_t *plan)
+{
+    if (!plan) return DASS_ERR_NULL;
+    if (T < 1 || K < 1 || N < 1 || groups < 1 || (!has_offsets && groups != 1)) return DASS_ERR_SHAPE;
+    if (mx4_too_large(T, K, N, groups)) return DASS_ERR_UNSUPPORTED;
+    const Mx4Plan p = mx4_plan(Mx4Sizes{T, K, N, groups, has_offsets != 0, has_up != 0, x_in_4_bits != 0});
+    const bool few = p.path == MX4_FEW;
+    plan[0] = p.path;
+    plan[1] = p.tile;
+    plan[2] = few ? p.sixteens : 0;
+    plan[3] = few ? p.split : 0;
+    plan[4] = few ? mx4_few_warps(K, p.tile, p.split) : 0;
+    return DASS_OK;
+}
+
 dass_status dass_linear_mx4(const void *X, int64_t ldx, const uint8_t *x_codes, const uint8_t *x_scales, int64_t T, int64_t K,
                             const uint8_t *w_codes, const uint8_t *w_scales, const uint8_t *up_codes, const uint8_t *up_scales, int64_t N,
                             const void *bias, const void *bias_up, dass_act act, const void *residual, int64_t ldr,

@@ -21,6 +21,10 @@ __host__ __device__ __forceinline__ Mx4Matrix mx4_group(const Mx4Matrix &m, int6
     return {m.codes + g * N * mx4_pitch(K), m.scales + g * ((N + MX4_TILE_ROWS - 1) / MX4_TILE_ROWS) * mx4_k_tiles(K) * MX4_TILE_BYTES};
 }
 
+// Warps of a block of mx4_few.cu.  16 hide the decoding's latency where each of them has two turns of k at least (up to 8 rows,
+// 1 x 4096 x 4096: 6.8 against 7.2 us, 1 x 14336 x 4096 15.2 against 18.2; but 1 x 2048 x 2048 gated 8.3 against 6.4).
+inline int mx4_few_warps(int64_t K, int eights, int split) { return eights == 1 && mx4_k_tiles(K) >= 32 * split ? 16 : 8; }
+
 // ------------------------------------------------------------------ waits of the warp that issues the products
 // A wait that finds its barrier complete still takes 130 cycles, as long as a short slab's products.  So the issuing warp
 // asks for the next stage's barrier before it issues this one's products, and looks at the answer after them.
