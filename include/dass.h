@@ -393,8 +393,9 @@ dass_status dass_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int
  * scales stand for, in f32 accumulators.  bias, bias_up, residual, Y in bf16, offsets and groups, alignment and what else is
  * not said here: as for dass_linear, whose dass_linear_status reports this call's bounded waits too.
  * bf16 rows meet the weights as they are, or, where few of them meet many weights, as sums of 4-bit rows that hold every
- * value of a block of 32 to 2^-24 of the largest in it; those rows go to the workspace: dass_linear_mx4_workspace_bytes(..)
- * bytes (may be 0), 16-byte aligned.  groups = 1 and has_offsets = 0 for a dense product.
+ * value of a block of 32 to 2^-24 of the largest in it, or to 2^-129 where that is more (half the smallest code's step); those
+ * rows go to the workspace: dass_linear_mx4_workspace_bytes(..) bytes (may be 0, which is where rows stay as they are),
+ * 16-byte aligned.  groups = 1 and has_offsets = 0 for a dense product.
  * (There a row's block that holds a NaN or an infinity is NaN.)
  * Errors: NULL / DTYPE / SHAPE / ALIGN / UNSUPPORTED (X in both forms; more than 2^26 rows; other limits of dass_linear) /
  * WORKSPACE / CUDA. */

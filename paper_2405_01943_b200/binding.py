@@ -1039,7 +1039,11 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
     """linear() with weights in 4 bits: Y = act(X W^T + bias) [* (X W_up^T + bias_up)] + residual in bfloat16.
 
     X [T x K] is a bfloat16 matrix or an MX4 (mx4_quantize's).  Dense: W (and W_up) [N x K]; per expert, with ``offsets``:
-    [G x N x K], as for linear().  ``Y`` may be the residual itself."""
+    [G x N x K], as for linear().  ``Y`` may be the residual itself.
+
+    Where few bf16 rows meet many weights (linear_mx4_workspace_bytes is not 0) the rows are held as sums of 4-bit ones: every
+    value to 2^-24 of the largest in its block of 32 along K, or to 2^-129 where that is more, and a block with a NaN or an
+    infinity is NaN.  A value that much smaller than its neighbours loses bits there; elsewhere rows are taken as they are."""
     quantized = isinstance(X, MX4)
     if quantized:
         first, ldx, x = X.codes, 0, None

@@ -7,10 +7,10 @@
 //   * rows in 4 bits are that other side as they are: tiles of up to 128 rows from a multiple of 128 on (a scale tile);
 //   * rows in bf16 are first split into MS_PIECES 4-bit rows each (mx4_split_kernel): the nearest e2m1 value under the block's
 //     own scale, then the same for what is left, and so on.  A step leaves at most a quarter of the block's largest value, so
-//     12 pieces hold every value of a block of 32 to 2^-24 of the largest one in it: f32's own rounding.  A row is 12
-//     columns of the accumulator, which the epilogue adds up.  The products cost four times the rate of bf16 ones, and the
-//     weights, which are what there is to read, need no decoding (in registers 2 instructions a weight, which costs
-//     mx4_few.cu 2.3 times the bytes' time on 8 experts of 4096 x 14336).
+//     12 pieces hold every value of a block of 32 to 2^-24 of the largest one in it, f32's own rounding (or to 2^-129: no
+//     scale is below 2^-127).  A row is 12 columns of the accumulator, which the epilogue adds up.  The products run at four
+//     times the rate of bf16 ones, and the weights, which are what there is to read, need no decoding (in registers 2
+//     instructions a weight, which costs mx4_few.cu 2.3 times the bytes' time on 8 experts of 4096 x 14336).
 // Bound by the weights' bytes: 8 experts of 4096 x 14336 gated, 32 bf16 rows 84 us (5.9 TB/s of weights); 64 rows in 4 bits
 // through 8192 x 28672 gated 44.5 us (5.6 TB/s).  Few columns leave SMs idle: 4096 x 4096 takes 9 us, 32 SMs at work.  The split
 // costs 3 us of latency, of which the ring's first weights hide a part (1 x 4096 x 14336 gated 15.8 -> 13.2 us).

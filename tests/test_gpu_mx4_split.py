@@ -65,3 +65,22 @@ def test_rows_of_many_sizes_come_back():
             X[:, lo:lo + 32] = 0.0
             X[:, lo] = 1.0
         _check(T, K, N, groups, glu, X)
+
+
+@pytest.mark.parametrize("e", [-104, -110, -121, -126])
+def test_small_rows_are_held_to_half_the_smallest_step(e):
+    T, K, N, groups, glu, _ = _cases()[0]
+    X = np.ldexp(np.random.default_rng(-e).normal(size=(T, K)), e)
+    X = torch.from_numpy(X).to(BF16).double().numpy()
+    base = torch.zeros((T, (K + 7) // 8 * 8), dtype=BF16, device=DEV)
+    base[:, :K] = torch.from_numpy(X).to(DEV)
+    at = torch.arange(N, device=DEV) * 37 % K
+    w = torch.zeros((N, K), dtype=BF16, device=DEV)
+    w[torch.arange(N, device=DEV), at] = 2.0 ** 40                     # so that no result is small
+    assert not glu and not groups
+    Y = eref.f64(b.linear_mx4(base[:, :K], b.mx4_quantize(w))) * 2.0 ** -40
+    b.linear_status()
+    k = at.cpu().numpy()
+    bound = np.maximum(2.0 ** -24 * s.block_max(X)[:, k], 2.0 ** -129)
+    bound = bound + 2.0 ** -8 * (np.abs(X[:, k]) + bound)
+    assert np.all(np.abs(Y - X[:, k]) <= bound)
