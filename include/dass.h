@@ -65,7 +65,7 @@ typedef enum {
 typedef enum { DASS_BF16 = 0, DASS_F32 = 1 } dass_dtype;
 typedef enum {
     DASS_ACT_SILU = 0, DASS_ACT_GELU_TANH = 1, DASS_ACT_RELU = 2,
-    DASS_ACT_NONE = 3                                   /* dass_linear only */
+    DASS_ACT_NONE = 3                                   /* dass_linear and dass_linear_mx4 only */
 } dass_act;
 /* Which matrix axis an index runs along: ROWS = the row index varies, COLS = the column index varies. */
 typedef enum { DASS_AXIS_ROWS = 0, DASS_AXIS_COLS = 1 } dass_axis;

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libdass.so")
 
 OK = 0
 BF16, F32 = 0, 1
-ACT_SILU, ACT_GELU_TANH, ACT_RELU, ACT_NONE = 0, 1, 2, 3      # ACT_NONE: linear() only
+ACT_SILU, ACT_GELU_TANH, ACT_RELU, ACT_NONE = 0, 1, 2, 3      # ACT_NONE: linear() and linear_mx4() only
 AXIS_ROWS, AXIS_COLS = 0, 1
 ROUTE_CHOSEN, ROUTE_ALL = 0, 1
 ACT_BY_NAME = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "relu": ACT_RELU}

@@ -32,8 +32,8 @@ __device__ __forceinline__ float mx4_scale(uint32_t s)
 
 // Decoding to bf16.  The 3 bits below the sign of a code, put where bf16 has the last two bits of its exponent and the
 // first of its mantissa, are the code's value times 2^-126 (a subnormal where the code is one): one exact product with
-// 2^(s - 1) gives the value.  For s up to 128 that factor is a bf16 itself; larger scales, which no matrix below 2^129 in
-// size has, take two products.
+// 2^(s - 1) gives the value.  For s up to 128 that factor is a bf16 itself; scales above 2, which blocks have whose largest
+// value is 16 or more, take two products (1 x 4096 x 4096 with all of its scales above 2: 7.0 us instead of 6.7).
 struct Mx4Factor { uint32_t first, second; };              // bf16 pairs; second is used where `two`
 __device__ __forceinline__ bool mx4_two(uint32_t s) { return s > 128u && s < 255u; }
 __device__ __forceinline__ Mx4Factor mx4_factor(uint32_t s)

@@ -10,7 +10,7 @@
 //
 // 32 weight rows a block (MT = 2) halve the traffic of X from L2, which in bf16 has four times the bytes of a weight's.
 //
-// Bound by the decoding, 17 instructions for 8 codes in a thread: 5.4 weights a ns (8 experts of 4096 x 14336 gated, 32 rows:
+// Bound by the decoding, 17 instructions for 8 codes in a thread: 5400 weights a ns (8 experts of 4096 x 14336 gated, 32 rows:
 // 174 us where the bytes take 76 and mx4_mid.cu 84), and for small products by the launch and the latency of a few turns:
 // 1 x 4096 x 4096 6.8 us (the bytes: 1.4), 1 x 1000 x 689 3.5 us.
 #include "linear_tc.cuh"

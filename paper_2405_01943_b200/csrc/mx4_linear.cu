@@ -16,13 +16,16 @@ struct Mx4Sizes { int64_t T, K, N, groups; bool grouped, glu, quantized; };
 
 // Which kernel a product takes: the shortest estimate, in microseconds, of a model fitted to measurements on a B200 (rows 1 ..
 // 4096, K 64 .. 14336, N 33 .. 28672, dense and per expert): on 160 such shapes, 110 of them random, the choice costs 3.5 % over
-// the best kernel, tile and split on average, at worst 1.95 times (short contractions).  Every kernel has a start, then
-//   mx4_few.cu    decodes every weight once per 8, 16 or 32 rows, at 5.4, 4.2 or 2.3 (gated, bf16 rows: 1.6) weights a ns;
+// the best kernel, tile and split on average.  Of the three worst, 1.95 and 1.72 times, two have a k below 300; 1.64 times is
+// 775 uneven rows of 5 experts at k = 2488, which take tiles of 64 rows where 128 are best; 17 more are 1.2 to 1.25 or less
+// (few rows at any k, where a split or a tile less would do, and gated 4-bit rows of a short k).  Every kernel has a start, then
+//   mx4_few.cu    decodes every weight once per 8, 16 or 32 rows, at 5400, 4200 or 2300 (gated, bf16 rows: 1600) weights a ns;
 //   mx4_mid.cu    works off stages of 256 k, one item of 128 columns (of each matrix) to an SM at a time, no faster than
 //                 5.8 TB/s of weights; bf16 rows are split first, and 4, 8 or 10 of them make a tile;
 //   mx4_tc.cu     the same with tiles of 256 rows and 256 (gated: 128) or 128 columns to a CTA pair;
 //   mx4_wide.cu   slabs of 64 k, tiles of 64, 128 or 256 rows and 256 columns to a CTA pair.
-// It goes by the rows of an average expert, since the host does not know the offsets.
+// It goes by the rows of an average expert, since the host does not know the offsets, and has no term for uneven loads but half a
+// tile a group.
 static double mx4_rounds(double items, double at_a_time) { return items <= at_a_time ? 1.0 : (double)(int64_t)(items / at_a_time + 0.999); }
 
 static Mx4Plan mx4_plan(const Mx4Sizes &z)

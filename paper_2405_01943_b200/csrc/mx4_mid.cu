@@ -12,8 +12,9 @@
 //     times the rate of bf16 ones, and the weights, which are what there is to read, need no decoding (in registers 2
 //     instructions a weight, which costs mx4_few.cu 2.3 times the bytes' time on 8 experts of 4096 x 14336).
 // Bound by the weights' bytes: 8 experts of 4096 x 14336 gated, 32 bf16 rows 84 us (5.9 TB/s of weights); 64 rows in 4 bits
-// through 8192 x 28672 gated 44.5 us (5.6 TB/s).  Few columns leave SMs idle: 4096 x 4096 takes 9 us, 32 SMs at work.  The split
-// costs 3 us of latency, of which the ring's first weights hide a part (1 x 4096 x 14336 gated 15.8 -> 13.2 us).
+// through 8192 x 28672 gated 44.5 us (5.6 TB/s).  Few columns leave SMs idle: 64 rows in 4 bits through 4096 x 4096 take 9 us, 32 SMs
+// at work, in bf16 18.  The split costs 3 us of latency, of which the ring's first weights hide a part (1 x 4096 x 14336 gated 15.8
+// -> 13.2 us).
 //   warp 0  TMA;  warp 1  TMEM, scale copies and MMAs;  warps 2..9  epilogue: a thread has one column of Y, the two warps of a
 //           quarter of the TMEM lanes take its rows in turn
 //

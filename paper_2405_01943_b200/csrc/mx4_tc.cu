@@ -16,8 +16,9 @@
 // multiple of 128 at or below its first row and store its own rows alone.
 //
 // Bound by the tensor pipe, and by the accumulator's way out: 8192^3 190 us (5.8 PFLOP/s), of a tile's 19000 cycles about 2000
-// between the last product of one tile and the first of the next; 16384 rows of 8 experts 4096 x 14336 gated 815 to 830 us
-// (4.7 PFLOP/s; K is half as long, and an expert's first and last tiles are part empty).  The scale copies cost 3 %.
+// between the last product of one tile and the first of the next (181 at best; with a bias 183, a residual 192, both 216; in
+// a loop of seconds, where power sets the clocks, 219 without both and 242 with); 16384 rows of 8 experts 4096 x 14336 gated
+// 786 to 876 us (4.4 to 4.9 PFLOP/s; K is half as long, and an expert's first and last tiles are part empty).  The scale copies cost 3 %.
 //
 // Every wait is bounded, as in linear_tc.cu.
 #include "linear_tc.cuh"

@@ -15,7 +15,9 @@
 // bf16 results there, hands it back, and stores under the next tile's products.
 // A decoded slab takes 300 cycles of the integer pipe and its products 512 at NT = 256, so those bound: 8192^3 680 to 690 us (1.6
 // PFLOP/s, bf16 weights in linear_tc.cu 868), 2048 x 4096 x 11008 121 us.  In the GLU form two matrices are decoded for the
-// same 512 cycles, at NT = 128, and the decoding bounds: 2048 x 4096 x 14336 415 us (1.16 PFLOP/s).
+// same 512 cycles, at NT = 128, and the decoding bounds: 2048 x 4096 x 14336 415 to 480 us (1.0 to
+// 1.16 PFLOP/s).  A residual costs 5 us of 119 at 2048 x 4096 x 11008, a bias nothing; in a loop of seconds, where power sets
+// the clocks, 146 us without both and 152 with.
 // Of the steps here, in us at 2048 x 4096 x 11008: two decoding warpgroups 246; a slab announced while the next is decoded,
 // without a release at cluster scope 153; epilogue in short loops 134; barriers asked for ahead of their use 131; a stage's
 // codes loaded at once 121.

@@ -7,7 +7,8 @@
 // of every token it meets: the column sums stay in its registers over all of its tokens, and nothing but the row's
 // maximum and sum crosses lanes.  At the end the groups of a block add up, then the 8 blocks of a cluster, which
 // writes one row of partial sums, and a second kernel adds the rows, all in a fixed order.  Small calls are one cluster and
-// one launch.  Choices are counted in shared memory; integer sums do not depend on their order.
+// one launch.  Choices are counted in shared memory; integer sums do not depend on their order.  Sums of probabilities are in
+// f32: a mean over 65536 tokens is off by 1.3e-7 of itself at most; added up in 64 bits, f32 probabilities leave 0.6e-7.
 //
 // Bound by latency: 65536 x 128 f32, k = 8 18.8 us for the loss (its bytes: 5.4), of which the second kernel takes 3.7, and 14.0
 // for the gradient (10.5): four rounds of loads, softmax and sums a warp.  Loads taken one by one 52, a row's loads together

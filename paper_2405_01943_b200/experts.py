@@ -102,6 +102,8 @@ class ExpertLayer:
     def router_gradient(self, dY: torch.Tensor, saved: Saved, balance: float = 0.0, counts: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Gradient of the router's logits [T x E] from that of the layer's output, the experts held fixed, plus ``balance``
         times that of the balance loss.  ``counts`` are the batch's own unless given (summed over several batches or ranks).
+        For bfloat16 logits the two are each rounded to bfloat16, as every gradient of them is: the first before the second is
+        added, the sum once more.
         (Through the router's product it is dWr = dlogits^T X, and dlogits Wr for the layer's input.)"""
         r = saved.routed
         _, dweight = b.expert_combine_backward(dY, saved.Ys, r.slot, r.weight, want_rows=False)
