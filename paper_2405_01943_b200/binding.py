@@ -254,18 +254,21 @@ def _new(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> Callable[..., 
 
 
 # torch's allocation of a dense tensor on the current device from its sizes, strides and dtype, without the general dispatch: 0.9
-# instead of 2 us, of which a call of the section below has up to three.  None where a torch version has no such function.  It
+# instead of 2 us, of which a call of the section below has up to four.  None where a torch version has no such function.  It
 # passes by what the dispatch does on request: other modes' allocation and the filling of new memory under deterministic
-# algorithms; where either is on, _empty takes the general way, as the calls above do.
+# algorithms; where either is on, outputs are made the general way, as those of the calls above.
 _cuda_empty = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
 _dispatch_modes = getattr(torch._C, "_len_torch_dispatch_stack", lambda: 1)
+_deterministic = getattr(torch._C, "_get_deterministic_algorithms", torch.are_deterministic_algorithms_enabled)      # the same, by its C name
 
 
-def _empty(t: torch.Tensor, stream: Optional[torch.cuda.Stream], shape: Tuple[int, ...], strides: Tuple[int, ...], dtype: torch.dtype) -> torch.Tensor:
-    """An output of a call on `stream` with tensor t, whose device is the current one (_stream_of has seen to that)."""
-    if stream is None and _cuda_empty is not None and type(t) is torch.Tensor and not _dispatch_modes() and not torch.are_deterministic_algorithms_enabled():
-        return _cuda_empty(shape, strides, dtype)
-    return _new(t, stream)(shape, dtype=dtype)
+def _maker(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> Callable[[Tuple[int, ...], Tuple[int, ...], torch.dtype], torch.Tensor]:
+    """What makes outputs (of sizes, strides and dtype) of a call on `stream` with tensor t, whose device is the current one
+    (_stream_of has seen to that)."""
+    if stream is None and _cuda_empty is not None and type(t) is torch.Tensor and not _dispatch_modes() and not _deterministic():
+        return _cuda_empty
+    new = _new(t, stream)
+    return lambda shape, strides, dtype: new(shape, dtype=dtype)
 
 
 def _workspace(t: torch.Tensor, device: torch.device) -> None:
@@ -869,21 +872,22 @@ def route_balance(logits: torch.Tensor, expert: torch.Tensor, loss: Optional[tor
     dt, dev, handle = _code(logits), logits.device, _stream_of(logits, stream)
     k = expert.shape[1] if expert.dim() == 2 else -1
     ids = _same(expert, "expert", (T, k), torch.int32, dev)
+    make = _maker(logits, stream)
     if loss is None:
-        loss = _empty(logits, stream, (), (), torch.float32)
+        loss = make((), (), torch.float32)
     else:
         _same(loss, "loss", (), torch.float32, dev)
     if counts is None:
-        counts = _empty(logits, stream, (E + 1,), (1,), torch.int32)
+        counts = make((E + 1,), (1,), torch.int32)
     else:
         _same(counts, "counts", (E + 1,), torch.int32, dev)
     if share is None:
-        share = _empty(logits, stream, (E,), (1,), torch.float32)
+        share = make((E,), (1,), torch.float32)
     else:
         _same(share, "share", (E,), torch.float32, dev)
     if workspace is None:
         need = _balance_bytes(T, E)
-        workspace = _empty(logits, stream, (need,), (1,), torch.uint8) if need else None
+        workspace = make((need,), (1,), torch.uint8) if need else None
     else:
         _workspace(workspace, dev)
     _check(load().dass_route_balance(logits.data_ptr(), T, E, ld, dt, ids, k, loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
@@ -905,7 +909,7 @@ def route_balance_backward(logits: torch.Tensor, expert: torch.Tensor, counts: t
     lda = _like(add, "add", T, E, logits) if add is not None else 0
     handle = _stream_of(logits, stream)
     if dlogits is None:
-        dlogits, ldd = _empty(logits, stream, (T, E), (E, 1), logits.dtype), E
+        dlogits, ldd = _maker(logits, stream)((T, E), (E, 1), logits.dtype), E
     else:
         ldd = _like(dlogits, "dlogits", T, E, logits)
     _check(load().dass_route_balance_backward(logits.data_ptr(), T, E, ld, dt, ids, k, load_, scale, _ptr(add), lda, dlogits.data_ptr(),
@@ -970,8 +974,8 @@ def mx4_quantize(X: torch.Tensor, out: Optional[MX4] = None, stream: Optional[to
     handle = _stream_of(X, stream)
     if out is None:
         codes, scales, code_strides, scale_strides = _mx4_shapes(shape[:-1], cols)
-        c = _empty(X, stream, codes, code_strides, torch.uint8)
-        s = _empty(X, stream, scales, scale_strides, torch.uint8)
+        make = _maker(X, stream)
+        c, s = make(codes, code_strides, torch.uint8), make(scales, scale_strides, torch.uint8)
         out = MX4(c, s, cols)
         codes, scales = c.data_ptr(), s.data_ptr()
     elif out.shape != shape:
@@ -994,7 +998,7 @@ def mx4_dequantize(Q: MX4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     lead = first.shape[:-1]
     G, rows = (lead[0], lead[1]) if len(lead) == 2 else (1, lead[0])
     if out is None:
-        out = _empty(first, stream, (*lead, cols), (rows * cols, cols, 1) if len(lead) == 2 else (cols, 1), dtype)
+        out = _maker(first, stream)((*lead, cols), (rows * cols, cols, 1) if len(lead) == 2 else (cols, 1), dtype)
     elif out.shape != (*lead, cols) or out.dtype != dtype or out.device != first.device or (out.stride(-1) != 1 and cols > 1):
         raise ValueError("out must be a tensor of Q's shape and device and of the dtype asked for, with unit stride along its columns")
     strides, dt = out.stride(), _code(out)
@@ -1090,12 +1094,13 @@ def linear_mx4(X: Union[torch.Tensor, MX4], W: MX4, bias: Optional[torch.Tensor]
         else:
             res, ldr = t.data_ptr(), ld
     handle = _stream_of(first, stream)
+    make = _maker(first, stream)
     if Y is None:
-        Y, ldy = _empty(first, stream, (T, N), (N, 1), dtype), N
+        Y, ldy = make((T, N), (N, 1), dtype), N
     if T:
         if workspace is None:
             need = _linear_mx4_bytes(index, T, K, N, groups, offsets is not None, W_up is not None, quantized)
-            workspace = _empty(first, stream, (need,), (1,), torch.uint8) if need else None
+            workspace = make((need,), (1,), torch.uint8) if need else None
         else:
             _workspace(workspace, device)
         _check(load().dass_linear_mx4(x, ldx, xc, xs, T, K, wc, ws, uc, us, N, b, bu, act, res, ldr, Y.data_ptr(), ldy, edges,

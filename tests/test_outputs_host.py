@@ -17,7 +17,7 @@ def direct(monkeypatch):
 
 
 def _made():
-    return b._empty(torch.zeros(4), None, (3, 2), (2, 1), torch.float32)
+    return b._maker(torch.zeros(4), None)((3, 2), (2, 1), torch.float32)
 
 
 def test_new_memory_is_filled_under_deterministic_algorithms(direct):
@@ -80,7 +80,7 @@ def test_quantisation_allocates_what_the_library_fills(monkeypatch, dims, rows, 
         x = X.as_subclass(_Device)
         with monkeypatch.context() as m:
             if direct:
-                m.setattr(b, "_empty", lambda t, stream, shape, strides, dtype: empty(shape, strides, dtype))
+                m.setattr(b, "_maker", lambda t, stream: empty)
             q = b.mx4_quantize(x)
         assert bool(asked) == direct
         assert q.codes.numel() == G * codes.value and q.scales.numel() == G * scales.value and q.shape == X.shape
