@@ -381,7 +381,7 @@ static cudaError_t rb_go(const BalanceArgs &a)
         return cudaGetLastError();
     }
     const size_t smem = ((size_t)(RB_THREADS / 32) * a.E + 2 * (a.E + 1)) * 4;   // at most 72 KB
-    if (smem > 48 * 1024) {                                                      // E above 682
+    if (smem > 47 * 1024) {                                                      // E above 668; rb_finish's static 128 bytes count too
         static DeviceMask configured{0ull};                                      // per device
         const cudaError_t e = ensure_dynamic_smem(route_balance_kernel<BF16, W, V, L, FULL>, 72 * 1024 + 8, configured);
         if (e != cudaSuccess) return e;
